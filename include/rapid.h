@@ -348,6 +348,61 @@ int rapid_verify_attention_paged(const void* q, const void* k_pool, const void* 
                                  void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /*
+ * Verify attention of a batch whose sequences share a long prefix (several requests, or several
+ * drafts, over one document: Section 3.1's long-document tasks).  The prefix's K/V are stored once
+ * and read once for the whole batch, instead of once per sequence.
+ *
+ * For every sequence b, query head h (KV head g = h / (Hq/Hkv)) and row i:
+ *   out[b,i,h,:] = softmax-weighted sum of the values of the *prefix_len prefix keys (every row sees them all)
+ *                  and of the keys 0 <= j <= ctx_lens[b] - R + i of sequence b's own cache.
+ * It equals rapid_verify_attention over each sequence's prefix and own keys written one behind the other.
+ *
+ *   k_prefix, v_prefix : device [Hkv, Pmax, D] bf16, D contiguous, geometry of `prefix`; entries at positions
+ *                        >= *prefix_len are never used, whatever their bits
+ *   prefix_len         : device int32, in [0, Pmax]
+ *   k_cache, v_cache   : device, the sequences' own keys, geometry of `shape` (strides honoured)
+ *   ctx_lens           : device int32 [B]: OWN keys of every sequence, the R newest included, in [R, Lmax]
+ *   params             : host, may be NULL; scale, num_ctas (at most 256), lse_out, out_f32 (16-byte aligned),
+ *                        split_done_event and wait_cycle_limit apply, anything else set is RAPID_ERR_UNSUPPORTED
+ *   workspace          : device, >= rapid_prefix_attention_workspace_bytes(), initialised
+ * D is 64 or 128, (Hq/Hkv) * R at most 128, B * Hkv at most 65,535; B * R may be large (thousands of rows
+ * per KV head).  A length out of its range is clamped and sets RAPID_STATUS_BAD_CTX_LEN.  lse_out is within
+ * 1e-4 of the exact value.  A value that is not finite in a V entry that some row sees reaches every row of
+ * that key's tile that the same product holds.  Two kernels per call; lengths are read on the device, so a
+ * captured call follows them.
+ */
+typedef struct rapid_prefix_kv {
+    int64_t Pmax;     /* capacity in keys                     */
+    int64_t stride_h; /* elements; 0 = dense, Pmax * stride_l */
+    int64_t stride_l; /* elements; 0 = D                      */
+} rapid_prefix_kv;
+
+/* Bytes of scratch the two calls below need (0 on invalid arguments; shape->Lmax and strides do not matter). */
+size_t rapid_prefix_attention_workspace_bytes(const rapid_attn_shape* shape, int gamma);
+
+int rapid_verify_attention_prefix(const void* q, const void* k_prefix, const void* v_prefix,
+                                  const rapid_prefix_kv* prefix, const int32_t* prefix_len,
+                                  const void* k_cache, const void* v_cache, const int32_t* ctx_lens,
+                                  int gamma, void* out, const rapid_attn_shape* shape,
+                                  const rapid_attn_params* params, void* workspace, size_t workspace_bytes,
+                                  void* cuda_stream);
+
+/*
+ * The same over a paged cache (see rapid_paged_kv) in which the sequences' first blocks are the same physical
+ * blocks: the first *prefix_len keys of EVERY sequence are read through row 0 of block_table, once for
+ * the batch; *prefix_len is rounded down to whole blocks (what is left over is read through each
+ * sequence's own entries).  Arguments, table and ctx_lens are those of rapid_verify_attention_paged (ctx_lens[b]
+ * counts ALL keys of sequence b, the prefix included, and must lie in [*prefix_len + R, Lmax]), and so is the
+ * result.  A prefix that does not leave room for R keys is shortened and sets RAPID_STATUS_BAD_CTX_LEN.
+ */
+int rapid_verify_attention_prefix_paged(const void* q, const void* k_pool, const void* v_pool,
+                                        const int32_t* block_table, const rapid_paged_kv* paged,
+                                        const int32_t* prefix_len, const int32_t* ctx_lens, int gamma,
+                                        void* out, const rapid_attn_shape* shape,
+                                        const rapid_attn_params* params, void* workspace,
+                                        size_t workspace_bytes, void* cuda_stream);
+
+/*
  * Accept / residual (Algorithm 1, validation loop and residual step;
  * Eq. (new_target); Section 2.4).
  *

@@ -29,6 +29,7 @@ EXPORTS = [
     "rapid_verify_step_host", "rapid_verify_step_host_arena_bytes", "rapid_kv_append", "rapid_kv_append_paged", "rapid_step_commit",
     "rapid_last_error",
     "rapid_version", "rapid_kernel_launch_count", "rapid_kernel_launch_count_reset",
+    "rapid_prefix_attention_workspace_bytes", "rapid_verify_attention_prefix", "rapid_verify_attention_prefix_paged",
 ]
 
 
@@ -48,6 +49,10 @@ class _PagedKv(ctypes.Structure):
     _fields_ = [("block_size", ctypes.c_int32), ("num_blocks", ctypes.c_int32),
                 ("max_blocks_per_seq", ctypes.c_int32), ("reserved", ctypes.c_int32),
                 ("stride_block", ctypes.c_int64), ("stride_h", ctypes.c_int64), ("stride_l", ctypes.c_int64)]
+
+
+class _PrefixKv(ctypes.Structure):
+    _fields_ = [("Pmax", ctypes.c_int64), ("stride_h", ctypes.c_int64), ("stride_l", ctypes.c_int64)]
 
 
 class _AttnParams(ctypes.Structure):
@@ -148,6 +153,13 @@ def load_library():
                                                  ctypes.POINTER(_LaunchInfo)]
         lib.rapid_verify_attention_paged.restype = i32
         lib.rapid_verify_attention_paged.argtypes = [vp, vp, vp, vp, ctypes.POINTER(_PagedKv)] + attn_args[3:] + [vp, sz, vp]
+        lib.rapid_prefix_attention_workspace_bytes.restype = sz
+        lib.rapid_prefix_attention_workspace_bytes.argtypes = [ctypes.POINTER(_AttnShape), i32]
+        attn_tail = [vp, i32, vp, ctypes.POINTER(_AttnShape), ctypes.POINTER(_AttnParams), vp, sz, vp]
+        lib.rapid_verify_attention_prefix.restype = i32
+        lib.rapid_verify_attention_prefix.argtypes = [vp, vp, vp, ctypes.POINTER(_PrefixKv), vp, vp, vp] + attn_tail
+        lib.rapid_verify_attention_prefix_paged.restype = i32
+        lib.rapid_verify_attention_prefix_paged.argtypes = [vp, vp, vp, vp, ctypes.POINTER(_PagedKv), vp] + attn_tail
         lib.rapid_draft_sample.restype = i32
         lib.rapid_draft_sample.argtypes = [vp, vp, f32, vp, vp, vp, i32, i64, i64, vp, sz, vp]
         lib.rapid_retrieval_select.restype = i32
@@ -379,6 +391,79 @@ def rapid_verify_attention_paged(q, k_pool, v_pool, block_table, ctx_lens, gamma
                                                        ctypes.byref(paged), _p(ctx_lens), gamma, _p(out),
                                                        ctypes.byref(shape), _attn_params(params), _p(workspace),
                                                        _nbytes(workspace), _stream_ptr(stream)))
+
+
+def prefix_attention_workspace_bytes(B, Hq, Hkv, D, gamma) -> int:
+    """Scratch of rapid_verify_attention_prefix and rapid_verify_attention_prefix_paged."""
+    s = _AttnShape(B, Hq, Hkv, D, gamma + 1, 0, 0, 0)
+    return int(load_library().rapid_prefix_attention_workspace_bytes(ctypes.byref(s), gamma))
+
+
+def _check_prefix_call(q, out, kv, ctx_lens, prefix_len, gamma, params):
+    if any(t.dtype != torch.bfloat16 for t in (q, out, *kv)) or ctx_lens.dtype != torch.int32 \
+            or prefix_len.dtype != torch.int32:
+        raise TypeError("q, out and the caches must be bfloat16, ctx_lens and prefix_len int32")
+    if q.dim() != 4 or not (q.is_contiguous() and out.is_contiguous()) or q.shape[1] != gamma + 1 or out.shape != q.shape:
+        raise ValueError("q and out must be dense [B, gamma+1, Hq, D]")
+    if ctx_lens.numel() != q.shape[0] or not ctx_lens.is_contiguous() or prefix_len.numel() != 1:
+        raise ValueError("ctx_lens must be dense [B] and prefix_len hold one length")
+    if params is not None:
+        for t, n in ((params.lse_out, q.numel() // q.shape[3]), (params.out_f32, q.numel())):
+            if t is not None and (t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous()):
+                raise ValueError("lse_out must be dense float32 [B, gamma+1, Hq] and out_f32 [B, gamma+1, Hq, D]")
+    _check_device(q, out, *kv, ctx_lens, prefix_len)
+
+
+def _check_device(*tensors):
+    """The library launches on the current device: every tensor has to live there."""
+    here = torch.cuda.current_device() if torch.cuda.is_available() else None
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != here):
+            raise ValueError("every tensor must be on the current CUDA device")
+
+
+def rapid_verify_attention_prefix(q, k_prefix, v_prefix, prefix_len, k_cache, v_cache, ctx_lens, gamma, out, workspace,
+                                  params: Optional[AttnParams] = None, stream=None) -> None:
+    """Verify attention of a batch over a prefix that is stored once (k_prefix / v_prefix [Hkv, Pmax, D], of which
+    prefix_len [1] keys count) and each sequence's own keys (k_cache / v_cache [B, Hkv, Lmax, D], ctx_lens [B] of
+    them, the gamma+1 newest included).  bf16; caches may be strided with a contiguous head_dim."""
+    _check_prefix_call(q, out, (k_prefix, v_prefix, k_cache, v_cache), ctx_lens, prefix_len, gamma, params)
+    if k_cache.stride() != v_cache.stride() or k_cache.shape != v_cache.shape or k_cache.dim() != 4:
+        raise ValueError("k_cache and v_cache must share shape [B, Hkv, Lmax, D] and strides")
+    if k_prefix.stride() != v_prefix.stride() or k_prefix.shape != v_prefix.shape or k_prefix.dim() != 3:
+        raise ValueError("k_prefix and v_prefix must share shape [Hkv, Pmax, D] and strides")
+    if k_prefix.stride(2) != 1 or k_prefix.shape[0] != k_cache.shape[1] or k_prefix.shape[2] != q.shape[3]:
+        raise ValueError("the prefix must have the cache's KV heads and a contiguous head_dim")
+    shape = _attn_shape(q, k_cache)
+    prefix = _PrefixKv(k_prefix.shape[1], k_prefix.stride(0), k_prefix.stride(1))
+    _check(load_library().rapid_verify_attention_prefix(
+        _p(q), _p(k_prefix), _p(v_prefix), ctypes.byref(prefix), _p(prefix_len), _p(k_cache), _p(v_cache), _p(ctx_lens),
+        gamma, _p(out), ctypes.byref(shape), _attn_params(params), _p(workspace), _nbytes(workspace),
+        _stream_ptr(stream)))
+
+
+def rapid_verify_attention_prefix_paged(q, k_pool, v_pool, block_table, prefix_len, ctx_lens, gamma, out, workspace,
+                                        params: Optional[AttnParams] = None, stream=None) -> None:
+    """rapid_verify_attention_paged for sequences whose first prefix_len [1] keys lie in the same blocks: those are
+    read once for the batch, through row 0 of block_table.  ctx_lens counts all keys, the prefix included."""
+    _check_prefix_call(q, out, (k_pool, v_pool), ctx_lens, prefix_len, gamma, params)
+    if k_pool.stride() != v_pool.stride() or k_pool.shape != v_pool.shape or k_pool.dim() != 4 or k_pool.stride(3) != 1:
+        raise ValueError("k_pool and v_pool must share shape and strides, with a contiguous head_dim")
+    if block_table.dtype != torch.int32:
+        raise TypeError("block_table must be int32")
+    B, _, Hq, D = q.shape
+    if not block_table.is_contiguous() or block_table.dim() != 2 or block_table.shape[0] != B:
+        raise ValueError("block_table must be dense [B, max_blocks_per_seq]")
+    _check_device(block_table)
+    nb, Hkv, bs, Dk = k_pool.shape
+    if Dk != D:
+        raise ValueError("q and k_pool disagree on head_dim")
+    mb = block_table.shape[1]
+    shape = _AttnShape(B, Hq, Hkv, D, mb * bs, 0, 0, 0)
+    paged = _PagedKv(bs, nb, mb, 0, k_pool.stride(0), k_pool.stride(1), k_pool.stride(2))
+    _check(load_library().rapid_verify_attention_prefix_paged(
+        _p(q), _p(k_pool), _p(v_pool), _p(block_table), ctypes.byref(paged), _p(prefix_len), _p(ctx_lens), gamma,
+        _p(out), ctypes.byref(shape), _attn_params(params), _p(workspace), _nbytes(workspace), _stream_ptr(stream)))
 
 
 def rapid_draft_sample(draft_logits, uniforms, temperature, out_token, out_logq, workspace, out_row_stats=None,

@@ -274,6 +274,38 @@ int rapid_verify_attention_paged(const void* q, const void* k_pool, const void* 
                                    block_table);
 }
 
+size_t rapid_prefix_attention_workspace_bytes(const rapid_attn_shape* shape, int gamma) {
+    return prefix_attention_workspace_bytes(shape, gamma);
+}
+
+int rapid_verify_attention_prefix(const void* q, const void* k_prefix, const void* v_prefix,
+                                  const rapid_prefix_kv* prefix, const int32_t* prefix_len,
+                                  const void* k_cache, const void* v_cache, const int32_t* ctx_lens,
+                                  int gamma, void* out, const rapid_attn_shape* shape,
+                                  const rapid_attn_params* params, void* workspace, size_t workspace_bytes,
+                                  void* cuda_stream) {
+    clear_error();
+    return launch_verify_attention_prefix(q, k_prefix, v_prefix, prefix, prefix_len, k_cache, v_cache, nullptr, nullptr,
+                                          ctx_lens, gamma, out, shape, params, workspace, workspace_bytes,
+                                          static_cast<cudaStream_t>(cuda_stream));
+}
+
+int rapid_verify_attention_prefix_paged(const void* q, const void* k_pool, const void* v_pool,
+                                        const int32_t* block_table, const rapid_paged_kv* paged,
+                                        const int32_t* prefix_len, const int32_t* ctx_lens, int gamma,
+                                        void* out, const rapid_attn_shape* shape,
+                                        const rapid_attn_params* params, void* workspace,
+                                        size_t workspace_bytes, void* cuda_stream) {
+    clear_error();
+    if (!paged || !block_table) {
+        set_error("rapid_verify_attention_prefix_paged: NULL paged geometry or block table");
+        return RAPID_ERR_INVALID_ARG;
+    }
+    return launch_verify_attention_prefix(q, nullptr, nullptr, nullptr, prefix_len, k_pool, v_pool, paged, block_table,
+                                          ctx_lens, gamma, out, shape, params, workspace, workspace_bytes,
+                                          static_cast<cudaStream_t>(cuda_stream));
+}
+
 int rapid_draft_sample(const float* draft_logits, const float* uniforms, float temperature, int32_t* out_token,
                        float* out_logq, float* out_row_stats, int32_t B, int64_t V, int64_t row_stride,
                        void* workspace, size_t workspace_bytes, void* cuda_stream) {

@@ -51,7 +51,7 @@ inline cudaError_t launch_dependent(void (*kernel)(KArgs...), dim3 grid, dim3 bl
 }
 #endif
 
-// internal launchers shared by the entry points (defined in attention.cu / accept.cu)
+// internal launchers shared by the entry points (defined in attention.cu / attention_prefix.cu / accept.cu / retrieval.cu)
 int launch_verify_attention(const void* q, const void* k_cache, const void* v_cache,
                             const int32_t* ctx_lens, int gamma, void* out,
                             const rapid_attn_shape* shape, const rapid_attn_params* params,
@@ -71,6 +71,14 @@ int launch_retrieval_select(const float* chunk_emb, const float* query_emb, cons
                             int32_t* sel_count, int32_t* status_word, cudaStream_t stream);
 int launch_merge_partials(const float* o_parts, const float* lse_parts, int P, int64_t rows, int D, void* out,
                           float* out_f32, float* lse_out, cudaStream_t stream);
+size_t prefix_attention_workspace_bytes(const rapid_attn_shape* s, int gamma);
+// paged == nullptr: prefix K/V apart from the own caches; else both in the pools k_cache / v_cache
+int launch_verify_attention_prefix(const void* q, const void* k_prefix, const void* v_prefix,
+                                   const rapid_prefix_kv* prefix, const int32_t* prefix_len, const void* k_cache,
+                                   const void* v_cache, const rapid_paged_kv* paged, const int32_t* block_table,
+                                   const int32_t* ctx_lens, int gamma, void* out, const rapid_attn_shape* shape,
+                                   const rapid_attn_params* params, void* workspace, size_t workspace_bytes,
+                                   cudaStream_t stream);
 int launch_accept(const float* target_logits, const float* draft_logits,
                   const int32_t* draft_tokens, const float* uniforms, float eta,
                   int32_t* out_accept_len, int32_t* out_next_token,
