@@ -41,11 +41,12 @@ namespace rapid {
 namespace {
 
 constexpr int kKeys = 128;             // keys per tile
-constexpr int kThreads = 384;          // two softmax groups of 128, then K/V producer, Q producer, QK^T, PV warps
+constexpr int kThreads = 352;          // two softmax groups of 128, then a warp each for K/V copies, Q copies, MMAs
 constexpr int kHalfBytes = kKeys * 128;  // one 64-column half of a tile of 128 rows
 constexpr int kPad = 3;                // single-stream tiles that a change of unit costs
 constexpr int kMaxPrefixCtas = 256;
-constexpr float kJump = 8.f;           // a maximum this far (log2) above a row's reference moves the reference
+constexpr float kJump = 40.f;          // a score this far (log2) above a row's reference moves it: probabilities stay below
+                                       // 2^40, far from the end of fp32's and bf16's range in any sum
 
 __host__ __device__ constexpr int k_slots(int D) { return D == 128 ? 2 : 4; }
 __host__ __device__ constexpr int v_slots(int D) { return D == 128 ? 3 : 6; }
@@ -70,151 +71,160 @@ struct PrefixArgs {
     int block_size, block_log2, num_blocks, max_blocks, box_rows;
     int rows_tile;               // (sequence, row) pairs in a row tile: 128 / G
     int nrt, np;                 // row tiles, pairs of row tiles
+    int max_teams, rounds;       // teams of np CTAs that the grid holds; passes over the prefix where np exceeds the grid
     int num_ctas;
     float scale_log2;
     long long wait_limit;
 };
 
-__device__ __forceinline__ int prefix_keys(const PrefixArgs& a) {
-    int P = *a.prefix_len;
+// Lengths as the device finds them, brought into range.
+__device__ __forceinline__ int clamp_prefix(const PrefixArgs& a, int P) {
     P = max(0, min(P, a.Pmax));
     if (a.block_table) P = min(P, a.Lmax - a.R) & ~(a.block_size - 1);  // whole blocks that leave room for the rows' own
     return P;
 }
-// A sequence's own keys (behind the prefix), brought into [R, capacity].
-__device__ __forceinline__ int own_keys(const PrefixArgs& a, int b, int P) {
-    int L = a.ctx_lens[b];
-    if (a.block_table) L -= P;
-    return max(a.R, min(L, a.block_table ? a.Lmax - P : a.Lmax));
+// A sequence's own keys (those behind the prefix) from its entry of ctx_lens.
+__device__ __forceinline__ int clamp_own(const PrefixArgs& a, int L, int P) {
+    const int before = a.block_table ? P : 0;  // keys that the entry counts too
+    return min(max(L, a.R + before), a.Lmax) - before;
 }
 __device__ __forceinline__ int tiles_of(int keys) { return (keys + kKeys - 1) / kKeys; }
 
 // What a CTA does, worked out by its first warp.
 struct Plan {
-    int P, nt, pad;         // prefix keys, tiles, and the virtual tiles in front of every KV head's
-    int team, pair, pairs;  // the CTA's team, its first pair, the step to its next (pairs < np only on a small grid)
-    int v0, v1;             // its range in the prefix's padded tile list; empty if it is in no team
-    int worker, s0, s1;     // its rank among the CTAs that hold own tiles, and its range in that padded list
-    int b, vb;              // the sequence s0 lies in, and where that sequence's tiles begin
+    int P, pad, span;      // prefix keys; virtual tiles in front of every KV head's, and those with the real ones
+    int team, pair, pairs;  // the CTA's team, its first pair (np: none), the step to its next
+    int h, o, len;         // its run of the prefix's padded tile list: KV head, offset in its span, length
+    int worker;            // its rank among the CTAs that hold own tiles
+    int own_b, own_h, own_o, own_len;  // its run of the own tiles' padded list
 };
 
-// Share i of n equal shares of `total`, the first total % n of them one larger.
-__device__ __forceinline__ int share_start(int total, int n, int i) {
-    const int base = total / n, more = total - base * n;
-    return i * base + min(i, more);
+// Where share i of n of `total` >= n begins; r = total / n, correctly rounded.  Never decreasing, and no share is
+// empty: r is 1, or at least 1 + 1/kMaxPrefixCtas, which the rounding of i * r cannot use up.
+__device__ __forceinline__ int share_start(int total, int n, float r, int i) {
+    return i >= n ? total : min(total, (int)((float)i * r));
+}
+// x / d for 0 <= x < 2^23 (a tile index of one sequence or one pass over the prefix, at most 2^31 / 128).
+__device__ __forceinline__ int small_div(int x, int d) {
+    int q = (int)__fdividef((float)x, (float)d);
+    if (q * d > x) --q;
+    if (x - q * d >= d) ++q;
+    return q;
 }
 
+// The length of the code matters as much as its running time: it is fetched anew by almost every launch.
 __device__ __noinline__ void make_plan(const PrefixArgs& a, int cta, Plan& out) {
     const int lane = threadIdx.x & 31;
-    Plan p;
-    p.P = prefix_keys(a);
-    p.nt = tiles_of(p.P);
+    const int given = *a.prefix_len;
+    const int first_len = lane < a.B ? a.ctx_lens[lane] : 0;  // (both loads are on their way before either is used)
+    const int P = clamp_prefix(a, given);
+    const int nt = tiles_of(P);
     int S = 0;
-    bool bad = false;  // lengths out of range: only the device can see them, the first CTA says so
+    bool bad = given != P && !(a.block_table && (given & ~(a.block_size - 1)) == P);
     for (int b = lane; b < a.B; b += 32) {
-        const int own = own_keys(a, b, p.P);
+        const int L = b < 32 ? first_len : a.ctx_lens[b];
+        const int own = clamp_own(a, L, P);
         S += a.Hkv * (tiles_of(own) + kPad);
-        bad |= a.ctx_lens[b] != own + (a.block_table ? p.P : 0);
+        bad |= L != own + (a.block_table ? P : 0);
     }
-    if (cta == 0) {
-        const int given = *a.prefix_len;
-        bad |= given != p.P && !(a.block_table && (given & ~(a.block_size - 1)) == p.P);
-        if (__any_sync(0xffffffffu, bad) && lane == 0) atomicOr(a.status, RAPID_STATUS_BAD_CTX_LEN);
-    }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) S += __shfl_xor_sync(0xffffffffu, S, o);
+    S = __reduce_add_sync(0xffffffffu, S);
+    if (cta == 0 && __any_sync(0xffffffffu, bad) && lane == 0) atomicOr(a.status, RAPID_STATUS_BAD_CTX_LEN);
 
-    const int C = a.num_ctas;
-    const int npc = min(a.np, C);
-    const int rounds = (a.np + npc - 1) / npc;
+    const int C = a.num_ctas, npc = min(a.np, C);
+    const int rounds = a.rounds, two = a.nrt > 1 ? 2 : 1;
     // teams: the prefix's share of all work, at most what the grid holds, at least one
-    int T = 0, w = 0, wh = 0;  // w, wh: cost of a team's range for a full pair and for a single row tile
-    const int NP = a.Hkv * p.nt;
-    p.pad = 0;
+    const int NP = a.Hkv * nt;
+    const float level = fmaxf(1.f, __fdividef((float)(NP * a.nrt + S), (float)C));
+    int T = 0, pad = 0, w = 0, wh = 0;  // w, wh: cost of a team's range for a full pair and for a single row tile
     if (NP > 0) {
-        const long long all = (long long)NP * a.nrt + S;
-        const int level = (int)max(1LL, min(all / C, 0x3fffffffLL));
-        T = max(1, min(min(C / npc, NP), (int)(((long long)NP * (a.nrt > 1 ? 2 : 1) * rounds + level - 1) / level)));
-        if (NP >= 4 * T) p.pad = kPad;
-        const int range = (a.Hkv * (p.nt + p.pad) + T - 1) / T;
-        w = (a.nrt > 1 ? 2 : 1) * range * rounds;
-        wh = w;
+        T = max(1, min(min(a.max_teams, NP), (int)ceilf(__fdividef((float)NP * two * rounds, level))));
+        if (NP >= 4 * T) pad = kPad;
+        w = wh = (int)ceilf(__fdividef((float)(NP + a.Hkv * pad) * two * rounds, (float)T));
     }
-    const int NPv = a.Hkv * (p.nt + p.pad);
+    const int span = nt + pad, NPv = a.Hkv * span;
     const int n_team = T * npc;
     const bool half_class = T > 0 && (a.nrt & 1) && a.np > 1 && rounds == 1;  // each team has one CTA with a single row tile
     const int nH = half_class ? T : 0, nA = n_team - nH, nB = C - n_team;
-    if (half_class) wh = w / 2;
+    if (half_class) wh = w >> 1;
+    Plan p;
+    p.P = P;
+    p.pad = pad;
+    p.span = span;
     p.team = -1;
-    p.pair = 0;
+    p.pair = a.np;
     p.pairs = npc;
-    p.v0 = p.v1 = 0;
+    p.h = p.o = p.len = 0;
     if (cta < n_team) {
-        p.team = cta / npc;
+        p.team = small_div(cta, npc);
         p.pair = cta - p.team * npc;
-        p.v0 = share_start(NPv, T, p.team);
-        p.v1 = share_start(NPv, T, p.team + 1);
+        const float r = __fdiv_rn((float)NPv, (float)T);
+        const int v0 = share_start(NPv, T, r, p.team);
+        p.len = share_start(NPv, T, r, p.team + 1) - v0;
+        p.h = small_div(v0, span);
+        p.o = v0 - p.h * span;
     }
     // own tiles: fill the classes (no prefix work; a single row tile; a full pair) up to one level
-    int SB = 0, SH = 0, SA = 0;
     int left = S;
-    const int l1 = (int)min((long long)left, (long long)nB * (half_class ? wh : w));
-    SB = l1;
-    left -= l1;
-    if (left > 0 && nH > 0) {
-        const int l2 = (int)min((long long)left, (long long)(nB + nH) * (w - wh));
-        const int forH = (int)((long long)l2 * nH / (nB + nH));
-        SH += forH;
-        SB += l2 - forH;
+    int SB = min((float)left, (float)nB * wh) < (float)left ? nB * wh : left, SH = 0, SA = 0;
+    left -= SB;
+    if (nH > 0 && left > 0) {
+        const float room = (float)(nB + nH) * (w - wh);
+        const int l2 = room < (float)left ? (nB + nH) * (w - wh) : left;
+        SH = min(l2, (int)((float)l2 * __fdividef((float)nH, (float)(nB + nH))));
+        SB += l2 - SH;
         left -= l2;
     }
     if (left > 0) {
-        const int each = left / C;
+        int each = (int)__fdividef((float)left, (float)C);
+        if ((float)each * C > (float)left) --each;
         SB += each * nB;
         SH += each * nH;
-        SA = left - each * (nB + nH);
+        left -= each * (nB + nH);
+        if (nA > 0) SA = left;
+        else if (nB > 0) SB += left;
+        else SH += left;
     }
-    if (nB == 0 && SB > 0) {  // (nothing to give to an empty class)
+    if (nB == 0 && SB > 0) {  // (rounding's crumbs have no CTA to go to)
         SA += SB;
         SB = 0;
     }
-    if (nA == 0 && SA > 0) {  // no CTA carries a full pair
-        if (nB) SB += SA; else SH += SA;
-        SA = 0;
-    }
     // workers: the CTAs of class B, then H, then A, those without a share left out
-    int cls_n, cls_total, cls_rank, off_w, off_s;
-    const int usedB = min(nB, SB), usedH = min(nH, SH);
+    int n, total, rank, off_w, off_s;
     if (cta >= n_team) {
-        cls_n = nB, cls_total = SB, cls_rank = cta - n_team, off_w = 0, off_s = 0;
+        n = nB, total = SB, rank = cta - n_team, off_w = 0, off_s = 0;
     } else if (half_class && p.pair == a.np - 1) {
-        cls_n = nH, cls_total = SH, cls_rank = p.team, off_w = usedB, off_s = SB;
+        n = nH, total = SH, rank = p.team, off_w = min(nB, SB), off_s = SB;
     } else {
-        cls_n = nA, cls_total = SA, off_w = usedB + usedH, off_s = SB + SH;
-        cls_rank = half_class ? p.team * (npc - 1) + p.pair : cta;
+        n = nA, total = SA, off_w = min(nB, SB) + min(nH, SH), off_s = SB + SH;
+        rank = half_class ? p.team * (npc - 1) + p.pair : cta;
     }
-    p.worker = off_w + cls_rank;
-    p.s0 = off_s + share_start(cls_total, cls_n, cls_rank);
-    p.s1 = off_s + share_start(cls_total, cls_n, cls_rank + 1);
-    // the sequence s0 lies in
-    p.b = 0;
-    p.vb = 0;
-    if (p.s1 > p.s0) {
+    n = min(n, total);  // (fewer tiles than CTAs: one each)
+    p.worker = off_w + rank;
+    const float r = __fdiv_rn((float)total, (float)max(n, 1));
+    const int s0 = off_s + share_start(total, n, r, rank);
+    p.own_len = off_s + share_start(total, n, r, rank + 1) - s0;  // 0 from rank n on
+    // the unit s0 lies in
+    p.own_b = p.own_h = p.own_o = 0;
+    if (p.own_len > 0) {
         int base = 0;
         for (int b0 = 0; b0 < a.B; b0 += 32) {
             const int b = b0 + lane;
-            const int span = b < a.B ? a.Hkv * (tiles_of(own_keys(a, b, p.P)) + kPad) : 0;
-            int incl = span;
-#pragma unroll
+            int one = 0;
+            if (b < a.B) one = tiles_of(clamp_own(a, b0 ? a.ctx_lens[b] : first_len, P)) + kPad;
+            int incl = a.Hkv * one;
+#pragma unroll 1
             for (int o = 1; o < 32; o <<= 1) {
                 const int x = __shfl_up_sync(0xffffffffu, incl, o);
                 if (lane >= o) incl += x;
             }
-            const unsigned past = __ballot_sync(0xffffffffu, base + incl > p.s0 && b < a.B);
+            const unsigned past = __ballot_sync(0xffffffffu, base + incl > s0);
             if (past) {
                 const int src = __ffs(past) - 1;
-                p.b = b0 + src;
-                p.vb = base + __shfl_sync(0xffffffffu, incl - span, src);
+                const int x = s0 - base - __shfl_sync(0xffffffffu, incl - a.Hkv * one, src);
+                const int d = __shfl_sync(0xffffffffu, one, src);
+                p.own_b = b0 + src;
+                p.own_h = small_div(x, d);
+                p.own_o = x - p.own_h * d;
                 break;
             }
             base += __shfl_sync(0xffffffffu, incl, 31);
@@ -229,72 +239,137 @@ struct Segment {
     int b, kvh, pair;   // sequence (own) or pair of row tiles (prefix)
     int tile0, tiles;   // run of tiles inside the unit
     int keys;           // keys of the unit: own keys or prefix keys
-    int unit_tiles;
 };
 struct Walk {
-    int pair, v, s, b, vb;
+    int pair, h, o, left;          // prefix part
+    int b, bh, bo, own_left, keys;  // own part; keys of sequence b
 };
-__device__ __forceinline__ void walk_begin(const Plan& p, Walk& w) {
+__device__ __forceinline__ void walk_begin(const PrefixArgs& a, const Plan& p, Walk& w) {
     w.pair = p.pair;
-    w.v = p.v0;
-    w.s = p.s0;
-    w.b = p.b;
-    w.vb = p.vb;
+    w.h = p.h;
+    w.o = p.o;
+    w.left = p.len;
+    w.b = p.own_b;
+    w.bh = p.own_h;
+    w.bo = p.own_o;
+    w.own_left = p.own_len;
+    w.keys = p.own_len > 0 ? clamp_own(a, a.ctx_lens[p.own_b], p.P) : 0;
 }
 __device__ __forceinline__ bool walk_next(const PrefixArgs& a, const Plan& p, Walk& w, Segment& g) {
-    while (w.pair < a.np && p.v1 > p.v0) {  // prefix ranges: one pass per pair
-        if (w.v >= p.v1) {
-            w.v = p.v0;
+    while (w.pair < a.np || w.own_left > 0) {
+        const bool own = w.pair >= a.np;
+        if (!own && w.left == 0) {  // the next pair, over the same keys
             w.pair += p.pairs;
+            w.h = p.h;
+            w.o = p.o;
+            w.left = p.len;
             continue;
         }
-        const int span = p.nt + p.pad;
-        const int h = w.v / span, o = w.v - h * span;
-        const int e = min(span, o + p.v1 - w.v);
-        w.v += e - o;
-        const int t0 = max(0, o - p.pad), t1 = max(0, e - p.pad);
-        if (t1 <= t0) continue;
-        g.own = false;
-        g.dual_row = 2 * w.pair + 1 < a.nrt;
-        g.b = 0;
-        g.kvh = h;
-        g.pair = w.pair;
-        g.tile0 = t0;
-        g.tiles = t1 - t0;
-        g.keys = p.P;
-        g.unit_tiles = p.nt;
-        return true;
-    }
-    while (w.s < p.s1 && w.b < a.B) {
-        const int keys = own_keys(a, w.b, p.P);
-        const int nt = tiles_of(keys), span = nt + kPad;
-        const int x = w.s - w.vb;
-        const int h = x / span, o = x - h * span;
-        if (h >= a.Hkv) {
-            w.vb += a.Hkv * span;
-            ++w.b;
-            continue;
+        const int pad = own ? kPad : p.pad;
+        const int span = own ? tiles_of(w.keys) + kPad : p.span;
+        const int o = own ? w.bo : w.o;
+        const int e = min(span, o + (own ? w.own_left : w.left));
+        g.own = own;
+        g.dual_row = !own && 2 * w.pair + 1 < a.nrt;
+        g.b = own ? w.b : 0;
+        g.kvh = own ? w.bh : w.h;
+        g.pair = own ? 0 : w.pair;
+        g.keys = own ? w.keys : p.P;
+        g.tile0 = max(0, o - pad);
+        g.tiles = max(0, e - pad) - g.tile0;
+        const int next = e == span ? 0 : e;
+        if (own) {
+            w.own_left -= e - o;
+            w.bo = next;
+            if (e == span && ++w.bh == a.Hkv) {
+                w.bh = 0;
+                ++w.b;
+                if (w.own_left > 0) w.keys = clamp_own(a, a.ctx_lens[w.b], p.P);
+            }
+        } else {
+            w.left -= e - o;
+            w.o = next;
+            w.h += e == span;
         }
-        const int e = min(span, o + p.s1 - w.s);
-        w.s += e - o;
-        const int t0 = max(0, o - kPad), t1 = max(0, e - kPad);
-        if (t1 <= t0) continue;
-        g.own = true;
-        g.dual_row = false;
-        g.b = w.b;
-        g.kvh = h;
-        g.pair = 0;
-        g.tile0 = t0;
-        g.tiles = t1 - t0;
-        g.keys = keys;
-        g.unit_tiles = nt;
-        return true;
+        if (g.tiles > 0) return true;
     }
     return false;
 }
 
+// One lane of a converged warp.  The roles that copy and multiply run as whole warps, loops and waits alike, and
+// elect a lane only around the instructions themselves: those take their operands from uniform registers, and
+// operands computed by a single lane would be moved there one by one (an MMA then costs its issuer some 150
+// cycles, more than it costs the tensor core).
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred P;\n\telect.sync _|P, 0xffffffff;\n\tselp.u32 %0, 1, 0, P;\n\t}" : "=r"(p));
+    return p != 0;
+}
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
+
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, const WaitCtx& wc) {
     return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, wc));
+}
+
+// Two fp32 values in one 64-bit register: the FMA and the addition of both in one instruction.
+__device__ __forceinline__ uint64_t f32x2(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void f32x2_split(uint64_t v, float& lo, float& hi) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ uint64_t f32x2_fma(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t f32x2_add(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
+// Moves the references of the rows that ask for it (`move`) up to `top`: the row's sum, its O accumulators (at
+// rest: the scores in hand came behind the PV of the tile before) and the probabilities of the tile that
+// are stored already (of its first 32 * chunks keys) are scaled by 2^(old - new).  References are whole
+// numbers, so the factor is a power of two and the stored bf16 probabilities lose nothing.  Rare: kept out
+// of the way.
+template <int D>
+__device__ __noinline__ void move_reference(bool move, float top, float& m_ref, float& l_run, uint32_t tO, bool has_o,
+                                            uint32_t tP, int chunks) {
+    const float factor = move ? fast_exp2(m_ref - top) : 1.f;  // 0 when there was no reference
+    if (move) {
+        l_run *= factor;
+        m_ref = top;
+    }
+#pragma unroll 1
+    for (int i = 0; i < (has_o ? D / 16 : 0); ++i) {
+        uint32_t o[16];
+        tmem_ld_x16(tO + 16 * i, o);
+        tmem_wait_ld();
+#pragma unroll
+        for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * factor);
+        tmem_st_x16(tO + 16 * i, o);
+    }
+    tmem_wait_st();
+#pragma unroll 1
+    for (int i = 0; i < chunks; ++i) {
+        uint32_t o[16];
+        tmem_ld_x16(tP + 16 * i, o);
+        tmem_wait_ld();
+#pragma unroll
+        for (int k = 0; k < 16; ++k)
+            o[k] = pack_bf16x2(__uint_as_float(o[k] << 16) * factor, __uint_as_float(o[k] & 0xffff0000u) * factor);
+        tmem_st_x16(tP + 16 * i, o);
+    }
 }
 
 template <int D>
@@ -310,7 +385,7 @@ prefix_attn_split_kernel(const __grid_constant__ CUtensorMap tmKp, const __grid_
 
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t k_full[NK], k_empty[NK], v_full[NV], v_empty[NV];
-    __shared__ uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], pv_done[2], drain_bar[2];
+    __shared__ uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], pv_done[2], drain_bar;
     __shared__ uint32_t tmem_slot;
     __shared__ int s_abort;
     __shared__ Plan plan;
@@ -329,8 +404,8 @@ prefix_attn_split_kernel(const __grid_constant__ CUtensorMap tmKp, const __grid_
             mbar_init(&s_full[i], 1);
             mbar_init(&p_full[i], 4);
             mbar_init(&pv_done[i], 1);
-            mbar_init(&drain_bar[i], 1);
         }
+        mbar_init(&drain_bar, 1);
         fence_mbar_init();
         s_abort = 0;
     }
@@ -352,164 +427,191 @@ prefix_attn_split_kernel(const __grid_constant__ CUtensorMap tmKp, const __grid_
     const WaitCtx wc = {&s_abort, a.wait_limit};
 
     Walk w;
-    walk_begin(plan, w);
+    walk_begin(a, plan, w);
     Segment g;
     if (warp == 8) {
         // ---------------- K/V producer ----------------
-        if (lane == 0) {
-            int n_k = 0, n_v = 0;  // K and V tiles whose copies were issued
-            bool ok = true;
-            while (ok && walk_next(a, plan, w, g)) {
-                const CUtensorMap* mk = g.own ? &tmKo : &tmKp;
-                const CUtensorMap* mv = g.own ? &tmVo : &tmVp;
-                const int parts = kKeys / a.box_rows;
-                const uint32_t part_bytes = kHalfBytes / parts;
-                for (int t = 0; t < g.tiles; ++t) {
-                    const int key0 = (g.tile0 + t) * kKeys;
-                    int c1[2] = {key0, 0}, c3[2] = {g.b, g.b};
-                    if (a.block_table) {
-                        for (int q = 0; q < parts; ++q) {
-                            const int in_unit = key0 + q * a.box_rows;
-                            const int pos = in_unit + (g.own ? plan.P : 0);
-                            c1[q] = pos & (a.block_size - 1);
-                            if (in_unit >= g.keys) {
-                                c3[q] = a.num_blocks;  // past the keys: zeros, no table entry is read
-                                continue;
-                            }
-                            c3[q] = __ldg(a.block_table + (size_t)g.b * a.max_blocks + (pos >> a.block_log2));
-                            if ((unsigned)c3[q] >= (unsigned)a.num_blocks) {
-                                atomicOr(a.status, RAPID_STATUS_BAD_BLOCK_TABLE);
-                                c3[q] = a.num_blocks;  // outside the pool: the copy reads zeros
-                            }
+        int n_k = 0, n_v = 0;  // K and V tiles whose copies were issued
+        bool ok = true;
+        const int parts = kKeys / a.box_rows;
+        const uint32_t part_bytes = kHalfBytes / parts;
+        while (ok && walk_next(a, plan, w, g)) {
+            const CUtensorMap* mk = g.own ? &tmKo : &tmKp;
+            const CUtensorMap* mv = g.own ? &tmVo : &tmVp;
+            const int kvh = uniform(g.kvh), tiles = uniform(g.tiles);
+            for (int t = 0; t < tiles; ++t) {
+                const int key0 = (g.tile0 + t) * kKeys;
+                int c1[2] = {key0, 0}, c3[2] = {g.b, g.b};
+                if (a.block_table) {
+                    for (int q = 0; q < parts; ++q) {
+                        const int in_unit = key0 + q * a.box_rows;
+                        const int pos = in_unit + (g.own ? plan.P : 0);
+                        c1[q] = pos & (a.block_size - 1);
+                        if (in_unit >= g.keys) {
+                            c3[q] = a.num_blocks;  // past the keys: zeros, no table entry is read
+                            continue;
+                        }
+                        c3[q] = __ldg(a.block_table + (size_t)g.b * a.max_blocks + (pos >> a.block_log2));
+                        if ((unsigned)c3[q] >= (unsigned)a.num_blocks) {
+                            if (lane == 0) atomicOr(a.status, RAPID_STATUS_BAD_BLOCK_TABLE);
+                            c3[q] = a.num_blocks;  // outside the pool: the copy reads zeros
                         }
                     }
-                    const int ks = n_k % NK, vs = n_v % NV;
-                    if (n_k >= NK) ok = mbar_wait_bounded_relaxed(&k_empty[ks], (n_k / NK - 1) & 1, wc);
-                    if (!ok) break;
+                }
+                const int ks = n_k % NK, vs = n_v % NV;
+                if (n_k >= NK) ok = warp_wait(&k_empty[ks], (n_k / NK - 1) & 1, wc);
+                if (!ok) break;
+                if (elect_one()) {
                     mbar_arrive_expect_tx(&k_full[ks], TILE);
                     for (int q = 0; q < parts; ++q)
 #pragma unroll
                         for (int h = 0; h < NH; ++h)
                             tma_load_4d(smem + OFF_K + ks * TILE + h * kHalfBytes + q * part_bytes, mk, &k_full[ks],
-                                        h * 64, c1[q], g.kvh, c3[q]);
-                    ++n_k;
-                    if (n_v >= NV) ok = mbar_wait_bounded_relaxed(&v_empty[vs], (n_v / NV - 1) & 1, wc);
-                    if (!ok) break;
+                                        h * 64, c1[q], kvh, c3[q]);
+                }
+                __syncwarp();
+                ++n_k;
+                if (n_v >= NV) ok = warp_wait(&v_empty[vs], (n_v / NV - 1) & 1, wc);
+                if (!ok) break;
+                if (elect_one()) {
                     mbar_arrive_expect_tx(&v_full[vs], TILE);
                     for (int q = 0; q < parts; ++q)
 #pragma unroll
                         for (int h = 0; h < NH; ++h)
                             tma_load_4d(smem + OFF_V + vs * TILE + h * kHalfBytes + q * part_bytes, mv, &v_full[vs],
-                                        h * 64, c1[q], g.kvh, c3[q]);
-                    ++n_v;
+                                        h * 64, c1[q], kvh, c3[q]);
                 }
+                __syncwarp();
+                ++n_v;
             }
-            // every copy lands before the CTA gives up its shared memory, whoever may have given up waiting for it
-            for (int s = 0; s < NK && s < n_k; ++s) mbar_wait_drain(&k_full[s], ((n_k - 1 - s) / NK) & 1);
-            for (int s = 0; s < NV && s < n_v; ++s) mbar_wait_drain(&v_full[s], ((n_v - 1 - s) / NV) & 1);
         }
+        // every copy lands before the CTA gives up its shared memory, whoever may have given up waiting for it
+        for (int s = 0; s < NK && s < n_k; ++s) mbar_wait_drain(&k_full[s], ((n_k - 1 - s) / NK) & 1);
+        for (int s = 0; s < NV && s < n_v; ++s) mbar_wait_drain(&v_full[s], ((n_v - 1 - s) / NV) & 1);
     } else if (warp == 9) {
         // ---------------- Q producer: a ring of two row tiles ----------------
-        if (lane == 0) {
-            int n = 0;
-            bool ok = true;
-            while (ok && walk_next(a, plan, w, g)) {
-                const int cnt = g.dual_row ? 2 : 1;
-                for (int i = 0; i < cnt; ++i, ++n) {
-                    const int s = n & 1;
-                    if (n >= 2) ok = mbar_wait_bounded_relaxed(&q_empty[s], (n / 2 - 1) & 1, wc);
-                    if (!ok) break;
-                    const int row0 = g.own ? g.b * a.R : (2 * g.pair + i) * a.rows_tile;
+        int n = 0;
+        bool ok = true;
+        while (ok && walk_next(a, plan, w, g)) {
+            const int cnt = g.dual_row ? 2 : 1;
+            for (int i = 0; i < cnt; ++i) {
+                const int s = n & 1;
+                if (n >= 2) ok = warp_wait(&q_empty[s], (n / 2 - 1) & 1, wc);
+                if (!ok) break;
+                const int row0 = g.own ? g.b * a.R : (2 * g.pair + i) * a.rows_tile;
+                if (elect_one()) {
                     mbar_arrive_expect_tx(&q_full[s], (uint32_t)a.rows_tile * a.G * D * 2);
 #pragma unroll
                     for (int h = 0; h < NH; ++h)
                         tma_load_4d(smem + OFF_Q + s * TILE + h * kHalfBytes, &tmQ, &q_full[s], h * 64, g.kvh * a.G,
                                     row0, 0);
                 }
+                __syncwarp();
+                ++n;
             }
-            for (int s = 0; s < 2 && s < n; ++s) mbar_wait_drain(&q_full[s], ((n - 1 - s) / 2) & 1);
         }
+        for (int s = 0; s < 2 && s < n; ++s) mbar_wait_drain(&q_full[s], ((n - 1 - s) / 2) & 1);
     } else if (warp == 10) {
-        // ---------------- QK^T issuer ----------------
-        if (lane == 0) {
-            constexpr uint32_t idesc = umma_idesc_bf16(128, kKeys, 0, 0);
-            const uint64_t q_desc = umma_smem_desc(smem_base + OFF_Q, 16, 1024);
-            const uint64_t k_desc = umma_smem_desc(smem_base + OFF_K, 16, 1024);
-            int n = 0, qn = 0, par = 0, done[2] = {0, 0};
-            bool ok = true;
-            while (ok && walk_next(a, plan, w, g)) {
-                const int cnt = g.dual_row ? 2 : 1;
-                for (int i = 0; i < cnt && ok; ++i) ok = mbar_wait_bounded(&q_full[(qn + i) & 1], ((qn + i) >> 1) & 1, wc);
-                for (int t = 0; t < g.tiles && ok; ++t, ++n) {
-                    const int ks = n % NK;
-                    ok = mbar_wait_bounded(&k_full[ks], (n / NK) & 1, wc);
-                    for (int i = 0; i < cnt && ok; ++i) {
-                        const int s = g.dual_row ? i : par & 1;
-                        // the stream's S columns are free once the PV of its previous tile has read P from them
-                        const int c = s ? done[1]++ : done[0]++;
-                        if (c > 0) ok = mbar_wait_bounded(&pv_done[s], (c - 1) & 1, wc);
-                        if (!ok) break;
-                        tc_fence_after_sync();
-                        const uint64_t qd = q_desc + (uint64_t)(((qn + i) & 1) * (TILE >> 4));
-                        const uint64_t kd = k_desc + (uint64_t)(ks * (TILE >> 4));
-                        const uint32_t d = tmem + COL_S + 128u * s;
+        // ---------------- MMA issuer ----------------
+        // One thread issues both products, because the tensor core works off its instructions in order: QK^T
+        // of a stream's next tile goes out right behind the PV of its last one and overwrites the P that
+        // PV reads, with no wait in between; and scores in hand mean that PV has completed.
+        constexpr uint32_t idesc_qk = umma_idesc_bf16(128, kKeys, 0, 0);
+        constexpr uint32_t idesc_pv = umma_idesc_bf16(128, D, 0, 1);
+        const uint32_t tm0 = uniform(tmem);
+        const uint64_t q_desc = umma_smem_desc(smem_base + OFF_Q, 16, 1024);
+        const uint64_t k_desc = umma_smem_desc(smem_base + OFF_K, 16, 1024);
+        const uint64_t v_desc = umma_smem_desc(smem_base + OFF_V, kHalfBytes, 1024);
+        Walk wq = w;  // the QK^T side runs ahead of the PV side
+        Segment gq;
+        bool more_q = walk_next(a, plan, wq, gq), more = walk_next(a, plan, w, g);
+        int rows_q = uniform(gq.dual_row ? 2 : 1), tiles_q = uniform(gq.tiles);
+        int rows = rows_q, tiles = tiles_q;  // row tiles and key tiles of the segment
+        int tq = 0, iq = 0, par_q = 0, n_k = 0, n_q = 0;  // tile, row tile, dual-key tiles met, K tiles, Q tiles
+        int t = 0, i = 0, par = 0, n_v = 0;
+        uint32_t busy = 0, p_phase = 0;  // bit s: stream s holds scores whose PV is to come; phase of its p_full
+        bool ok = true;
+        while (more && ok) {
+            while (more_q) {
+                const int s = rows_q == 2 ? iq : par_q & 1;
+                if (busy >> s & 1) break;
+                const int ks = n_k % NK, qs = (n_q + iq) & 1;
+                if (tq == 0) ok = warp_wait(&q_full[qs], ((n_q + iq) >> 1) & 1, wc);
+                if (ok && iq == 0) ok = warp_wait(&k_full[ks], (n_k / NK) & 1, wc);
+                if (!ok) break;
+                tc_fence_after_sync();
+                const uint64_t qd = q_desc + (uint64_t)(qs * (TILE >> 4)), kd = k_desc + (uint64_t)(ks * (TILE >> 4));
+                const bool last = tq + 1 == tiles_q, tile_done = iq + 1 == rows_q;
+                if (elect_one()) {
 #pragma unroll
-                        for (int kk = 0; kk < D / 16; ++kk) {
-                            const uint32_t off = (kk >> 2) * (kHalfBytes >> 4) + (kk & 3) * 2;
-                            umma_bf16_ss(d, qd + off, kd + off, idesc, kk > 0);
-                        }
-                        umma_commit(&s_full[s]);
+                    for (int kk = 0; kk < D / 16; ++kk) {
+                        const uint32_t off = (kk >> 2) * (kHalfBytes >> 4) + (kk & 3) * 2;
+                        umma_bf16_ss(tm0 + COL_S + 128u * s, qd + off, kd + off, idesc_qk, kk > 0);
                     }
-                    if (!ok) break;
-                    umma_commit(&k_empty[ks]);
-                    if (!g.dual_row) ++par;
+                    umma_commit(&s_full[s]);
+                    if (last) umma_commit(&q_empty[qs]);
+                    if (tile_done) umma_commit(&k_empty[ks]);
                 }
-                if (ok)
-                    for (int i = 0; i < cnt; ++i) umma_commit(&q_empty[(qn + i) & 1]);
-                qn += cnt;
-            }
-            if (!ok) {  // every MMA issued here has completed before tensor memory is freed
-                umma_commit(&drain_bar[0]);
-                mbar_wait_drain(&drain_bar[0], 0);
-            }
-        }
-    } else if (warp == 11) {
-        // ---------------- PV issuer ----------------
-        if (lane == 0) {
-            constexpr uint32_t idesc = umma_idesc_bf16(128, D, 0, 1);
-            const uint64_t v_desc = umma_smem_desc(smem_base + OFF_V, kHalfBytes, 1024);
-            int n = 0, par = 0, done[2] = {0, 0};
-            bool ok = true;
-            while (ok && walk_next(a, plan, w, g)) {
-                const int cnt = g.dual_row ? 2 : 1;
-                for (int t = 0; t < g.tiles && ok; ++t, ++n) {
-                    const int vs = n % NV;
-                    ok = mbar_wait_bounded(&v_full[vs], (n / NV) & 1, wc);
-                    for (int i = 0; i < cnt && ok; ++i) {
-                        const int s = g.dual_row ? i : par & 1;
-                        const bool fresh = g.dual_row ? t == 0 : t < 2;  // the stream's first tile of the segment
-                        const int c = s ? done[1]++ : done[0]++;
-                        ok = mbar_wait_bounded(&p_full[s], c & 1, wc);
-                        if (!ok) break;
-                        tc_fence_after_sync();
-                        const uint64_t vd = v_desc + (uint64_t)(vs * (TILE >> 4));
-                        const uint32_t d = tmem + COL_O + 128u * s, p = tmem + COL_S + 128u * s;
-#pragma unroll
-                        for (int kk = 0; kk < kKeys / 16; ++kk)
-                            umma_bf16_ts(d, p + 8 * kk, vd + kk * (2048 >> 4), idesc, (!fresh || kk > 0) ? 1u : 0u);
-                        umma_commit(&pv_done[s]);
-                    }
-                    if (!ok) break;
-                    umma_commit(&v_empty[vs]);
-                    if (!g.dual_row) ++par;
+                __syncwarp();
+                busy |= 1u << s;
+                if (!tile_done) {
+                    iq = 1;
+                    continue;
+                }
+                ++n_k;
+                if (rows_q == 1) ++par_q;
+                iq = 0;
+                if (++tq == tiles_q) {
+                    n_q += rows_q;
+                    tq = 0;
+                    more_q = walk_next(a, plan, wq, gq);
+                    rows_q = uniform(gq.dual_row ? 2 : 1);
+                    tiles_q = uniform(gq.tiles);
                 }
             }
-            if (!ok) {
-                umma_commit(&drain_bar[1]);
-                mbar_wait_drain(&drain_bar[1], 0);
+            if (!ok) break;
+            const int s = rows == 2 ? i : par & 1;
+            const int vs = n_v % NV;
+            if (i == 0) ok = warp_wait(&v_full[vs], (n_v / NV) & 1, wc);
+            if (ok) ok = warp_wait(&p_full[s], p_phase >> s & 1, wc);
+            if (!ok) break;
+            p_phase ^= 1u << s;
+            tc_fence_after_sync();
+            const int turns = rows == 2 ? 1 : 2;     // tiles from one of a stream to its next
+            const bool fresh = t < turns;            // the stream's first tile of the segment
+            const bool last = t >= tiles - turns;    // ... and its last
+            const bool tile_done = i + 1 == rows;
+            const uint64_t vd = v_desc + (uint64_t)(vs * (TILE >> 4));
+            if (elect_one()) {
+#pragma unroll
+                for (int kk = 0; kk < kKeys / 16; ++kk)
+                    umma_bf16_ts(tm0 + COL_O + 128u * s, tm0 + COL_S + 128u * s + 8 * kk, vd + kk * (2048 >> 4), idesc_pv,
+                                 (!fresh || kk > 0) ? 1u : 0u);
+                if (last) umma_commit(&pv_done[s]);
+                if (tile_done) umma_commit(&v_empty[vs]);
+            }
+            __syncwarp();
+            busy &= ~(1u << s);
+            if (!tile_done) {
+                i = 1;
+                continue;
+            }
+            ++n_v;
+            i = 0;
+            if (rows == 1) ++par;
+            if (++t == tiles) {
+                t = 0;
+                more = walk_next(a, plan, w, g);
+                rows = uniform(g.dual_row ? 2 : 1);
+                tiles = uniform(g.tiles);
             }
         }
-    } else {
+        if (!ok) {  // every MMA issued here has completed before tensor memory is freed
+            if (elect_one()) umma_commit(&drain_bar);
+            __syncwarp();
+            mbar_wait_drain(&drain_bar, 0);
+        }
+    } else if (warp < 8) {
         // ---------------- softmax warps: stream = warp / 4, row of the tile = 32 (warp % 4) + lane ----------------
         const int stream = warp >> 2;
         const int row = (warp & 3) * 32 + lane;
@@ -517,7 +619,7 @@ prefix_attn_split_kernel(const __grid_constant__ CUtensorMap tmKp, const __grid_
         const uint32_t tS = tmem + lane_base + COL_S + 128u * stream;
         const uint32_t tO = tmem + lane_base + COL_O + 128u * stream;
         const float c = a.scale_log2;
-        int n = 0, par = 0, cnt = 0;  // CTA-wide tile index, dual-key tiles met, tiles of this stream
+        int n = 0, par = 0, cnt = 0, segs = 0;  // CTA-wide tile index, dual-key tiles met, tiles and segments of this stream
         bool ok = true;
         while (ok && walk_next(a, plan, w, g)) {
             // the tile's rows: (sequence, row, head in group) of the batch, or (row, head) of one sequence
@@ -537,62 +639,48 @@ prefix_attn_split_kernel(const __grid_constant__ CUtensorMap tmKp, const __grid_
                 const int key0 = (g.tile0 + t) * kKeys;
                 if (warp_active) {
                     tc_fence_after_sync();
-                    uint32_t sr[4][32];
+                    uint32_t sr[2][32];  // scores of 32 keys, and the next 32 on their way
+                    tmem_ld_x32(tS, sr[0]);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) tmem_ld_x32(tS + 32 * i, sr[i]);
-                    tmem_wait_ld();
-                    if (key0 + kKeys - 1 > all_see) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
+                    for (int h = 0; h < 4; ++h) {
+                        uint32_t(&x)[32] = sr[h & 1];
+                        tmem_wait_ld();
+                        if (h < 3) tmem_ld_x32(tS + 32 * (h + 1), sr[(h + 1) & 1]);
+                        if (key0 + 32 * h + 31 > all_see) {
 #pragma unroll
                             for (int k = 0; k < 32; ++k)
-                                if (key0 + 32 * i + k > lim) sr[i][k] = __float_as_uint(-INFINITY);
-                    }
-                    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) mx[k & 3] = fmaxf(mx[k & 3], __uint_as_float(sr[i][k]));
-                    const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
-                    const bool move = row_valid && top > m_ref + kJump;
-                    if (__any_sync(0xffffffffu, move)) {
-                        const float factor = move ? fast_exp2(m_ref - top) : 1.f;  // 0 when there was no reference
-                        if (move) {
-                            l_run *= factor;
-                            m_ref = top;
+                                if (key0 + 32 * h + k > lim) x[k] = __float_as_uint(-INFINITY);
                         }
-                        if (!first) {
-                            // O at rest: the stream's previous PV has completed
-                            ok = warp_wait(&pv_done[stream], (cnt - 1) & 1, wc);
-                            if (!ok) break;
-                            tc_fence_after_sync();
+                        float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-                            for (int i = 0; i < D / 16; ++i) {
-                                uint32_t o[16];
-                                tmem_ld_x16(tO + 16 * i, o);
-                                tmem_wait_ld();
-#pragma unroll
-                                for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * factor);
-                                tmem_st_x16(tO + 16 * i, o);
-                            }
+                        for (int k = 0; k < 32; k += 4) {
+                            mx[0] = max3(mx[0], __uint_as_float(x[k]), __uint_as_float(x[k + 1]));
+                            mx[1] = max3(mx[1], __uint_as_float(x[k + 2]), __uint_as_float(x[k + 3]));
                         }
-                    }
-                    const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
-                    float s0 = 0.f, s1 = 0.f;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                        const float top = ceilf(fmaxf(mx[0], mx[1]) * c);
+                        // no reference yet, or scores that outgrow it
+                        const bool move = row_valid && top > m_ref + kJump;
+                        if (__any_sync(0xffffffffu, move)) {
+                            tmem_wait_ld();  // (the next scores are in their registers before the call)
+                            move_reference<D>(move, top, m_ref, l_run, tO, !first, tS, h);
+                        }
+                        const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
+                        const uint64_t c2 = f32x2(c, c), m2 = f32x2(-m_use, -m_use);
+                        uint64_t acc[2] = {0, 0};
                         uint32_t pk[16];
 #pragma unroll
                         for (int k = 0; k < 32; k += 2) {
-                            const float p0 = fast_exp2(fmaf(__uint_as_float(sr[i][k]), c, -m_use));
-                            const float p1 = fast_exp2(fmaf(__uint_as_float(sr[i][k + 1]), c, -m_use));
-                            s0 += p0;
-                            s1 += p1;
+                            float y0, y1;
+                            f32x2_split(f32x2_fma(f32x2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), c2, m2), y0, y1);
+                            const float p0 = fast_exp2(y0), p1 = fast_exp2(y1);
+                            acc[(k >> 1) & 1] = f32x2_add(acc[(k >> 1) & 1], f32x2(p0, p1));
                             pk[k >> 1] = pack_bf16x2(p0, p1);
                         }
-                        tmem_st_x16(tS + 16 * i, pk);
+                        tmem_st_x16(tS + 16 * h, pk);
+                        float s0, s1;
+                        f32x2_split(f32x2_add(acc[0], acc[1]), s0, s1);
+                        l_run += s0 + s1;
                     }
-                    l_run += s0 + s1;
                     first = false;
                 }
                 if (key0 + kKeys > g.keys) {
@@ -623,7 +711,7 @@ prefix_attn_split_kernel(const __grid_constant__ CUtensorMap tmKp, const __grid_
             float* slot = g.own ? a.part_own + (size_t)((plan.worker + unit) * 2 + stream) * slot_floats(a.GR, D)
                                 : a.part_prefix + (size_t)((plan.team + g.kvh) * 2 * a.np + 2 * g.pair + stream) * slot_floats(128, D);
             if (!first) {
-                ok = warp_wait(&pv_done[stream], (cnt - 1) & 1, wc);
+                ok = warp_wait(&pv_done[stream], segs & 1, wc);
                 if (!ok) break;
                 tc_fence_after_sync();
 #pragma unroll
@@ -650,9 +738,10 @@ prefix_attn_split_kernel(const __grid_constant__ CUtensorMap tmKp, const __grid_
                 const int who = g.own ? plan.worker : plan.team;
                 if (g.own || g.pair == 0) {
                     if (g.tile0 == 0) range->x = who;
-                    if (g.tile0 + g.tiles == g.unit_tiles) range->y = who;
+                    if (g.tile0 + g.tiles == tiles_of(g.keys)) range->y = who;
                 }
             }
+            if (g.dual_row || g.tiles > ((stream ^ par) & 1)) ++segs;  // the stream had a tile of it
             n += g.tiles;
             if (!g.dual_row) par += g.tiles;
         }
@@ -692,12 +781,11 @@ prefix_attn_merge_kernel(const __grid_constant__ PrefixArgs a, __nv_bfloat16* ou
 
     griddep_wait();
     griddep_launch_dependents();
-    const int P = prefix_keys(a);
+    const int P = clamp_prefix(a, *a.prefix_len);
     int2 pr = P > 0 ? __ldcg(a.prefix_range + kvh) : make_int2(0, -1);
     int2 orr = __ldcg(a.own_range + unit);
     // (a split kernel whose waits ran out may not have written them: whatever they hold, stay inside the slots)
-    const int teams = max(1, a.num_ctas / a.np);
-    if (pr.x < 0 || pr.y >= teams) pr = make_int2(0, -1);
+    if (pr.x < 0 || pr.y >= a.max_teams) pr = make_int2(0, -1);
     if (orr.x < 0 || orr.y >= a.num_ctas) orr = make_int2(0, -1);
     // The row's slots as one list: index x < np_slots is in the prefix part (one slot per team, or two where a
     // single row tile's keys went to both streams), the rest in the own part (two per worker).
@@ -1003,6 +1091,8 @@ int launch_verify_attention_prefix(const void* q, const void* k_prefix, const vo
     a.nrt = (int)nrt;
     a.np = np;
     a.num_ctas = num_ctas;
+    a.max_teams = num_ctas / (np < num_ctas ? np : num_ctas);
+    a.rounds = (np + num_ctas - 1) / num_ctas;
     a.scale_log2 = scale * 1.4426950408889634f;
     a.wait_limit = wait_limit;
 
