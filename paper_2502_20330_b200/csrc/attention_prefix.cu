@@ -19,12 +19,12 @@
 //   S_s[128 x 128] = Q_s K^T      A = Q tile, B = K tile, both K-major in shared memory
 //   O_s[128 x D]  += P_s V        A = P (bf16, over the first half of S_s's columns), B = V tile, MN-major
 //
-// Work split (make_plan, one warp of every CTA: no plan kernel, no plan to go stale).  Cost is counted in
+// Work split (worked out by every CTA for itself: no plan kernel, no plan to go stale).  Cost is counted in
 // single-stream tiles: 2 for a dual-row tile, 1 for a dual-key tile, kPad for changing to another unit.
-// With np pairs of row tiles the prefix is cut into T equal ranges of key tiles, each for a team of np CTAs,
-// one pair each: a team reads the same K/V tiles at the same time, so they leave HBM once.  T is the
-// share of the machine that the prefix is of the whole work; the sequences' own tiles fill up every CTA
-// to the same level (CTAs outside the teams first, then those with a single row tile, then all).
+// With np pairs of row tiles the prefix is cut into equal ranges of key tiles, each for a team of np CTAs, one
+// pair each: a team reads the same K/V tiles at the same time, so they leave HBM once.  The sequences'
+// own tiles fill up every CTA to the same level (CTAs outside the teams first, then those with a single
+// row tile, then all).
 //
 // Bound: up to 256 rows per KV head (one pair) a K/V tile of 64 KB is read for every 256 x 128 scores, and HBM
 // is the limit; from two pairs on the tensor cores and the exponentials are.
@@ -41,7 +41,7 @@ namespace rapid {
 namespace {
 
 constexpr int kKeys = 128;             // keys per tile
-constexpr int kThreads = 352;          // two softmax groups of 128, then a warp each for K/V copies, Q copies, MMAs
+constexpr int kThreads = 384;          // two softmax groups of 128, then a warp each for K/V copies, Q copies, MMAs, planning
 constexpr int kHalfBytes = kKeys * 128;  // one 64-column half of a tile of 128 rows
 constexpr int kPad = 3;                // single-stream tiles that a change of unit costs
 constexpr int kMaxPrefixCtas = 256;
@@ -71,7 +71,8 @@ struct PrefixArgs {
     int block_size, block_log2, num_blocks, max_blocks, box_rows;
     int rows_tile;               // (sequence, row) pairs in a row tile: 128 / G
     int nrt, np;                 // row tiles, pairs of row tiles
-    int max_teams, rounds;       // teams of np CTAs that the grid holds; passes over the prefix where np exceeds the grid
+    int team_ctas, max_teams;    // CTAs of a team (np, at most the grid) and teams that the grid holds
+    int rounds, row_cost;        // passes over the prefix where np exceeds the grid; cost of a prefix tile to a CTA
     int num_ctas;
     float scale_log2;
     long long wait_limit;
@@ -90,12 +91,14 @@ __device__ __forceinline__ int clamp_own(const PrefixArgs& a, int L, int P) {
 }
 __device__ __forceinline__ int tiles_of(int keys) { return (keys + kKeys - 1) / kKeys; }
 
-// What a CTA does, worked out by its first warp.
+// What a CTA does.  The prefix part follows from the prefix's length alone and is worked out before anything
+// else; the own part needs every sequence's length, is worked out by a warp of its own while the CTA is at
+// its prefix tiles, and is waited for (own_ready) only by who comes to it.
 struct Plan {
-    int P, pad, span;      // prefix keys; virtual tiles in front of every KV head's, and those with the real ones
-    int team, pair, pairs;  // the CTA's team, its first pair (np: none), the step to its next
-    int h, o, len;         // its run of the prefix's padded tile list: KV head, offset in its span, length
-    int worker;            // its rank among the CTAs that hold own tiles
+    int P, nt, pad, span;   // prefix keys and tiles; virtual tiles in front of every KV head's, and those with the real ones
+    int teams, team, pair;  // teams, the CTA's team (-1: none) and its first pair of row tiles
+    int h, o, len;          // its run of the prefix's padded tile list: KV head, offset in its span, length
+    int worker;             // its rank among the CTAs that hold own tiles
     int own_b, own_h, own_o, own_len;  // its run of the own tiles' padded list
 };
 
@@ -112,15 +115,44 @@ __device__ __forceinline__ int small_div(int x, int d) {
     return q;
 }
 
-// The length of the code matters as much as its running time: it is fetched anew by almost every launch.
-__device__ __noinline__ void make_plan(const PrefixArgs& a, int cta, Plan& out) {
+// (In both functions the length of the code matters as much as anything: a launch fetches it anew, at several
+// cycles an instruction.)
+__device__ __forceinline__ void plan_prefix(const PrefixArgs& a, int cta, Plan& p) {
+    p.P = clamp_prefix(a, *a.prefix_len);
+    p.nt = tiles_of(p.P);
+    // Teams: one tile each while that leaves half of the grid's teams idle, then eight tiles each up to all teams
+    // (a team's partials cost a write and a read of 128 KB per pair and KV head, a tile about 1.5 us).
+    const int NP = a.Hkv * p.nt;
+    p.teams = min(a.max_teams, max(min(NP, (a.max_teams + 1) >> 1), NP >> 3));
+    p.pad = NP >= 4 * p.teams ? kPad : 0;
+    p.span = p.nt + p.pad;
+    p.team = small_div(cta, a.team_ctas);
+    p.pair = cta - p.team * a.team_ctas;
+    p.h = p.o = p.len = 0;
+    if (p.team < p.teams) {
+        const int total = a.Hkv * p.span;
+        const float r = __fdiv_rn((float)total, (float)p.teams);
+        const int v0 = share_start(total, p.teams, r, p.team);
+        p.len = share_start(total, p.teams, r, p.team + 1) - v0;
+        p.h = small_div(v0, p.span);
+        p.o = v0 - p.h * p.span;
+    } else {
+        p.team = -1;
+        p.pair = a.np;
+    }
+}
+
+// The own part.  w = cost of a team's range for a CTA with a full pair of row tiles, wh for one with a single row
+// tile (class H: the last CTA of every team if the number of row tiles is odd; A: the teams' others; B: the CTAs
+// in no team).  All are filled up to one level X: nB X + nH (X - wh)+ + nA (X - w)+ = S, whose solution is the
+// smallest of the three that leave out no, one or both of the upper classes.
+__device__ __noinline__ void plan_own(const PrefixArgs& a, int cta, Plan& p) {
     const int lane = threadIdx.x & 31;
-    const int given = *a.prefix_len;
-    const int first_len = lane < a.B ? a.ctx_lens[lane] : 0;  // (both loads are on their way before either is used)
-    const int P = clamp_prefix(a, given);
-    const int nt = tiles_of(P);
+    const int first_len = lane < a.B ? a.ctx_lens[lane] : 0;
+    const int P = p.P;
     int S = 0;
-    bool bad = given != P && !(a.block_table && (given & ~(a.block_size - 1)) == P);
+    bool bad = false;  // lengths out of range: only the device can see them, the first CTA says so
+#pragma unroll 1
     for (int b = lane; b < a.B; b += 32) {
         const int L = b < 32 ? first_len : a.ctx_lens[b];
         const int own = clamp_own(a, L, P);
@@ -128,109 +160,68 @@ __device__ __noinline__ void make_plan(const PrefixArgs& a, int cta, Plan& out) 
         bad |= L != own + (a.block_table ? P : 0);
     }
     S = __reduce_add_sync(0xffffffffu, S);
-    if (cta == 0 && __any_sync(0xffffffffu, bad) && lane == 0) atomicOr(a.status, RAPID_STATUS_BAD_CTX_LEN);
-
-    const int C = a.num_ctas, npc = min(a.np, C);
-    const int rounds = a.rounds, two = a.nrt > 1 ? 2 : 1;
-    // teams: the prefix's share of all work, at most what the grid holds, at least one
-    const int NP = a.Hkv * nt;
-    const float level = fmaxf(1.f, __fdividef((float)(NP * a.nrt + S), (float)C));
-    int T = 0, pad = 0, w = 0, wh = 0;  // w, wh: cost of a team's range for a full pair and for a single row tile
-    if (NP > 0) {
-        T = max(1, min(min(a.max_teams, NP), (int)ceilf(__fdividef((float)NP * two * rounds, level))));
-        if (NP >= 4 * T) pad = kPad;
-        w = wh = (int)ceilf(__fdividef((float)(NP + a.Hkv * pad) * two * rounds, (float)T));
+    if (cta == 0) {
+        const int given = *a.prefix_len;
+        bad |= given != P && !(a.block_table && (given & ~(a.block_size - 1)) == P);
+        if (__any_sync(0xffffffffu, bad) && lane == 0) atomicOr(a.status, RAPID_STATUS_BAD_CTX_LEN);
     }
-    const int span = nt + pad, NPv = a.Hkv * span;
-    const int n_team = T * npc;
-    const bool half_class = T > 0 && (a.nrt & 1) && a.np > 1 && rounds == 1;  // each team has one CTA with a single row tile
-    const int nH = half_class ? T : 0, nA = n_team - nH, nB = C - n_team;
-    if (half_class) wh = w >> 1;
-    Plan p;
-    p.P = P;
-    p.pad = pad;
-    p.span = span;
-    p.team = -1;
-    p.pair = a.np;
-    p.pairs = npc;
-    p.h = p.o = p.len = 0;
-    if (cta < n_team) {
-        p.team = small_div(cta, npc);
-        p.pair = cta - p.team * npc;
-        const float r = __fdiv_rn((float)NPv, (float)T);
-        const int v0 = share_start(NPv, T, r, p.team);
-        p.len = share_start(NPv, T, r, p.team + 1) - v0;
-        p.h = small_div(v0, span);
-        p.o = v0 - p.h * span;
-    }
-    // own tiles: fill the classes (no prefix work; a single row tile; a full pair) up to one level
-    int left = S;
-    int SB = min((float)left, (float)nB * wh) < (float)left ? nB * wh : left, SH = 0, SA = 0;
-    left -= SB;
-    if (nH > 0 && left > 0) {
-        const float room = (float)(nB + nH) * (w - wh);
-        const int l2 = room < (float)left ? (nB + nH) * (w - wh) : left;
-        SH = min(l2, (int)((float)l2 * __fdividef((float)nH, (float)(nB + nH))));
-        SB += l2 - SH;
-        left -= l2;
-    }
-    if (left > 0) {
-        int each = (int)__fdividef((float)left, (float)C);
-        if ((float)each * C > (float)left) --each;
-        SB += each * nB;
-        SH += each * nH;
-        left -= each * (nB + nH);
-        if (nA > 0) SA = left;
-        else if (nB > 0) SB += left;
-        else SH += left;
-    }
-    if (nB == 0 && SB > 0) {  // (rounding's crumbs have no CTA to go to)
-        SA += SB;
-        SB = 0;
+    const int in_teams = p.teams * a.team_ctas;
+    const bool half = (a.nrt & 1) && a.np > 1 && a.rounds == 1;
+    const int nH = half ? p.teams : 0, nA = in_teams - nH, nB = a.num_ctas - in_teams;
+    const float w = p.teams > 0 ? ceilf(__fdividef((float)(a.Hkv * p.span) * a.row_cost, (float)p.teams)) : 0.f;
+    const float wh = half ? 0.5f * w : w;
+    const float fS = (float)S;
+    const float X1 = nB > 0 ? __fdividef(fS, (float)nB) : INFINITY;
+    const float X2 = nB + nH > 0 ? __fdividef(fS + nH * wh, (float)(nB + nH)) : INFINITY;
+    const float X3 = __fdividef(fS + nH * wh + nA * w, (float)a.num_ctas);
+    const float X = fminf(X1, fminf(X2, X3));
+    // class totals: whole tiles, what is left over goes to the last class that has CTAs and a share
+    int SB = min(S, (int)(X * nB)), SH = min(S - SB, (int)(fmaxf(X - wh, 0.f) * nH)), SA = S - SB - SH;
+    if (nA == 0 || X <= w) {
+        if (nH > 0 && (nB == 0 || X > wh)) SH += SA, SA = 0;
+        else if (nB > 0) SB += SA, SA = 0;
     }
     // workers: the CTAs of class B, then H, then A, those without a share left out
-    int n, total, rank, off_w, off_s;
-    if (cta >= n_team) {
-        n = nB, total = SB, rank = cta - n_team, off_w = 0, off_s = 0;
-    } else if (half_class && p.pair == a.np - 1) {
-        n = nH, total = SH, rank = p.team, off_w = min(nB, SB), off_s = SB;
-    } else {
-        n = nA, total = SA, off_w = min(nB, SB) + min(nH, SH), off_s = SB + SH;
-        rank = half_class ? p.team * (npc - 1) + p.pair : cta;
-    }
+    int n = nA, total = SA, off = SB + SH, off_w = min(nB, SB) + min(nH, SH);
+    int rank = half ? p.team * (a.team_ctas - 1) + p.pair : cta;
+    if (p.team < 0) n = nB, total = SB, off = 0, off_w = 0, rank = cta - in_teams;
+    else if (half && p.pair == a.np - 1) n = nH, total = SH, off = SB, off_w = min(nB, SB), rank = p.team;
     n = min(n, total);  // (fewer tiles than CTAs: one each)
-    p.worker = off_w + rank;
     const float r = __fdiv_rn((float)total, (float)max(n, 1));
-    const int s0 = off_s + share_start(total, n, r, rank);
-    p.own_len = off_s + share_start(total, n, r, rank + 1) - s0;  // 0 from rank n on
+    const int s0 = off + share_start(total, n, r, rank);
+    const int len = off + share_start(total, n, r, rank + 1) - s0;  // 0 from rank n on
     // the unit s0 lies in
-    p.own_b = p.own_h = p.own_o = 0;
-    if (p.own_len > 0) {
-        int base = 0;
-        for (int b0 = 0; b0 < a.B; b0 += 32) {
-            const int b = b0 + lane;
-            int one = 0;
-            if (b < a.B) one = tiles_of(clamp_own(a, b0 ? a.ctx_lens[b] : first_len, P)) + kPad;
-            int incl = a.Hkv * one;
+    int base = 0, ub = 0, uh = 0, uo = 0;
 #pragma unroll 1
-            for (int o = 1; o < 32; o <<= 1) {
-                const int x = __shfl_up_sync(0xffffffffu, incl, o);
-                if (lane >= o) incl += x;
-            }
-            const unsigned past = __ballot_sync(0xffffffffu, base + incl > s0);
-            if (past) {
-                const int src = __ffs(past) - 1;
-                const int x = s0 - base - __shfl_sync(0xffffffffu, incl - a.Hkv * one, src);
-                const int d = __shfl_sync(0xffffffffu, one, src);
-                p.own_b = b0 + src;
-                p.own_h = small_div(x, d);
-                p.own_o = x - p.own_h * d;
-                break;
-            }
-            base += __shfl_sync(0xffffffffu, incl, 31);
+    for (int b0 = 0; b0 < a.B && len > 0; b0 += 32) {
+        const int b = b0 + lane;
+        int one = 0;
+        if (b < a.B) one = tiles_of(clamp_own(a, b0 ? a.ctx_lens[b] : first_len, P)) + kPad;
+        int incl = a.Hkv * one;
+#pragma unroll 1
+        for (int o = 1; o < 32; o <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += x;
         }
+        const unsigned past = __ballot_sync(0xffffffffu, base + incl > s0);
+        if (past) {
+            const int src = __ffs(past) - 1;
+            const int x = s0 - base - __shfl_sync(0xffffffffu, incl - a.Hkv * one, src);
+            const int d = __shfl_sync(0xffffffffu, one, src);
+            ub = b0 + src;
+            uh = small_div(x, d);
+            uo = x - uh * d;
+            break;
+        }
+        base += __shfl_sync(0xffffffffu, incl, 31);
     }
-    if (lane == 0) out = p;
+    if (lane == 0) {
+        p.worker = off_w + rank;
+        p.own_b = ub;
+        p.own_h = uh;
+        p.own_o = uo;
+        p.own_len = len;
+    }
 }
 
 // One CTA's way through its segments; every role walks it for itself.
@@ -242,28 +233,53 @@ struct Segment {
 };
 struct Walk {
     int pair, h, o, left;          // prefix part
-    int b, bh, bo, own_left, keys;  // own part; keys of sequence b
+    int b, bh, bo, own_left, keys;  // own part (own_left < 0: not begun); keys of sequence b
 };
-__device__ __forceinline__ void walk_begin(const PrefixArgs& a, const Plan& p, Walk& w) {
+// One lane of a converged warp.  The roles that copy and multiply run as whole warps, loops included, and elect a
+// lane only around the instructions themselves: those take their operands from uniform registers, and operands
+// computed by a lone lane would be moved there one by one (an MMA then costs its issuer some 150 cycles, more
+// than it costs the tensor core).
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred P;\n\telect.sync _|P, 0xffffffff;\n\tselp.u32 %0, 1, 0, P;\n\t}" : "=r"(p));
+    return p != 0;
+}
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
+
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, const WaitCtx& wc) {
+    return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, wc));
+}
+
+__device__ __forceinline__ void walk_begin(const Plan& p, Walk& w) {
     w.pair = p.pair;
     w.h = p.h;
     w.o = p.o;
     w.left = p.len;
-    w.b = p.own_b;
-    w.bh = p.own_h;
-    w.bo = p.own_o;
-    w.own_left = p.own_len;
-    w.keys = p.own_len > 0 ? clamp_own(a, a.ctx_lens[p.own_b], p.P) : 0;
+    w.own_left = -1;
 }
-__device__ __forceinline__ bool walk_next(const PrefixArgs& a, const Plan& p, Walk& w, Segment& g) {
-    while (w.pair < a.np || w.own_left > 0) {
-        const bool own = w.pair >= a.np;
-        if (!own && w.left == 0) {  // the next pair, over the same keys
-            w.pair += p.pairs;
+__device__ __forceinline__ bool walk_at_own(const PrefixArgs& a, const Walk& w) {
+    return w.own_left < 0 && (w.pair >= a.np || (w.left == 0 && w.pair + a.team_ctas >= a.np));
+}
+// The next segment, or false.  Whole warps; a wait for the own part that runs out ends the walk.
+__device__ __forceinline__ bool walk_next(const PrefixArgs& a, const Plan& p, uint64_t* own_ready, const WaitCtx& wc,
+                                          Walk& w, Segment& g) {
+    while (true) {
+        if (w.pair < a.np && w.left == 0) {  // the next pair, over the same keys
+            w.pair += a.team_ctas;
             w.h = p.h;
             w.o = p.o;
             w.left = p.len;
-            continue;
+        }
+        const bool own = w.pair >= a.np;
+        if (own) {
+            if (w.own_left < 0) {
+                w.own_left = warp_wait(own_ready, 0, wc) ? p.own_len : 0;
+                w.b = p.own_b;
+                w.bh = p.own_h;
+                w.bo = p.own_o;
+                if (w.own_left > 0) w.keys = clamp_own(a, a.ctx_lens[w.b], p.P);
+            }
+            if (w.own_left == 0) return false;
         }
         const int pad = own ? kPad : p.pad;
         const int span = own ? tiles_of(w.keys) + kPad : p.span;
@@ -293,22 +309,6 @@ __device__ __forceinline__ bool walk_next(const PrefixArgs& a, const Plan& p, Wa
         }
         if (g.tiles > 0) return true;
     }
-    return false;
-}
-
-// One lane of a converged warp.  The roles that copy and multiply run as whole warps, loops and waits alike, and
-// elect a lane only around the instructions themselves: those take their operands from uniform registers, and
-// operands computed by a single lane would be moved there one by one (an MMA then costs its issuer some 150
-// cycles, more than it costs the tensor core).
-__device__ __forceinline__ bool elect_one() {
-    uint32_t p;
-    asm volatile("{\n\t.reg .pred P;\n\telect.sync _|P, 0xffffffff;\n\tselp.u32 %0, 1, 0, P;\n\t}" : "=r"(p));
-    return p != 0;
-}
-__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
-
-__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, const WaitCtx& wc) {
-    return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, wc));
 }
 
 // Two fp32 values in one 64-bit register: the FMA and the addition of both in one instruction.
@@ -387,6 +387,7 @@ prefix_attn_split_kernel(const __grid_constant__ CUtensorMap tmKp, const __grid_
     __shared__ uint64_t k_full[NK], k_empty[NK], v_full[NV], v_empty[NV];
     __shared__ uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], pv_done[2], drain_bar;
     __shared__ uint32_t tmem_slot;
+    __shared__ uint64_t own_ready;
     __shared__ int s_abort;
     __shared__ Plan plan;
 
@@ -406,6 +407,7 @@ prefix_attn_split_kernel(const __grid_constant__ CUtensorMap tmKp, const __grid_
             mbar_init(&pv_done[i], 1);
         }
         mbar_init(&drain_bar, 1);
+        mbar_init(&own_ready, 1);
         fence_mbar_init();
         s_abort = 0;
     }
@@ -419,7 +421,7 @@ prefix_attn_split_kernel(const __grid_constant__ CUtensorMap tmKp, const __grid_
     if (warp == 10) tmem_alloc(&tmem_slot, TMEM_COLS);  // the same warp frees it
     griddep_wait();  // lengths are read from here on
     griddep_launch_dependents();
-    if (warp == 0) make_plan(a, cta, plan);
+    if (threadIdx.x == 0) plan_prefix(a, cta, plan);
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
@@ -427,7 +429,7 @@ prefix_attn_split_kernel(const __grid_constant__ CUtensorMap tmKp, const __grid_
     const WaitCtx wc = {&s_abort, a.wait_limit};
 
     Walk w;
-    walk_begin(a, plan, w);
+    walk_begin(plan, w);
     Segment g;
     if (warp == 8) {
         // ---------------- K/V producer ----------------
@@ -435,7 +437,7 @@ prefix_attn_split_kernel(const __grid_constant__ CUtensorMap tmKp, const __grid_
         bool ok = true;
         const int parts = kKeys / a.box_rows;
         const uint32_t part_bytes = kHalfBytes / parts;
-        while (ok && walk_next(a, plan, w, g)) {
+        while (ok && walk_next(a, plan, &own_ready, wc, w, g)) {
             const CUtensorMap* mk = g.own ? &tmKo : &tmKp;
             const CUtensorMap* mv = g.own ? &tmVo : &tmVp;
             const int kvh = uniform(g.kvh), tiles = uniform(g.tiles);
@@ -492,7 +494,7 @@ prefix_attn_split_kernel(const __grid_constant__ CUtensorMap tmKp, const __grid_
         // ---------------- Q producer: a ring of two row tiles ----------------
         int n = 0;
         bool ok = true;
-        while (ok && walk_next(a, plan, w, g)) {
+        while (ok && walk_next(a, plan, &own_ready, wc, w, g)) {
             const int cnt = g.dual_row ? 2 : 1;
             for (int i = 0; i < cnt; ++i) {
                 const int s = n & 1;
@@ -514,103 +516,105 @@ prefix_attn_split_kernel(const __grid_constant__ CUtensorMap tmKp, const __grid_
     } else if (warp == 10) {
         // ---------------- MMA issuer ----------------
         // One thread issues both products, because the tensor core works off its instructions in order: QK^T
-        // of a stream's next tile goes out right behind the PV of its last one and overwrites the P that
-        // PV reads, with no wait in between; and scores in hand mean that PV has completed.
+        // of a stream's next tile goes out behind the PV of its last one and overwrites the P that PV reads,
+        // with no wait in between; and scores in hand mean that PV has completed.
+        // The products are numbered over the CTA's whole walk: product k belongs to stream k & 1 (a dual-row tile
+        // is two of them, and dual-row segments come first).  QK^T runs up to two products ahead of PV.
+        // The control flow of the warp never depends on a wait; once one has run out nothing is issued any more.
         constexpr uint32_t idesc_qk = umma_idesc_bf16(128, kKeys, 0, 0);
         constexpr uint32_t idesc_pv = umma_idesc_bf16(128, D, 0, 1);
         const uint32_t tm0 = uniform(tmem);
         const uint64_t q_desc = umma_smem_desc(smem_base + OFF_Q, 16, 1024);
         const uint64_t k_desc = umma_smem_desc(smem_base + OFF_K, 16, 1024);
         const uint64_t v_desc = umma_smem_desc(smem_base + OFF_V, kHalfBytes, 1024);
-        Walk wq = w;  // the QK^T side runs ahead of the PV side
+        Walk wq = w;
         Segment gq;
-        bool more_q = walk_next(a, plan, wq, gq), more = walk_next(a, plan, w, g);
-        int rows_q = uniform(gq.dual_row ? 2 : 1), tiles_q = uniform(gq.tiles);
-        int rows = rows_q, tiles = tiles_q;  // row tiles and key tiles of the segment
-        int tq = 0, iq = 0, par_q = 0, n_k = 0, n_q = 0;  // tile, row tile, dual-key tiles met, K tiles, Q tiles
-        int t = 0, i = 0, par = 0, n_v = 0;
-        uint32_t busy = 0, p_phase = 0;  // bit s: stream s holds scores whose PV is to come; phase of its p_full
-        bool ok = true;
-        while (more && ok) {
-            while (more_q) {
-                const int s = rows_q == 2 ? iq : par_q & 1;
-                if (busy >> s & 1) break;
-                const int ks = n_k % NK, qs = (n_q + iq) & 1;
-                if (tq == 0) ok = warp_wait(&q_full[qs], ((n_q + iq) >> 1) & 1, wc);
-                if (ok && iq == 0) ok = warp_wait(&k_full[ks], (n_k / NK) & 1, wc);
-                if (!ok) break;
-                tc_fence_after_sync();
-                const uint64_t qd = q_desc + (uint64_t)(qs * (TILE >> 4)), kd = k_desc + (uint64_t)(ks * (TILE >> 4));
-                const bool last = tq + 1 == tiles_q, tile_done = iq + 1 == rows_q;
-                if (elect_one()) {
-#pragma unroll
-                    for (int kk = 0; kk < D / 16; ++kk) {
-                        const uint32_t off = (kk >> 2) * (kHalfBytes >> 4) + (kk & 3) * 2;
-                        umma_bf16_ss(tm0 + COL_S + 128u * s, qd + off, kd + off, idesc_qk, kk > 0);
-                    }
-                    umma_commit(&s_full[s]);
-                    if (last) umma_commit(&q_empty[qs]);
-                    if (tile_done) umma_commit(&k_empty[ks]);
-                }
-                __syncwarp();
-                busy |= 1u << s;
-                if (!tile_done) {
-                    iq = 1;
-                    continue;
-                }
-                ++n_k;
-                if (rows_q == 1) ++par_q;
-                iq = 0;
-                if (++tq == tiles_q) {
+        int rows_q = 0, tiles_q = 0, tq = 0, iq = 0, kq = 0, ks = 0, k_par = 0, n_q = 0;  // QK^T side: segment, place in it, K slot
+        int rows = 0, tiles = 0, t = 0, i = 0, k = 0, vs = 0, v_par = 0;                  // PV side, V slot
+        bool ended = false, alive = true;
+        while (true) {
+            while (kq < k + 2 && !ended) {
+                if (tq == tiles_q) {
+                    // (the own part may not be worked out yet: wait for it only when nothing else is left to do)
+                    if (walk_at_own(a, wq) && k < kq && !__all_sync(0xffffffffu, mbar_try_wait(&own_ready, 0))) break;
+                    ended = !walk_next(a, plan, &own_ready, wc, wq, gq);
+                    if (ended) break;
                     n_q += rows_q;
-                    tq = 0;
-                    more_q = walk_next(a, plan, wq, gq);
                     rows_q = uniform(gq.dual_row ? 2 : 1);
                     tiles_q = uniform(gq.tiles);
+                    tq = 0;
+                }
+                const int s = kq & 1, qs = (n_q + iq) & 1;
+                const bool first = tq == 0, last = tq + 1 == tiles_q, tile_done = iq + 1 == rows_q;
+                if (elect_one()) {
+                    if (alive && first) alive = mbar_wait_bounded(&q_full[qs], ((n_q + iq) >> 1) & 1, wc);
+                    if (alive && iq == 0) alive = mbar_wait_bounded(&k_full[ks], k_par, wc);
+                    if (alive) {
+                        tc_fence_after_sync();
+                        const uint64_t qd = q_desc + (uint64_t)(qs * (TILE >> 4)), kd = k_desc + (uint64_t)(ks * (TILE >> 4));
+#pragma unroll
+                        for (int kk = 0; kk < D / 16; ++kk) {
+                            const uint32_t off = (kk >> 2) * (kHalfBytes >> 4) + (kk & 3) * 2;
+                            umma_bf16_ss(tm0 + COL_S + 128u * s, qd + off, kd + off, idesc_qk, kk > 0);
+                        }
+                        umma_commit(&s_full[s]);
+                        if (tile_done) umma_commit(&k_empty[ks]);
+                        if (last) umma_commit(&q_empty[qs]);
+                    }
+                }
+                __syncwarp();
+                ++kq;
+                iq = tile_done ? 0 : 1;
+                if (tile_done) {
+                    ++tq;
+                    if (++ks == NK) ks = 0, k_par ^= 1;
                 }
             }
-            if (!ok) break;
-            const int s = rows == 2 ? i : par & 1;
-            const int vs = n_v % NV;
-            if (i == 0) ok = warp_wait(&v_full[vs], (n_v / NV) & 1, wc);
-            if (ok) ok = warp_wait(&p_full[s], p_phase >> s & 1, wc);
-            if (!ok) break;
-            p_phase ^= 1u << s;
-            tc_fence_after_sync();
-            const int turns = rows == 2 ? 1 : 2;     // tiles from one of a stream to its next
+            if (k == kq) break;
+            if (t == tiles) {
+                walk_next(a, plan, &own_ready, wc, w, g);  // (there is one: its QK^T went out)
+                rows = uniform(g.dual_row ? 2 : 1);
+                tiles = uniform(g.tiles);
+                t = 0;
+            }
+            const int s = k & 1;
+            const int turns = 3 - rows;              // tiles from one of a stream to its next
             const bool fresh = t < turns;            // the stream's first tile of the segment
             const bool last = t >= tiles - turns;    // ... and its last
             const bool tile_done = i + 1 == rows;
-            const uint64_t vd = v_desc + (uint64_t)(vs * (TILE >> 4));
             if (elect_one()) {
+                if (alive && i == 0) alive = mbar_wait_bounded(&v_full[vs], v_par, wc);
+                if (alive) alive = mbar_wait_bounded(&p_full[s], (k >> 1) & 1, wc);
+                if (alive) {
+                    tc_fence_after_sync();
+                    const uint64_t vd = v_desc + (uint64_t)(vs * (TILE >> 4));
+                    const uint32_t d = tm0 + COL_O + 128u * s, pm = tm0 + COL_S + 128u * s;
 #pragma unroll
-                for (int kk = 0; kk < kKeys / 16; ++kk)
-                    umma_bf16_ts(tm0 + COL_O + 128u * s, tm0 + COL_S + 128u * s + 8 * kk, vd + kk * (2048 >> 4), idesc_pv,
-                                 (!fresh || kk > 0) ? 1u : 0u);
-                if (last) umma_commit(&pv_done[s]);
-                if (tile_done) umma_commit(&v_empty[vs]);
+                    for (int kk = 0; kk < kKeys / 16; ++kk)
+                        umma_bf16_ts(d, pm + 8 * kk, vd + kk * (2048 >> 4), idesc_pv, (!fresh || kk > 0) ? 1u : 0u);
+                    if (tile_done) umma_commit(&v_empty[vs]);
+                    if (last) umma_commit(&pv_done[s]);
+                }
             }
             __syncwarp();
-            busy &= ~(1u << s);
-            if (!tile_done) {
-                i = 1;
-                continue;
-            }
-            ++n_v;
-            i = 0;
-            if (rows == 1) ++par;
-            if (++t == tiles) {
-                t = 0;
-                more = walk_next(a, plan, w, g);
-                rows = uniform(g.dual_row ? 2 : 1);
-                tiles = uniform(g.tiles);
+            ++k;
+            i = tile_done ? 0 : 1;
+            if (tile_done) {
+                ++t;
+                if (++vs == NV) vs = 0, v_par ^= 1;
             }
         }
-        if (!ok) {  // every MMA issued here has completed before tensor memory is freed
-            if (elect_one()) umma_commit(&drain_bar);
-            __syncwarp();
+        // every MMA issued here has completed before tensor memory is freed
+        if (elect_one()) {
+            umma_commit(&drain_bar);
             mbar_wait_drain(&drain_bar, 0);
         }
+        __syncwarp();
+    } else if (warp == 11) {
+        // ---------------- planner of the own part ----------------
+        plan_own(a, cta, plan);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&own_ready);
     } else if (warp < 8) {
         // ---------------- softmax warps: stream = warp / 4, row of the tile = 32 (warp % 4) + lane ----------------
         const int stream = warp >> 2;
@@ -621,7 +625,7 @@ prefix_attn_split_kernel(const __grid_constant__ CUtensorMap tmKp, const __grid_
         const float c = a.scale_log2;
         int n = 0, par = 0, cnt = 0, segs = 0;  // CTA-wide tile index, dual-key tiles met, tiles and segments of this stream
         bool ok = true;
-        while (ok && walk_next(a, plan, w, g)) {
+        while (ok && walk_next(a, plan, &own_ready, wc, w, g)) {
             // the tile's rows: (sequence, row, head in group) of the batch, or (row, head) of one sequence
             const int tile_row0 = (2 * g.pair + (g.dual_row ? stream : 0)) * a.rows_tile;
             const int rows = g.own ? a.GR : min(a.rows_tile, a.B * a.R - tile_row0) * a.G;
@@ -758,18 +762,22 @@ prefix_attn_split_kernel(const __grid_constant__ CUtensorMap tmKp, const __grid_
 
 // Merge: out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s over the partials of a row: those of the prefix
 // (one per team whose range touches the KV head) and those of the row's own sequence.  A block takes 32
-// rows of a KV head (lane = row: slots are stored so that this reads whole lines) and 32 columns, four
-// to a warp.  The order of the sums is fixed: results do not depend on timing.
+// rows of a KV head (lane = row: slots are stored so that this reads whole lines) and 16 columns; its warps
+// take the slots w, w + 8, ... each, all loads of four slots in flight at once, and meet in shared memory.
+// Latency is what counts here (the call's partials are some 20 MB, in L2): one round trip for the ranges, one or
+// two for the slots.  The order of the sums is fixed: results do not depend on timing.
 template <int D>
 __global__ void __launch_bounds__(256)
 prefix_attn_merge_kernel(const __grid_constant__ PrefixArgs a, __nv_bfloat16* out, float* lse_out, float* out_f32) {
+    constexpr int UN = 4;
+    __shared__ float4 sh_acc[8][4][32];
     __shared__ float sh_m[8][32], sh_l[8][32];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int kvh = blockIdx.y;
     const int total_rows = a.B * a.R * a.G;
-    const int flat = blockIdx.x * 32 + lane;
-    const bool valid = flat < total_rows;
-    const int f = (valid ? flat : total_rows - 1) / a.G, gh = (valid ? flat : total_rows - 1) - f * a.G;  // (sequence, row), head in group
+    const int row0 = blockIdx.x * 32;
+    const int flat = min(row0 + lane, total_rows - 1);  // past the end: the last row again, not written
+    const int f = flat / a.G, gh = flat - f * a.G;      // (sequence, row), head in group
     const int b = f / a.R, i = f - b * a.R;
     const int rt = f / a.rows_tile;
     const int prow = (f - rt * a.rows_tile) * a.G + gh;
@@ -777,75 +785,97 @@ prefix_attn_merge_kernel(const __grid_constant__ PrefixArgs a, __nv_bfloat16* ou
     const bool dual = 2 * pair + 1 < a.nrt;
     const int orow = i * a.G + gh;
     const int unit = b * a.Hkv + kvh;
-    const long long sp = slot_floats(128, D), so = slot_floats(a.GR, D);
+    const int sp = (int)slot_floats(128, D), so = (int)slot_floats(a.GR, D);
 
     griddep_wait();
     griddep_launch_dependents();
-    const int P = clamp_prefix(a, *a.prefix_len);
-    int2 pr = P > 0 ? __ldcg(a.prefix_range + kvh) : make_int2(0, -1);
-    int2 orr = __ldcg(a.own_range + unit);
+    const int given = *a.prefix_len;
+    int2 pr = __ldcg(a.prefix_range + kvh), orr = __ldcg(a.own_range + unit);
     // (a split kernel whose waits ran out may not have written them: whatever they hold, stay inside the slots)
-    if (pr.x < 0 || pr.y >= a.max_teams) pr = make_int2(0, -1);
+    if (clamp_prefix(a, given) == 0 || pr.x < 0 || pr.y >= a.max_teams) pr = make_int2(0, -1);
     if (orr.x < 0 || orr.y >= a.num_ctas) orr = make_int2(0, -1);
-    // The row's slots as one list: index x < np_slots is in the prefix part (one slot per team, or two where a
-    // single row tile's keys went to both streams), the rest in the own part (two per worker).
-    const int per = dual ? 1 : 2;
-    const int n_p = max(0, pr.y - pr.x + 1) * per, n_all = n_p + max(0, orr.y - orr.x + 1) * 2;
-    const float* pbase = a.part_prefix + (size_t)((pr.x + kvh) * 2 * a.np + 2 * pair + (dual ? rt & 1 : 0)) * sp;
-    const long long pstep = (long long)2 * a.np * sp;
+    // The row's slots as one list: the first n_p in the prefix part (one per team, or two where a single row tile's
+    // keys went to both streams), the rest in the own part (two per worker).
+    const int n_p = max(0, pr.y - pr.x + 1) << (dual ? 0 : 1), n_all = n_p + max(0, orr.y - orr.x + 1) * 2;
+    const float* pbase = a.part_prefix + (size_t)((pr.x + kvh) * 2 * a.np + (dual ? rt : 2 * pair)) * sp;
     const float* obase = a.part_own + (size_t)(orr.x + unit) * 2 * so;
-    auto slot_of = [&](int x) -> const float* {
-        if (x < n_p) return dual ? pbase + x * pstep : pbase + (x >> 1) * pstep + (x & 1) * sp;
-        return obase + (x - n_p) * so;
-    };
+    const int d4 = blockIdx.z * 4;
+
     float m = -INFINITY, l = 0.f;
-    for (int x = warp; x < n_all; x += 8) {
-        const float* s = slot_of(x);
-        const bool pre = x < n_p;
-        const float ms = s[(pre ? 128LL : a.GR) * D + (pre ? prow : orow)];
-        const float ls = s[(pre ? 128LL : a.GR) * (D + 1) + (pre ? prow : orow)];
-        if (ms == -INFINITY) continue;  // (its sum is 0)
-        if (ms > m) {
-            l = l * exp2f(m - ms) + ls;
-            m = ms;
-        } else {
-            l += ls * exp2f(ms - m);
+    float4 acc[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int x0 = warp; x0 < n_all; x0 += 8 * UN) {
+        float ms[UN], ls[UN];
+        float4 o[UN][4];
+#pragma unroll
+        for (int u = 0; u < UN; ++u) {
+            const int x = x0 + 8 * u;
+            ms[u] = -INFINITY;
+            if (x < n_all) {
+                const bool pre = x < n_p;
+                const int rows = pre ? 128 : a.GR, r = pre ? prow : orow;
+                const float* s = pre ? (dual ? pbase + (size_t)x * 2 * a.np * sp : pbase + ((size_t)(x >> 1) * 2 * a.np + (x & 1)) * sp)
+                                     : obase + (size_t)(x - n_p) * so;
+                ms[u] = __ldcg(s + rows * D + r);
+                ls[u] = __ldcg(s + rows * (D + 1) + r);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[u][j] = __ldcg(reinterpret_cast<const float4*>(s) + (d4 + j) * rows + r);
+            }
+        }
+        float top = m;
+#pragma unroll
+        for (int u = 0; u < UN; ++u) top = fmaxf(top, ms[u]);
+        const float keep = m == -INFINITY ? 0.f : exp2f(m - top);
+        m = top;
+        l *= keep;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[j].x *= keep, acc[j].y *= keep, acc[j].z *= keep, acc[j].w *= keep;
+#pragma unroll
+        for (int u = 0; u < UN; ++u) {
+            if (ms[u] == -INFINITY) continue;  // an untouched slot holds neither a sum nor an O row: its bits are not used
+            const float wgt = exp2f(ms[u] - top);
+            l += wgt * ls[u];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                acc[j].x += wgt * o[u][j].x;
+                acc[j].y += wgt * o[u][j].y;
+                acc[j].z += wgt * o[u][j].z;
+                acc[j].w += wgt * o[u][j].w;
+            }
         }
     }
     sh_m[warp][lane] = m;
     sh_l[warp][lane] = l;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sh_acc[warp][j][lane] = acc[j];
     __syncthreads();
-    float M = -INFINITY;
+    if (threadIdx.x >= 128) return;
+    // four neighbouring threads write the 16 columns of a row
+    const int row = threadIdx.x >> 2, j = threadIdx.x & 3;
+    if (row0 + row >= total_rows) return;
+    float M = -INFINITY, L = 0.f;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) M = fmaxf(M, sh_m[k][lane]);
-    float Lsum = 0.f;
+    for (int k = 0; k < 8; ++k) M = fmaxf(M, sh_m[k][row]);
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-        if (sh_m[k][lane] != -INFINITY) Lsum += sh_l[k][lane] * exp2f(sh_m[k][lane] - M);
-
-    const int d4 = blockIdx.z * 8 + warp;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int x = 0; x < n_all; ++x) {
-        const float* s = slot_of(x);
-        const bool pre = x < n_p;
-        const int rows = pre ? 128 : a.GR, r = pre ? prow : orow;
-        const float ms = s[(long long)rows * D + r];
-        const float4 o = *reinterpret_cast<const float4*>(s + ((long long)d4 * rows + r) * 4);
-        if (ms != -INFINITY) {  // an untouched slot holds no O: its bits are not used
-            const float wgt = exp2f(ms - M);
-            acc.x += wgt * o.x;
-            acc.y += wgt * o.y;
-            acc.z += wgt * o.z;
-            acc.w += wgt * o.w;
-        }
+    for (int k = 0; k < 8; ++k) {
+        if (sh_m[k][row] == -INFINITY) continue;
+        const float wgt = exp2f(sh_m[k][row] - M);
+        const float4 o = sh_acc[k][j][row];
+        L += wgt * sh_l[k][row];
+        v.x += wgt * o.x;
+        v.y += wgt * o.y;
+        v.z += wgt * o.z;
+        v.w += wgt * o.w;
     }
-    if (!valid) return;
-    const size_t orow_g = ((size_t)f * a.Hq + (size_t)kvh * a.G + gh);
-    const float4 v = make_float4(acc.x / Lsum, acc.y / Lsum, acc.z / Lsum, acc.w / Lsum);
-    *reinterpret_cast<uint2*>(out + orow_g * D + d4 * 4) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
-    if (out_f32) *reinterpret_cast<float4*>(out_f32 + orow_g * D + d4 * 4) = v;
-    if (lse_out && d4 == 0) lse_out[orow_g] = (M + log2f(Lsum)) * 0.69314718055994530942f;
+    const int fo = (row0 + row) / a.G, go = row0 + row - fo * a.G;
+    const size_t at = (size_t)fo * a.Hq + (size_t)kvh * a.G + go;
+    const float inv = 1.f / L;
+    v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+    *reinterpret_cast<uint2*>(out + at * D + (d4 + j) * 4) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+    if (out_f32) *reinterpret_cast<float4*>(out_f32 + at * D + (d4 + j) * 4) = v;
+    if (lse_out && d4 + j == 0) lse_out[at] = (M + log2f(L)) * 0.69314718055994530942f;
 }
 
 // ---- host side ----------------------------------------------------------------------------
@@ -929,7 +959,7 @@ int launch(const CUtensorMap (&tm)[5], const PrefixArgs& a, __nv_bfloat16* out, 
                                       tm[0], tm[1], tm[2], tm[3], tm[4], a));
     if (split_done) RAPID_CUDA_CHECK(cudaEventRecord(static_cast<cudaEvent_t>(split_done), stream));
     const int rows = a.B * a.R * a.G;
-    RAPID_CUDA_CHECK(launch_dependent(prefix_attn_merge_kernel<D>, dim3((rows + 31) / 32, a.Hkv, D / 32), dim3(256), 0,
+    RAPID_CUDA_CHECK(launch_dependent(prefix_attn_merge_kernel<D>, dim3((rows + 31) / 32, a.Hkv, D / 16), dim3(256), 0,
                                       stream, a, out, lse, out_f32));
     count_launch(2);
     return RAPID_OK;
@@ -1091,8 +1121,10 @@ int launch_verify_attention_prefix(const void* q, const void* k_prefix, const vo
     a.nrt = (int)nrt;
     a.np = np;
     a.num_ctas = num_ctas;
-    a.max_teams = num_ctas / (np < num_ctas ? np : num_ctas);
+    a.team_ctas = np < num_ctas ? np : num_ctas;
+    a.max_teams = num_ctas / a.team_ctas;
     a.rounds = (np + num_ctas - 1) / num_ctas;
+    a.row_cost = (nrt > 1 ? 2 : 1) * a.rounds;
     a.scale_log2 = scale * 1.4426950408889634f;
     a.wait_limit = wait_limit;
 
