@@ -9,18 +9,20 @@
 // and a CTA takes two such row tiles through the same K/V tiles.  Each sequence's own keys are work of
 // the same kernel, as further units; the merge kernel joins what the units left by their log-sum-exp.
 //
-// Segments.  A CTA works through segments: a run of 128-key tiles of one unit.
-//   dual-row segment  prefix of one KV head, two row tiles: stream s (one of two groups of four softmax warps,
-//                     with its own S and O accumulators) takes row tile s through every key tile;
+// Segments.  A CTA works through segments: a run of 128-key tiles of one unit.  Two streams (groups of four softmax
+// warps, each with S and O accumulators and an MMA issuer of its own) take every tile in blocks of 64 keys:
+//   dual-row segment  prefix of one KV head, two row tiles: stream s takes row tile s through both blocks;
 //   dual-key segment  one row tile (the last prefix tile of an odd count, or the R*G rows of one sequence over
-//                     its own keys): the streams take alternate key tiles of the CTA, each with a partial
-//                     of its own, so that segments of a single tile alternate between them as well.
+//                     its own keys): stream s takes block s, and leaves a partial of its own.
 //
-//   S_s[128 x 128] = Q_s K^T      A = Q tile, B = K tile, both K-major in shared memory
-//   O_s[128 x D]  += P_s V        A = P (bf16, over the first half of S_s's columns), B = V tile, MN-major
+//   S_s[128 x 64] = Q_s K_block^T   A = Q tile, B = 64 rows of the K tile, both K-major in shared memory
+//   O_s[128 x D] += P_s V_block     A = P (bf16, over the first half of the S block's columns), B = V rows, MN-major
+//
+// S has room for two blocks: while the softmax warps are at one, the PV and the next QK^T of the other run (with
+// one S of 128 keys a stream's softmax and products alternate: 190 us for the 60K-key batch of 1,120 rows).
 //
 // Work split (worked out by every CTA for itself: no plan kernel, no plan to go stale).  Cost is counted in
-// single-stream tiles: 2 for a dual-row tile, 1 for a dual-key tile, kPad for changing to another unit.
+// half tiles of a stream's work: 2 for a dual-row tile, 1 for a dual-key tile, kPad for changing to another unit.
 // With np pairs of row tiles the prefix is cut into equal ranges of key tiles, each for a team of np CTAs, one
 // pair each: a team reads the same K/V tiles at the same time, so they leave HBM once.  The sequences'
 // own tiles fill up every CTA to the same level (CTAs outside the teams first, then those with a single
@@ -29,8 +31,10 @@
 // Bound: up to 256 rows per KV head (one pair) a K/V tile of 64 KB is read for every 256 x 128 scores, and HBM
 // is the limit; from two pairs on the tensor cores and the exponentials are.
 //
-// Waits are bounded as everywhere in this library; see mbar_wait_bounded.  Every mbarrier here is one
-// whose next phase cannot complete before all its waiters have passed the current one.
+// Waits are bounded as everywhere in this library; see mbar_wait_bounded.  A parity wait tells a phase from its
+// neighbours only, so every barrier here is one that at a wait is in the phase waited for or just past it.
+// Per stream there are two of each block barrier, for even and for odd blocks: scores of block j in hand
+// mean that the PV of block j - 2 has completed, but say nothing of j - 1.
 #include <math.h>
 
 #include "common.cuh"
@@ -41,7 +45,8 @@ namespace rapid {
 namespace {
 
 constexpr int kKeys = 128;             // keys per tile
-constexpr int kThreads = 384;          // two softmax groups of 128, then a warp each for K/V copies, Q copies, MMAs, planning
+constexpr int kThreads = 384;          // two softmax groups of 128; the producer, the walk, an MMA warp for each stream
+constexpr int kBlock = 64;             // keys of a block: what a stream takes at a time
 constexpr int kHalfBytes = kKeys * 128;  // one 64-column half of a tile of 128 rows
 constexpr int kPad = 3;                // single-stream tiles that a change of unit costs
 constexpr int kMaxPrefixCtas = 256;
@@ -92,8 +97,7 @@ __device__ __forceinline__ int clamp_own(const PrefixArgs& a, int L, int P) {
 __device__ __forceinline__ int tiles_of(int keys) { return (keys + kKeys - 1) / kKeys; }
 
 // What a CTA does.  The prefix part follows from the prefix's length alone and is worked out before anything
-// else; the own part needs every sequence's length, is worked out by a warp of its own while the CTA is at
-// its prefix tiles, and is waited for (own_ready) only by who comes to it.
+// else; the own part needs every sequence's length and is worked out while the CTA is at its prefix tiles.
 struct Plan {
     int P, nt, pad, span;   // prefix keys and tiles; virtual tiles in front of every KV head's, and those with the real ones
     int teams, team, pair;  // teams, the CTA's team (-1: none) and its first pair of row tiles
@@ -224,91 +228,91 @@ __device__ __noinline__ void plan_own(const PrefixArgs& a, int cta, Plan& p) {
     }
 }
 
-// One CTA's way through its segments; every role walks it for itself.
-struct Segment {
-    bool own, dual_row;
-    int b, kvh, pair;   // sequence (own) or pair of row tiles (prefix)
-    int tile0, tiles;   // run of tiles inside the unit
-    int keys;           // keys of the unit: own keys or prefix keys
-};
-struct Walk {
-    int pair, h, o, left;          // prefix part
-    int b, bh, bo, own_left, keys;  // own part (own_left < 0: not begun); keys of sequence b
-};
-// One lane of a converged warp.  The roles that copy and multiply run as whole warps, loops included, and elect a
-// lane only around the instructions themselves: those take their operands from uniform registers, and operands
-// computed by a lone lane would be moved there one by one (an MMA then costs its issuer some 150 cycles, more
-// than it costs the tensor core).
+// One lane of a converged warp.
 __device__ __forceinline__ bool elect_one() {
     uint32_t p;
     asm volatile("{\n\t.reg .pred P;\n\telect.sync _|P, 0xffffffff;\n\tselp.u32 %0, 1, 0, P;\n\t}" : "=r"(p));
     return p != 0;
 }
-__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
-
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, const WaitCtx& wc) {
     return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, wc));
 }
 
-__device__ __forceinline__ void walk_begin(const Plan& p, Walk& w) {
-    w.pair = p.pair;
-    w.h = p.h;
-    w.o = p.o;
-    w.left = p.len;
-    w.own_left = -1;
-}
-__device__ __forceinline__ bool walk_at_own(const PrefixArgs& a, const Walk& w) {
-    return w.own_left < 0 && (w.pair >= a.np || (w.left == 0 && w.pair + a.team_ctas >= a.np));
-}
-// The next segment, or false.  Whole warps; a wait for the own part that runs out ends the walk.
-__device__ __forceinline__ bool walk_next(const PrefixArgs& a, const Plan& p, uint64_t* own_ready, const WaitCtx& wc,
-                                          Walk& w, Segment& g) {
-    while (true) {
-        if (w.pair < a.np && w.left == 0) {  // the next pair, over the same keys
-            w.pair += a.team_ctas;
-            w.h = p.h;
-            w.o = p.o;
-            w.left = p.len;
-        }
-        const bool own = w.pair >= a.np;
-        if (own) {
-            if (w.own_left < 0) {
-                w.own_left = warp_wait(own_ready, 0, wc) ? p.own_len : 0;
-                w.b = p.own_b;
-                w.bh = p.own_h;
-                w.bo = p.own_o;
-                if (w.own_left > 0) w.keys = clamp_own(a, a.ctx_lens[w.b], p.P);
-            }
-            if (w.own_left == 0) return false;
-        }
-        const int pad = own ? kPad : p.pad;
-        const int span = own ? tiles_of(w.keys) + kPad : p.span;
-        const int o = own ? w.bo : w.o;
-        const int e = min(span, o + (own ? w.own_left : w.left));
-        g.own = own;
-        g.dual_row = !own && 2 * w.pair + 1 < a.nrt;
-        g.b = own ? w.b : 0;
-        g.kvh = own ? w.bh : w.h;
-        g.pair = own ? 0 : w.pair;
-        g.keys = own ? w.keys : p.P;
-        g.tile0 = max(0, o - pad);
-        g.tiles = max(0, e - pad) - g.tile0;
-        const int next = e == span ? 0 : e;
-        if (own) {
-            w.own_left -= e - o;
-            w.bo = next;
-            if (e == span && ++w.bh == a.Hkv) {
-                w.bh = 0;
-                ++w.b;
-                if (w.own_left > 0) w.keys = clamp_own(a, a.ctx_lens[w.b], p.P);
-            }
-        } else {
-            w.left -= e - o;
-            w.o = next;
-            w.h += e == span;
-        }
-        if (g.tiles > 0) return true;
+// A CTA's segments: one warp walks through its plan and hands them to the other roles through a ring in shared
+// memory (the walk inlined in every role was 700 to 2,900 cycles a segment in each, most of it instruction fetch).
+struct __align__(16) Segment {
+    int tiles;          // run of tiles inside the unit; 0 = the end
+    int flags;          // kOwn, kDualRow
+    int keys, tile0;    // keys of the unit (own keys or prefix keys), first tile
+    int b, kvh, pair;   // sequence (own) or pair of row tiles (prefix)
+    int reserved;
+};
+constexpr int kOwn = 1, kDualRow = 2;
+constexpr int kRing = 8;       // segments in the ring
+constexpr int kRingUsers = 11;  // arrivals that free one: 8 softmax warps, the producer, two MMA threads
+
+struct Ring {
+    Segment seg[kRing];
+    uint64_t full[kRing], empty[kRing];
+};
+// Puts segment number i into the ring (a whole warp; lane 0 writes).
+__device__ __forceinline__ bool ring_put(Ring& r, int i, const Segment& g, const WaitCtx& wc) {
+    const int s = i & (kRing - 1);
+    if (i >= kRing && !warp_wait(&r.empty[s], (i / kRing - 1) & 1, wc)) return false;
+    if ((threadIdx.x & 31) == 0) {
+        r.seg[s] = g;
+        mbar_arrive(&r.full[s]);
     }
+    __syncwarp();
+    return true;
+}
+
+__device__ __forceinline__ void walk(const PrefixArgs& a, const Plan& p, Ring& ring, int cta, Plan& out, const WaitCtx& wc) {
+    int n = 0;
+    Segment g = {};
+    // the prefix part: every pair of the CTA's over the same run of tiles
+    for (int pair = p.pair; pair < a.np; pair += a.team_ctas) {
+        int h = p.h, o = p.o, left = p.len;
+        while (left > 0) {
+            const int e = min(p.span, o + left);
+            g.flags = 2 * pair + 1 < a.nrt ? kDualRow : 0;
+            g.keys = p.P;
+            g.kvh = h;
+            g.pair = pair;
+            g.tile0 = max(0, o - p.pad);
+            g.tiles = max(0, e - p.pad) - g.tile0;
+            left -= e - o;
+            o = 0;
+            ++h;
+            if (g.tiles > 0 && !ring_put(ring, n++, g, wc)) return;
+        }
+    }
+    // the own part
+    plan_own(a, cta, out);
+    __syncwarp();
+    int b = p.own_b, h = p.own_h, o = p.own_o, left = p.own_len, keys = 0;
+    if (left > 0) keys = clamp_own(a, a.ctx_lens[b], p.P);
+    g.flags = kOwn;
+    g.pair = 0;
+    while (left > 0) {
+        const int span = tiles_of(keys) + kPad;
+        const int e = min(span, o + left);
+        g.keys = keys;
+        g.b = b;
+        g.kvh = h;
+        g.tile0 = max(0, o - kPad);
+        g.tiles = max(0, e - kPad) - g.tile0;
+        left -= e - o;
+        o = 0;
+        if (left > 0 && ++h == a.Hkv) {
+            h = 0;
+            ++b;
+            keys = clamp_own(a, a.ctx_lens[b], p.P);
+        }
+        if (g.tiles > 0 && !ring_put(ring, n++, g, wc)) return;
+    }
+    g.tiles = 0;
+    ring_put(ring, n, g, wc);
 }
 
 // Two fp32 values in one 64-bit register: the FMA and the addition of both in one instruction.
@@ -337,21 +341,11 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return r;
 }
 
-// Moves the references of the rows that ask for it (`move`) up to `top`: the row's sum, its O accumulators (at
-// rest: the scores in hand came behind the PV of the tile before) and the probabilities of the tile that
-// are stored already (of its first 32 * chunks keys) are scaled by 2^(old - new).  References are whole
-// numbers, so the factor is a power of two and the stored bf16 probabilities lose nothing.  Rare: kept out
-// of the way.
+// Scales a row's O accumulators when its reference moves.  Rare: kept out of the way.
 template <int D>
-__device__ __noinline__ void move_reference(bool move, float top, float& m_ref, float& l_run, uint32_t tO, bool has_o,
-                                            uint32_t tP, int chunks) {
-    const float factor = move ? fast_exp2(m_ref - top) : 1.f;  // 0 when there was no reference
-    if (move) {
-        l_run *= factor;
-        m_ref = top;
-    }
+__device__ __noinline__ void scale_o(uint32_t tO, float factor) {
 #pragma unroll 1
-    for (int i = 0; i < (has_o ? D / 16 : 0); ++i) {
+    for (int i = 0; i < D / 16; ++i) {
         uint32_t o[16];
         tmem_ld_x16(tO + 16 * i, o);
         tmem_wait_ld();
@@ -360,16 +354,6 @@ __device__ __noinline__ void move_reference(bool move, float top, float& m_ref, 
         tmem_st_x16(tO + 16 * i, o);
     }
     tmem_wait_st();
-#pragma unroll 1
-    for (int i = 0; i < chunks; ++i) {
-        uint32_t o[16];
-        tmem_ld_x16(tP + 16 * i, o);
-        tmem_wait_ld();
-#pragma unroll
-        for (int k = 0; k < 16; ++k)
-            o[k] = pack_bf16x2(__uint_as_float(o[k] << 16) * factor, __uint_as_float(o[k] & 0xffff0000u) * factor);
-        tmem_st_x16(tP + 16 * i, o);
-    }
 }
 
 template <int D>
@@ -385,9 +369,9 @@ prefix_attn_split_kernel(const __grid_constant__ CUtensorMap tmKp, const __grid_
 
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t k_full[NK], k_empty[NK], v_full[NV], v_empty[NV];
-    __shared__ uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], pv_done[2], drain_bar;
+    __shared__ uint64_t q_full[2], q_empty[2], s_full[2][2], p_full[2][2], o_rest[2][2], drain_bar[2];
     __shared__ uint32_t tmem_slot;
-    __shared__ uint64_t own_ready;
+    __shared__ Ring ring;
     __shared__ int s_abort;
     __shared__ Plan plan;
 
@@ -397,17 +381,15 @@ prefix_attn_split_kernel(const __grid_constant__ CUtensorMap tmKp, const __grid_
     const int cta = blockIdx.x;
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < NK; ++i) mbar_init(&k_full[i], 1), mbar_init(&k_empty[i], 1);
-        for (int i = 0; i < NV; ++i) mbar_init(&v_full[i], 1), mbar_init(&v_empty[i], 1);
+        for (int i = 0; i < NK; ++i) mbar_init(&k_full[i], 1), mbar_init(&k_empty[i], 2);
+        for (int i = 0; i < NV; ++i) mbar_init(&v_full[i], 1), mbar_init(&v_empty[i], 2);
         for (int i = 0; i < 2; ++i) {
             mbar_init(&q_full[i], 1);
-            mbar_init(&q_empty[i], 1);
-            mbar_init(&s_full[i], 1);
-            mbar_init(&p_full[i], 4);
-            mbar_init(&pv_done[i], 1);
+            mbar_init(&q_empty[i], 2);
+            for (int b = 0; b < 2; ++b) mbar_init(&s_full[i][b], 1), mbar_init(&p_full[i][b], 4), mbar_init(&o_rest[i][b], 1);
+            mbar_init(&drain_bar[i], 1);
         }
-        mbar_init(&drain_bar, 1);
-        mbar_init(&own_ready, 1);
+        for (int i = 0; i < kRing; ++i) mbar_init(&ring.full[i], 1), mbar_init(&ring.empty[i], kRingUsers);
         fence_mbar_init();
         s_abort = 0;
     }
@@ -428,26 +410,45 @@ prefix_attn_split_kernel(const __grid_constant__ CUtensorMap tmKp, const __grid_
     const uint32_t tmem = tmem_slot;
     const WaitCtx wc = {&s_abort, a.wait_limit};
 
-    Walk w;
-    walk_begin(plan, w);
-    Segment g;
+    int r = 0;  // segments taken from the ring; a role that comes to the end marker stops
+    // (a wait that runs out ends a role's work as well)
+#define RAPID_SEG(i) ring.seg[(i) & (kRing - 1)]
     if (warp == 8) {
-        // ---------------- K/V producer ----------------
-        int n_k = 0, n_v = 0;  // K and V tiles whose copies were issued
+        // ---------------- producer: Q tiles (a ring of two) and K/V tiles ----------------
+        int n_q = 0, n_k = 0, n_v = 0;  // tiles whose copies were issued
         bool ok = true;
         const int parts = kKeys / a.box_rows;
         const uint32_t part_bytes = kHalfBytes / parts;
-        while (ok && walk_next(a, plan, &own_ready, wc, w, g)) {
-            const CUtensorMap* mk = g.own ? &tmKo : &tmKp;
-            const CUtensorMap* mv = g.own ? &tmVo : &tmVp;
-            const int kvh = uniform(g.kvh), tiles = uniform(g.tiles);
-            for (int t = 0; t < tiles; ++t) {
+        while (ok) {
+            ok = warp_wait(&ring.full[r & (kRing - 1)], (r / kRing) & 1, wc);
+            const Segment g = RAPID_SEG(r);
+            if (!ok || g.tiles == 0) break;
+            const bool own = g.flags & kOwn;
+            const CUtensorMap* mk = own ? &tmKo : &tmKp;
+            const CUtensorMap* mv = own ? &tmVo : &tmVp;
+            const int row_tiles = g.flags & kDualRow ? 2 : 1;
+            for (int i = 0; i < row_tiles; ++i) {
+                const int s = n_q & 1;
+                if (n_q >= 2) ok = warp_wait(&q_empty[s], (n_q / 2 - 1) & 1, wc);
+                if (!ok) break;
+                const int row0 = own ? g.b * a.R : (2 * g.pair + i) * a.rows_tile;
+                if (elect_one()) {
+                    mbar_arrive_expect_tx(&q_full[s], (uint32_t)a.rows_tile * a.G * D * 2);
+#pragma unroll
+                    for (int h = 0; h < NH; ++h)
+                        tma_load_4d(smem + OFF_Q + s * TILE + h * kHalfBytes, &tmQ, &q_full[s], h * 64, g.kvh * a.G,
+                                    row0, 0);
+                }
+                __syncwarp();
+                ++n_q;
+            }
+            for (int t = 0; t < g.tiles && ok; ++t) {
                 const int key0 = (g.tile0 + t) * kKeys;
                 int c1[2] = {key0, 0}, c3[2] = {g.b, g.b};
                 if (a.block_table) {
                     for (int q = 0; q < parts; ++q) {
                         const int in_unit = key0 + q * a.box_rows;
-                        const int pos = in_unit + (g.own ? plan.P : 0);
+                        const int pos = in_unit + (own ? plan.P : 0);
                         c1[q] = pos & (a.block_size - 1);
                         if (in_unit >= g.keys) {
                             c3[q] = a.num_blocks;  // past the keys: zeros, no table entry is read
@@ -469,7 +470,7 @@ prefix_attn_split_kernel(const __grid_constant__ CUtensorMap tmKp, const __grid_
 #pragma unroll
                         for (int h = 0; h < NH; ++h)
                             tma_load_4d(smem + OFF_K + ks * TILE + h * kHalfBytes + q * part_bytes, mk, &k_full[ks],
-                                        h * 64, c1[q], kvh, c3[q]);
+                                        h * 64, c1[q], g.kvh, c3[q]);
                 }
                 __syncwarp();
                 ++n_k;
@@ -481,242 +482,232 @@ prefix_attn_split_kernel(const __grid_constant__ CUtensorMap tmKp, const __grid_
 #pragma unroll
                         for (int h = 0; h < NH; ++h)
                             tma_load_4d(smem + OFF_V + vs * TILE + h * kHalfBytes + q * part_bytes, mv, &v_full[vs],
-                                        h * 64, c1[q], kvh, c3[q]);
+                                        h * 64, c1[q], g.kvh, c3[q]);
                 }
                 __syncwarp();
                 ++n_v;
             }
+            if (lane == 0) mbar_arrive(&ring.empty[r & (kRing - 1)]);
+            __syncwarp();
+            ++r;
         }
         // every copy lands before the CTA gives up its shared memory, whoever may have given up waiting for it
+        for (int s = 0; s < 2 && s < n_q; ++s) mbar_wait_drain(&q_full[s], ((n_q - 1 - s) / 2) & 1);
         for (int s = 0; s < NK && s < n_k; ++s) mbar_wait_drain(&k_full[s], ((n_k - 1 - s) / NK) & 1);
         for (int s = 0; s < NV && s < n_v; ++s) mbar_wait_drain(&v_full[s], ((n_v - 1 - s) / NV) & 1);
     } else if (warp == 9) {
-        // ---------------- Q producer: a ring of two row tiles ----------------
-        int n = 0;
-        bool ok = true;
-        while (ok && walk_next(a, plan, &own_ready, wc, w, g)) {
-            const int cnt = g.dual_row ? 2 : 1;
-            for (int i = 0; i < cnt; ++i) {
-                const int s = n & 1;
-                if (n >= 2) ok = warp_wait(&q_empty[s], (n / 2 - 1) & 1, wc);
-                if (!ok) break;
-                const int row0 = g.own ? g.b * a.R : (2 * g.pair + i) * a.rows_tile;
-                if (elect_one()) {
-                    mbar_arrive_expect_tx(&q_full[s], (uint32_t)a.rows_tile * a.G * D * 2);
-#pragma unroll
-                    for (int h = 0; h < NH; ++h)
-                        tma_load_4d(smem + OFF_Q + s * TILE + h * kHalfBytes, &tmQ, &q_full[s], h * 64, g.kvh * a.G,
-                                    row0, 0);
-                }
-                __syncwarp();
-                ++n;
-            }
-        }
-        for (int s = 0; s < 2 && s < n; ++s) mbar_wait_drain(&q_full[s], ((n - 1 - s) / 2) & 1);
-    } else if (warp == 10) {
-        // ---------------- MMA issuer ----------------
-        // One thread issues both products, because the tensor core works off its instructions in order: QK^T
-        // of a stream's next tile goes out behind the PV of its last one and overwrites the P that PV reads,
-        // with no wait in between; and scores in hand mean that PV has completed.
-        // The products are numbered over the CTA's whole walk: product k belongs to stream k & 1 (a dual-row tile
-        // is two of them, and dual-row segments come first).  QK^T runs up to two products ahead of PV.
-        // The control flow of the warp never depends on a wait; once one has run out nothing is issued any more.
-        constexpr uint32_t idesc_qk = umma_idesc_bf16(128, kKeys, 0, 0);
-        constexpr uint32_t idesc_pv = umma_idesc_bf16(128, D, 0, 1);
-        const uint32_t tm0 = uniform(tmem);
-        const uint64_t q_desc = umma_smem_desc(smem_base + OFF_Q, 16, 1024);
-        const uint64_t k_desc = umma_smem_desc(smem_base + OFF_K, 16, 1024);
-        const uint64_t v_desc = umma_smem_desc(smem_base + OFF_V, kHalfBytes, 1024);
-        Walk wq = w;
-        Segment gq;
-        int rows_q = 0, tiles_q = 0, tq = 0, iq = 0, kq = 0, ks = 0, k_par = 0, n_q = 0;  // QK^T side: segment, place in it, K slot
-        int rows = 0, tiles = 0, t = 0, i = 0, k = 0, vs = 0, v_par = 0;                  // PV side, V slot
-        bool ended = false, alive = true;
-        while (true) {
-            while (kq < k + 2 && !ended) {
-                if (tq == tiles_q) {
-                    // (the own part may not be worked out yet: wait for it only when nothing else is left to do)
-                    if (walk_at_own(a, wq) && k < kq && !__all_sync(0xffffffffu, mbar_try_wait(&own_ready, 0))) break;
-                    ended = !walk_next(a, plan, &own_ready, wc, wq, gq);
-                    if (ended) break;
-                    n_q += rows_q;
-                    rows_q = uniform(gq.dual_row ? 2 : 1);
-                    tiles_q = uniform(gq.tiles);
-                    tq = 0;
-                }
-                const int s = kq & 1, qs = (n_q + iq) & 1;
-                const bool first = tq == 0, last = tq + 1 == tiles_q, tile_done = iq + 1 == rows_q;
-                if (elect_one()) {
-                    if (alive && first) alive = mbar_wait_bounded(&q_full[qs], ((n_q + iq) >> 1) & 1, wc);
-                    if (alive && iq == 0) alive = mbar_wait_bounded(&k_full[ks], k_par, wc);
-                    if (alive) {
+        // ---------------- the walk ----------------
+        walk(a, plan, ring, cta, plan, wc);
+    } else if (warp >= 10) {
+        // ---------------- MMA issuers: a thread for each stream ----------------
+        // It issues both products of its stream, because the tensor core works off a thread's instructions in
+        // order: the QK^T that refills one half of S goes out behind the PV that reads P from it, with no wait
+        // in between.  It runs up to two blocks ahead of PV.
+        if (elect_one()) {
+            constexpr uint32_t idesc_qk = umma_idesc_bf16(128, kBlock, 0, 0);
+            constexpr uint32_t idesc_pv = umma_idesc_bf16(128, D, 0, 1);
+            constexpr uint32_t BLOCK16 = kBlock * 128 >> 4;  // from a tile's first block of keys to its second, in descriptor units
+            const int st = warp - 10;
+            const uint32_t tS = tmem + COL_S + 128u * st, tO = tmem + COL_O + 128u * st;
+            const uint64_t q_desc = umma_smem_desc(smem_base + OFF_Q, 16, 1024);
+            const uint64_t k_desc = umma_smem_desc(smem_base + OFF_K, 16, 1024);
+            const uint64_t v_desc = umma_smem_desc(smem_base + OFF_V, kHalfBytes, 1024);
+            // QK^T side: segments begun, tiles left of the last and whether it is dual-row, block of the tile, block number, K slot
+            int rq = 0, left_q = 0, dual_q = 0, h_q = 0, j_q = 0, ks = 0, k_par = 0;
+            int n_q = 0, took_q = 0;  // Q tiles before the segment, and of it
+            // PV side
+            int left = 0, dual = 0, h = 0, j = 0, vs = 0, v_par = 0;
+            uint64_t qd = 0;
+            bool ended = false, fresh = true;
+            while (true) {
+                if (j_q < j + 2 && !ended) {
+                    // (the next segment may not be there yet: wait for it only when nothing else is left to do)
+                    if (left_q == 0 && (j == j_q || mbar_try_wait(&ring.full[rq & (kRing - 1)], (rq / kRing) & 1))) {
+                        if (!mbar_wait_bounded(&ring.full[rq & (kRing - 1)], (rq / kRing) & 1, wc)) break;
+                        left_q = RAPID_SEG(rq).tiles;
+                        ended = left_q == 0;
+                        if (!ended) {
+                            dual_q = RAPID_SEG(rq).flags & kDualRow ? 1 : 0;
+                            ++rq;
+                            n_q += took_q;
+                            took_q = 1 + dual_q;
+                            const int n = n_q + (dual_q & st);
+                            if (!mbar_wait_bounded(&q_full[n & 1], (n >> 1) & 1, wc)) break;
+                            qd = q_desc + (uint32_t)(n & 1) * (TILE >> 4);
+                        }
+                    }
+                    if (left_q > 0) {
+                        if (h_q == 0 && !mbar_wait_bounded(&k_full[ks], k_par, wc)) break;
                         tc_fence_after_sync();
-                        const uint64_t qd = q_desc + (uint64_t)(qs * (TILE >> 4)), kd = k_desc + (uint64_t)(ks * (TILE >> 4));
+                        const uint64_t kd = k_desc + (uint32_t)ks * (TILE >> 4) + (uint32_t)(dual_q ? h_q : st) * BLOCK16;
+                        const uint32_t d = tS + kBlock * (j_q & 1);
 #pragma unroll
                         for (int kk = 0; kk < D / 16; ++kk) {
                             const uint32_t off = (kk >> 2) * (kHalfBytes >> 4) + (kk & 3) * 2;
-                            umma_bf16_ss(tm0 + COL_S + 128u * s, qd + off, kd + off, idesc_qk, kk > 0);
+                            umma_bf16_ss(d, qd + off, kd + off, idesc_qk, kk > 0);
                         }
-                        umma_commit(&s_full[s]);
-                        if (tile_done) umma_commit(&k_empty[ks]);
-                        if (last) umma_commit(&q_empty[qs]);
+                        umma_commit(&s_full[st][j_q & 1]);
+                        ++j_q;
+                        if (h_q == dual_q) {
+                            umma_commit(&k_empty[ks]);
+                            h_q = 0;
+                            if (++ks == NK) ks = 0, k_par ^= 1;
+                            if (--left_q == 0) {
+                                umma_commit(&q_empty[(n_q + (dual_q & st)) & 1]);
+                                if (dual_q) {  // the other stream's row tile: given up for this stream too, once it is there
+                                    const int n = n_q + 1 - st;
+                                    if (!mbar_wait_bounded(&q_full[n & 1], (n >> 1) & 1, wc)) break;
+                                    mbar_arrive(&q_empty[n & 1]);
+                                }
+                            }
+                        } else {
+                            h_q = 1;
+                        }
+                        if (j_q < j + 2) continue;
                     }
                 }
-                __syncwarp();
-                ++kq;
-                iq = tile_done ? 0 : 1;
-                if (tile_done) {
-                    ++tq;
-                    if (++ks == NK) ks = 0, k_par ^= 1;
+                if (j == j_q) {
+                    if (ended) break;
+                    continue;
                 }
-            }
-            if (k == kq) break;
-            if (t == tiles) {
-                walk_next(a, plan, &own_ready, wc, w, g);  // (there is one: its QK^T went out)
-                rows = uniform(g.dual_row ? 2 : 1);
-                tiles = uniform(g.tiles);
-                t = 0;
-            }
-            const int s = k & 1;
-            const int turns = 3 - rows;              // tiles from one of a stream to its next
-            const bool fresh = t < turns;            // the stream's first tile of the segment
-            const bool last = t >= tiles - turns;    // ... and its last
-            const bool tile_done = i + 1 == rows;
-            if (elect_one()) {
-                if (alive && i == 0) alive = mbar_wait_bounded(&v_full[vs], v_par, wc);
-                if (alive) alive = mbar_wait_bounded(&p_full[s], (k >> 1) & 1, wc);
-                if (alive) {
-                    tc_fence_after_sync();
-                    const uint64_t vd = v_desc + (uint64_t)(vs * (TILE >> 4));
-                    const uint32_t d = tm0 + COL_O + 128u * s, pm = tm0 + COL_S + 128u * s;
+                if (left == 0) {  // (the segment is there: its first QK^T went out)
+                    left = RAPID_SEG(r).tiles;
+                    dual = RAPID_SEG(r).flags & kDualRow ? 1 : 0;
+                    fresh = true;
+                }
+                if (h == 0 && !mbar_wait_bounded(&v_full[vs], v_par, wc)) break;
+                if (!mbar_wait_bounded(&p_full[st][j & 1], (j >> 1) & 1, wc)) break;
+                tc_fence_after_sync();
+                const uint64_t vd = v_desc + (uint32_t)vs * (TILE >> 4) + (uint32_t)(dual ? h : st) * BLOCK16;
+                const uint32_t pm = tS + kBlock * (j & 1);
 #pragma unroll
-                    for (int kk = 0; kk < kKeys / 16; ++kk)
-                        umma_bf16_ts(d, pm + 8 * kk, vd + kk * (2048 >> 4), idesc_pv, (!fresh || kk > 0) ? 1u : 0u);
-                    if (tile_done) umma_commit(&v_empty[vs]);
-                    if (last) umma_commit(&pv_done[s]);
+                for (int kk = 0; kk < kBlock / 16; ++kk)
+                    umma_bf16_ts(tO, pm + 8 * kk, vd + kk * (2048 >> 4), idesc_pv, (!fresh || kk > 0) ? 1u : 0u);
+                fresh = false;
+                umma_commit(&o_rest[st][j & 1]);
+                ++j;
+                if (h == dual) {
+                    umma_commit(&v_empty[vs]);
+                    h = 0;
+                    if (++vs == NV) vs = 0, v_par ^= 1;
+                    if (--left == 0) mbar_arrive(&ring.empty[r++ & (kRing - 1)]);
+                } else {
+                    h = 1;
                 }
             }
-            __syncwarp();
-            ++k;
-            i = tile_done ? 0 : 1;
-            if (tile_done) {
-                ++t;
-                if (++vs == NV) vs = 0, v_par ^= 1;
-            }
-        }
-        // every MMA issued here has completed before tensor memory is freed
-        if (elect_one()) {
-            umma_commit(&drain_bar);
-            mbar_wait_drain(&drain_bar, 0);
+            // every MMA issued here has completed before tensor memory is freed
+            umma_commit(&drain_bar[st]);
+            const long long t0 = clock64();
+            while (!mbar_try_wait(&drain_bar[st], 0) && clock64() - t0 < kWaitCycleLimit) {}
         }
         __syncwarp();
-    } else if (warp == 11) {
-        // ---------------- planner of the own part ----------------
-        plan_own(a, cta, plan);
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&own_ready);
-    } else if (warp < 8) {
+    } else {
         // ---------------- softmax warps: stream = warp / 4, row of the tile = 32 (warp % 4) + lane ----------------
         const int stream = warp >> 2;
         const int row = (warp & 3) * 32 + lane;
         const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t tS = tmem + lane_base + COL_S + 128u * stream;
         const uint32_t tO = tmem + lane_base + COL_O + 128u * stream;
         const float c = a.scale_log2;
-        int n = 0, par = 0, cnt = 0, segs = 0;  // CTA-wide tile index, dual-key tiles met, tiles and segments of this stream
+        int n = 0, j = 0;  // tiles of the CTA before the segment, blocks of this stream so far
         bool ok = true;
-        while (ok && walk_next(a, plan, &own_ready, wc, w, g)) {
+        while (true) {
+            ok = warp_wait(&ring.full[r & (kRing - 1)], (r / kRing) & 1, wc);
+            const Segment g = RAPID_SEG(r);
+            if (!ok || g.tiles == 0) break;
+            const bool own = g.flags & kOwn;
+            const int dual = g.flags & kDualRow ? 1 : 0, blocks = g.tiles << dual;
             // the tile's rows: (sequence, row, head in group) of the batch, or (row, head) of one sequence
-            const int tile_row0 = (2 * g.pair + (g.dual_row ? stream : 0)) * a.rows_tile;
-            const int rows = g.own ? a.GR : min(a.rows_tile, a.B * a.R - tile_row0) * a.G;
+            const int tile_row0 = (2 * g.pair + (dual ? stream : 0)) * a.rows_tile;
+            const int rows = own ? a.GR : min(a.rows_tile, a.B * a.R - tile_row0) * a.G;
             const bool row_valid = row < rows;
             const bool warp_active = (warp & 3) * 32 < rows;
             // keys a row sees: all of the prefix; its own sequence's up to itself
-            const int lim = g.own ? g.keys - a.R + row / a.G : g.keys - 1;
-            const int all_see = g.own ? g.keys - a.R : g.keys - 1;
+            const int lim = own ? g.keys - a.R + row / a.G : g.keys - 1;
+            const int all_see = own ? g.keys - a.R : g.keys - 1;
             float m_ref = -INFINITY, l_run = 0.f;
-            bool first = true;
-            const int step = g.dual_row ? 1 : 2;
-            for (int t = g.dual_row ? 0 : (stream ^ par) & 1; t < g.tiles && ok; t += step) {
-                ok = warp_wait(&s_full[stream], cnt & 1, wc);
+            for (int u = 0; u < blocks; ++u, ++j) {
+                const int t = u >> dual, kb = dual ? u & 1 : stream;  // the block's tile, and which half of its keys
+                const uint32_t tS = tmem + lane_base + COL_S + 128u * stream + kBlock * (j & 1);
+                ok = warp_wait(&s_full[stream][j & 1], (j >> 1) & 1, wc);
                 if (!ok) break;
-                const int key0 = (g.tile0 + t) * kKeys;
+                const int key0 = (g.tile0 + t) * kKeys + kBlock * kb;
                 if (warp_active) {
                     tc_fence_after_sync();
-                    uint32_t sr[2][32];  // scores of 32 keys, and the next 32 on their way
-                    tmem_ld_x32(tS, sr[0]);
+                    uint32_t x[kBlock];
+                    tmem_ld_x32(tS, reinterpret_cast<uint32_t(&)[32]>(x[0]));
+                    tmem_ld_x32(tS + 32, reinterpret_cast<uint32_t(&)[32]>(x[32]));
+                    tmem_wait_ld();
+                    if (key0 + kBlock - 1 > all_see) {
 #pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-                        uint32_t(&x)[32] = sr[h & 1];
-                        tmem_wait_ld();
-                        if (h < 3) tmem_ld_x32(tS + 32 * (h + 1), sr[(h + 1) & 1]);
-                        if (key0 + 32 * h + 31 > all_see) {
-#pragma unroll
-                            for (int k = 0; k < 32; ++k)
-                                if (key0 + 32 * h + k > lim) x[k] = __float_as_uint(-INFINITY);
-                        }
-                        float mx[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-                        for (int k = 0; k < 32; k += 4) {
-                            mx[0] = max3(mx[0], __uint_as_float(x[k]), __uint_as_float(x[k + 1]));
-                            mx[1] = max3(mx[1], __uint_as_float(x[k + 2]), __uint_as_float(x[k + 3]));
-                        }
-                        const float top = ceilf(fmaxf(mx[0], mx[1]) * c);
-                        // no reference yet, or scores that outgrow it
-                        const bool move = row_valid && top > m_ref + kJump;
-                        if (__any_sync(0xffffffffu, move)) {
-                            tmem_wait_ld();  // (the next scores are in their registers before the call)
-                            move_reference<D>(move, top, m_ref, l_run, tO, !first, tS, h);
-                        }
-                        const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
-                        const uint64_t c2 = f32x2(c, c), m2 = f32x2(-m_use, -m_use);
-                        uint64_t acc[2] = {0, 0};
-                        uint32_t pk[16];
-#pragma unroll
-                        for (int k = 0; k < 32; k += 2) {
-                            float y0, y1;
-                            f32x2_split(f32x2_fma(f32x2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), c2, m2), y0, y1);
-                            const float p0 = fast_exp2(y0), p1 = fast_exp2(y1);
-                            acc[(k >> 1) & 1] = f32x2_add(acc[(k >> 1) & 1], f32x2(p0, p1));
-                            pk[k >> 1] = pack_bf16x2(p0, p1);
-                        }
-                        tmem_st_x16(tS + 16 * h, pk);
-                        float s0, s1;
-                        f32x2_split(f32x2_add(acc[0], acc[1]), s0, s1);
-                        l_run += s0 + s1;
+                        for (int k = 0; k < kBlock; ++k)
+                            if (key0 + k > lim) x[k] = __float_as_uint(-INFINITY);
                     }
-                    first = false;
+                    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int k = 0; k < kBlock; k += 2)
+                        mx[(k >> 1) & 3] = max3(mx[(k >> 1) & 3], __uint_as_float(x[k]), __uint_as_float(x[k + 1]));
+                    const float top = ceilf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c);
+                    // no reference yet, or scores that outgrow it
+                    const bool move = row_valid && top > m_ref + kJump;
+                    if (__any_sync(0xffffffffu, move)) {
+                        const float factor = move ? fast_exp2(m_ref - top) : 1.f;  // 0 when there was no reference
+                        if (move) {
+                            l_run *= factor;
+                            m_ref = top;
+                        }
+                        if (u > 0) {  // O at rest: the PV of the stream's latest block has completed
+                            ok = warp_wait(&o_rest[stream][(j - 1) & 1], ((j - 1) >> 1) & 1, wc);
+                            if (!ok) break;
+                            tc_fence_after_sync();
+                            scale_o<D>(tO, factor);
+                        }
+                    }
+                    const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
+                    const uint64_t c2 = f32x2(c, c), m2 = f32x2(-m_use, -m_use);
+                    uint64_t acc[2] = {0, 0};
+                    uint32_t pk[kBlock / 2];
+#pragma unroll
+                    for (int k = 0; k < kBlock; k += 2) {
+                        float y0, y1;
+                        f32x2_split(f32x2_fma(f32x2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), c2, m2), y0, y1);
+                        const float p0 = fast_exp2(y0), p1 = fast_exp2(y1);
+                        acc[(k >> 1) & 1] = f32x2_add(acc[(k >> 1) & 1], f32x2(p0, p1));
+                        pk[k >> 1] = pack_bf16x2(p0, p1);
+                    }
+                    tmem_st_x32(tS, pk);
+                    float s0, s1;
+                    f32x2_split(f32x2_add(acc[0], acc[1]), s0, s1);
+                    l_run += s0 + s1;
                 }
-                if (key0 + kKeys > g.keys) {
+                if (key0 + kBlock > g.keys) {
                     // V rows past the keys may hold any bits: zero them so that 0 * row = 0
                     const int vs = (n + t) % NV;
                     ok = warp_wait(&v_full[vs], ((n + t) / NV) & 1, wc);
                     if (!ok) break;
-                    const int first_bad = g.keys - key0;
-                    const int chunks = (kKeys - first_bad) * 8;
+                    const int bad = max(0, g.keys - key0);
+                    const int chunks = (kBlock - bad) * 8;
 #pragma unroll
                     for (int h = 0; h < NH; ++h)
                         for (int ch = row; ch < chunks; ch += 128)
-                            *reinterpret_cast<uint4*>(smem + OFF_V + vs * TILE + h * kHalfBytes + first_bad * 128 + ch * 16) =
+                            *reinterpret_cast<uint4*>(smem + OFF_V + vs * TILE + h * kHalfBytes + (kBlock * kb + bad) * 128 + ch * 16) =
                                 make_uint4(0, 0, 0, 0);
                     fence_proxy_async_smem();
                 }
                 tmem_wait_st();
                 tc_fence_before_sync();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&p_full[stream]);
-                ++cnt;
+                if (lane == 0) mbar_arrive(&p_full[stream][j & 1]);
             }
             if (!ok) break;
 
             // ---- end of the segment: the partial of this stream ----
             const int unit = g.b * a.Hkv + g.kvh;
-            const int slot_rows = g.own ? a.GR : 128;
-            float* slot = g.own ? a.part_own + (size_t)((plan.worker + unit) * 2 + stream) * slot_floats(a.GR, D)
+            const int slot_rows = own ? a.GR : 128;
+            float* slot = own ? a.part_own + (size_t)((plan.worker + unit) * 2 + stream) * slot_floats(a.GR, D)
                                 : a.part_prefix + (size_t)((plan.team + g.kvh) * 2 * a.np + 2 * g.pair + stream) * slot_floats(128, D);
-            if (!first) {
-                ok = warp_wait(&pv_done[stream], segs & 1, wc);
-                if (!ok) break;
+            ok = warp_wait(&o_rest[stream][(j - 1) & 1], ((j - 1) >> 1) & 1, wc);
+            if (!ok) break;
+            if (warp_active) {
                 tc_fence_after_sync();
 #pragma unroll
                 for (int i = 0; i < D / 32; ++i) {
@@ -731,25 +722,28 @@ prefix_attn_split_kernel(const __grid_constant__ CUtensorMap tmKp, const __grid_
                     }
                 }
                 tc_fence_before_sync();
-            }
-            if (row_valid) {
-                slot[(size_t)slot_rows * D + row] = m_ref;
-                slot[(size_t)slot_rows * (D + 1) + row] = l_run;
+                if (row_valid) {
+                    slot[(size_t)slot_rows * D + row] = m_ref;
+                    slot[(size_t)slot_rows * (D + 1) + row] = l_run;
+                }
             }
             // which workers hold tiles of a unit, for the merge
             if (threadIdx.x == 0) {
-                int2* range = g.own ? a.own_range + unit : a.prefix_range + g.kvh;
-                const int who = g.own ? plan.worker : plan.team;
-                if (g.own || g.pair == 0) {
+                int2* range = own ? a.own_range + unit : a.prefix_range + g.kvh;
+                const int who = own ? plan.worker : plan.team;
+                if (own || g.pair == 0) {
                     if (g.tile0 == 0) range->x = who;
                     if (g.tile0 + g.tiles == tiles_of(g.keys)) range->y = who;
                 }
             }
-            if (g.dual_row || g.tiles > ((stream ^ par) & 1)) ++segs;  // the stream had a tile of it
             n += g.tiles;
-            if (!g.dual_row) par += g.tiles;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&ring.empty[r & (kRing - 1)]);
+            ++r;
         }
     }
+
+#undef RAPID_SEG
 
     tc_fence_before_sync();
     __syncthreads();
