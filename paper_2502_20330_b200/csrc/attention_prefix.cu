@@ -49,6 +49,7 @@ constexpr int kThreads = 384;          // two softmax groups of 128; the produce
 constexpr int kBlock = 64;             // keys of a block: what a stream takes at a time
 constexpr int kHalfBytes = kKeys * 128;  // one 64-column half of a tile of 128 rows
 constexpr int kPad = 3;                // single-stream tiles that a change of unit costs
+constexpr int kPoly = 3;               // of 8 pairs of exponentials, those that the FMA pipe takes from the special-function unit
 constexpr int kMaxPrefixCtas = 256;
 constexpr float kJump = 40.f;          // a score this far (log2) above a row's reference moves it: probabilities stay below
                                        // 2^40, far from the end of fp32's and bf16's range in any sum
@@ -335,10 +336,31 @@ __device__ __forceinline__ uint64_t f32x2_add(uint64_t a, uint64_t b) {
     return r;
 }
 
+// The largest of three; NaN if any is (a NaN score has to reach the row's reference and so its output).
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float r;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
+}
+
+// 2^y0 and 2^y1, y at most 126, without the special-function unit: adding 1.5 * 2^23 leaves n, the whole number
+// next to y, in the low bits of the sum; f = y - n in [-1/2, 1/2] goes through the minimax polynomial of
+// degree 4 of 2^f (Remez exchange on the relative error, 2.7e-6 with fp32 coefficients), and n is added to the
+// exponent.  Below -125 the result is 2^-125.
+__device__ __forceinline__ void exp2_poly(float& y0, float& y1) {
+    constexpr float kMagic = 12582912.f;
+    const uint64_t y = f32x2(fmaxf(y0, -125.f), fmaxf(y1, -125.f));
+    const uint64_t t = f32x2_add(y, f32x2(kMagic, kMagic));
+    const uint64_t f = f32x2_fma(f32x2_add(t, f32x2(-kMagic, -kMagic)), f32x2(-1.f, -1.f), y);
+    uint64_t p = f32x2_fma(f, f32x2(0.009570102207362652f, 0.009570102207362652f), f32x2(0.05591785907745361f, 0.05591785907745361f));
+    p = f32x2_fma(p, f, f32x2(0.240247443318367f, 0.240247443318367f));
+    p = f32x2_fma(p, f, f32x2(0.6931217908859253f, 0.6931217908859253f));
+    p = f32x2_fma(p, f, f32x2(0.9999992847442627f, 0.9999992847442627f));
+    float t0, t1;
+    f32x2_split(t, t0, t1);
+    f32x2_split(p, y0, y1);
+    y0 = __int_as_float(__float_as_int(y0) + (__float_as_int(t0) << 23));
+    y1 = __int_as_float(__float_as_int(y1) + (__float_as_int(t1) << 23));
 }
 
 // Scales a row's O accumulators when its reference moves.  Rare: kept out of the way.
@@ -648,7 +670,7 @@ prefix_attn_split_kernel(const __grid_constant__ CUtensorMap tmKp, const __grid_
                         mx[(k >> 1) & 3] = max3(mx[(k >> 1) & 3], __uint_as_float(x[k]), __uint_as_float(x[k + 1]));
                     const float top = ceilf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c);
                     // no reference yet, or scores that outgrow it
-                    const bool move = row_valid && top > m_ref + kJump;
+                    const bool move = row_valid && !(top <= m_ref + kJump) && top != -INFINITY;
                     if (__any_sync(0xffffffffu, move)) {
                         const float factor = move ? fast_exp2(m_ref - top) : 1.f;  // 0 when there was no reference
                         if (move) {
@@ -668,9 +690,14 @@ prefix_attn_split_kernel(const __grid_constant__ CUtensorMap tmKp, const __grid_
                     uint32_t pk[kBlock / 2];
 #pragma unroll
                     for (int k = 0; k < kBlock; k += 2) {
-                        float y0, y1;
-                        f32x2_split(f32x2_fma(f32x2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), c2, m2), y0, y1);
-                        const float p0 = fast_exp2(y0), p1 = fast_exp2(y1);
+                        float p0, p1;
+                        f32x2_split(f32x2_fma(f32x2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), c2, m2), p0, p1);
+                        if ((k >> 1) % 8 < kPoly) {
+                            exp2_poly(p0, p1);
+                        } else {
+                            p0 = fast_exp2(p0);
+                            p1 = fast_exp2(p1);
+                        }
                         acc[(k >> 1) & 1] = f32x2_add(acc[(k >> 1) & 1], f32x2(p0, p1));
                         pk[k >> 1] = pack_bf16x2(p0, p1);
                     }
