@@ -64,6 +64,7 @@ extern "C" {
 #define RAPID_STATUS_BAD_BLOCK_TABLE 16  /* a block-table entry outside [0, num_blocks): read as 0s  */
 #define RAPID_STATUS_STALE_PLAN 32       /* the plan in the workspace was made for other lengths or another
                                             geometry than this call's: outputs invalid               */
+#define RAPID_STATUS_FP8_SATURATED 64    /* a value beyond what its scale can hold was written as +-448 * scale */
 
 /* residual_mode */
 #define RAPID_RESIDUAL_PAPER 0 /* norm(max(p - phat, p - q, 0)): Algorithm 1, residual step               */
@@ -587,6 +588,79 @@ int rapid_kv_append(const void* k_new, const void* v_new, void* k_cache, void* v
 int rapid_kv_append_paged(const void* k_new, const void* v_new, void* k_pool, void* v_pool,
                           const int32_t* block_table, const rapid_paged_kv* paged, int32_t* ctx_lens,
                           int gamma, int B, int Hkv, int D, int32_t* status_word, void* cuda_stream);
+
+/*
+ * Where the rows lie that the two calls below quantise: bf16, D contiguous, element strides between sequences / tokens /
+ * KV heads (0 = dense [B, T, Hkv, D]); multiples of 8.
+ */
+typedef struct rapid_kv_rows {
+    int64_t stride_b;
+    int64_t stride_t;
+    int64_t stride_h;
+} rapid_kv_rows;
+
+/*
+ * Writes a prompt's K/V rows into an FP8 E4M3 cache (the one rapid_verify_attention_fp8 reads) and chooses its scales.
+ * (Not in the paper, which fixes no storage precision; see rapid_verify_attention_fp8.)  For every sequence b and
+ * KV head, over the rows 0 .. n_tokens[b] - 1:
+ *   scale = 2^headroom * (the smallest power of two with max |x| <= 448 * scale);  1 where there is nothing but zeros
+ *   code  = E4M3(x / scale), to nearest, ties to even
+ * into positions 0 .. n_tokens[b] - 1; the cache behind them is left as it was.  `headroom` (0 .. 8) leaves that many
+ * powers of two for later, larger rows (rapid_kv_append_fp8 keeps the scale).  A power of two makes
+ * rapid_kv_read_fp8 exact for these codes.  NaN is stored as NaN and takes no part in the maximum; an
+ * infinity counts as the largest finite value there, is stored as +-448 and sets RAPID_STATUS_FP8_SATURATED.
+ *   k_new, v_new : device bf16, T rows per sequence, geometry of `rows` (NULL = dense [B, T, Hkv, D])
+ *   n_tokens     : device int32 [B], or NULL = T each.  A sequence with a count outside [0, min(T, Lmax)] is left
+ *                  untouched (cache, scales and length) and sets RAPID_STATUS_BAD_CTX_LEN
+ *   k_cache, v_cache, shape : as in rapid_verify_attention_fp8 (strides in elements, multiples of 16; D % 16 == 0)
+ *   k_scale, v_scale : device fp32 [B, Hkv], written
+ *   ctx_lens_out : device int32 [B], receives n_tokens[b]; or NULL
+ *   workspace    : device, >= rapid_kv_fill_workspace_bytes(), initialised; the status word is its first
+ */
+size_t rapid_kv_fill_workspace_bytes(int B, int Hkv);
+int rapid_kv_fill_fp8(const void* k_new, const void* v_new, const rapid_kv_rows* rows, int T,
+                      const int32_t* n_tokens, void* k_cache, void* v_cache, float* k_scale, float* v_scale,
+                      int32_t* ctx_lens_out, int headroom, const rapid_attn_shape* shape, void* workspace,
+                      size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * rapid_kv_append for an FP8 E4M3 cache: quantises the R = gamma+1 newest rows with the scales in place,
+ *   code = E4M3(x / scale), to nearest, ties to even;  beyond +-448 the code is +-448 and
+ *   RAPID_STATUS_FP8_SATURATED is set (NaN is stored as NaN),
+ * into positions ctx_lens[b] .. ctx_lens[b] + gamma.  (Also for the later parts of a prompt that arrives in pieces: R may
+ * be large.)  Unlike rapid_kv_append it need not count the rows: the layers of a step share one length vector.
+ *   k_new, v_new : device bf16, R rows per sequence, geometry of `rows` (NULL = dense [B, R, Hkv, D])
+ *   k_scale, v_scale : device fp32 [B, Hkv], positive and finite
+ *   ctx_lens     : device int32 [B], tokens in the cache before the call
+ *   ctx_lens_out : device int32 [B], receives ctx_lens[b] + R; may be ctx_lens itself (one more kernel); or NULL
+ * A sequence whose cache cannot take R more rows (or with a negative length) is left untouched, its length
+ * is passed on as it is, and RAPID_STATUS_BAD_CTX_LEN is set in *status_word.
+ */
+int rapid_kv_append_fp8(const void* k_new, const void* v_new, const rapid_kv_rows* rows, void* k_cache,
+                        void* v_cache, const float* k_scale, const float* v_scale, const int32_t* ctx_lens,
+                        int32_t* ctx_lens_out, int gamma, const rapid_attn_shape* shape, int32_t* status_word,
+                        void* cuda_stream);
+
+/*
+ * Reads chunks of an FP8 E4M3 cache back into a bf16 cache, one behind the other: the chunks that
+ * rapid_retrieval_select chose become the cache that the drafter (or, as the shared prefix of
+ * rapid_verify_attention_prefix, a batch of them) attends over (Section 2.3: the drafter runs on the retrieved
+ * context); or a whole cache goes back to bf16.
+ *   out = bf16(scale * decode(code)), the product in fp32 (exact for the scales of rapid_kv_fill_fp8)
+ *   ctx_lens  : device int32 [B], tokens in the cache; out of [0, Lmax]: clamped, sets RAPID_STATUS_BAD_CTX_LEN
+ *   chunk_idx : device int32 [B, n_chunks]: chunk i holds positions [i * chunk_tokens, (i+1) * chunk_tokens), as far
+ *               as ctx_lens[b] reaches; -1 is no chunk; any other that holds nothing sets RAPID_STATUS_BAD_CTX_LEN.
+ *               The same chunk may be named twice.  NULL: chunks 0 .. n_chunks - 1
+ *   k_out, v_out, out_shape : device bf16 cache, geometry as in rapid_verify_attention; what would go beyond its
+ *               Lmax is left out and sets RAPID_STATUS_BAD_CTX_LEN; rows behind the last written are left as they were
+ *   out_lens  : device int32 [B], rows written per KV head
+ * k_scale, v_scale fp32 [B, Hkv]; D % 16 == 0.  The output must not overlap the cache.
+ */
+int rapid_kv_read_fp8(const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
+                      const int32_t* ctx_lens, const rapid_attn_shape* shape, const int32_t* chunk_idx,
+                      int n_chunks, int chunk_tokens, void* k_out, void* v_out,
+                      const rapid_attn_shape* out_shape, int32_t* out_lens, int32_t* status_word,
+                      void* cuda_stream);
 
 /*
  * Closes a verify step (Algorithm 1: accepted drafts become x_j, the rest is discarded): of the R

@@ -17,6 +17,7 @@ STATUS_RESIDUAL_FALLBACK = 4
 STATUS_PIPELINE_TIMEOUT = 8
 STATUS_BAD_BLOCK_TABLE = 16
 STATUS_STALE_PLAN = 32
+STATUS_FP8_SATURATED = 64
 ATTN_KERNEL_AUTO, ATTN_KERNEL_ROWS_ON_M, ATTN_KERNEL_KEYS_ON_M, ATTN_KERNEL_CLUSTER_MERGE = 0, 1, 2, 3
 PLAN_NONE, PLAN_READY, PLAN_SETTLED = 0, 1, 2
 RESIDUAL_PAPER = 0
@@ -30,6 +31,7 @@ EXPORTS = [
     "rapid_last_error",
     "rapid_version", "rapid_kernel_launch_count", "rapid_kernel_launch_count_reset",
     "rapid_prefix_attention_workspace_bytes", "rapid_verify_attention_prefix", "rapid_verify_attention_prefix_paged",
+    "rapid_kv_fill_workspace_bytes", "rapid_kv_fill_fp8", "rapid_kv_append_fp8", "rapid_kv_read_fp8",
 ]
 
 
@@ -53,6 +55,10 @@ class _PagedKv(ctypes.Structure):
 
 class _PrefixKv(ctypes.Structure):
     _fields_ = [("Pmax", ctypes.c_int64), ("stride_h", ctypes.c_int64), ("stride_l", ctypes.c_int64)]
+
+
+class _KvRows(ctypes.Structure):
+    _fields_ = [("stride_b", ctypes.c_int64), ("stride_t", ctypes.c_int64), ("stride_h", ctypes.c_int64)]
 
 
 class _AttnParams(ctypes.Structure):
@@ -182,6 +188,15 @@ def load_library():
         lib.rapid_kv_append.argtypes = [vp, vp, vp, vp, vp, i32, ctypes.POINTER(_AttnShape), vp, vp]
         lib.rapid_kv_append_paged.restype = i32
         lib.rapid_kv_append_paged.argtypes = [vp, vp, vp, vp, vp, ctypes.POINTER(_PagedKv), vp, i32, i32, i32, i32, vp, vp]
+        shape_p, rows_p = ctypes.POINTER(_AttnShape), ctypes.POINTER(_KvRows)
+        lib.rapid_kv_fill_workspace_bytes.restype = sz
+        lib.rapid_kv_fill_workspace_bytes.argtypes = [i32, i32]
+        lib.rapid_kv_fill_fp8.restype = i32
+        lib.rapid_kv_fill_fp8.argtypes = [vp, vp, rows_p, i32, vp, vp, vp, vp, vp, vp, i32, shape_p, vp, sz, vp]
+        lib.rapid_kv_append_fp8.restype = i32
+        lib.rapid_kv_append_fp8.argtypes = [vp, vp, rows_p, vp, vp, vp, vp, vp, vp, i32, shape_p, vp, vp]
+        lib.rapid_kv_read_fp8.restype = i32
+        lib.rapid_kv_read_fp8.argtypes = [vp, vp, vp, vp, vp, shape_p, vp, i32, i32, vp, vp, shape_p, vp, vp, vp]
         lib.rapid_step_commit.restype = i32
         lib.rapid_step_commit.argtypes = [vp, vp, i32, i32, vp, vp]
         lib.rapid_last_error.restype = ctypes.c_char_p
@@ -414,6 +429,14 @@ def _check_prefix_call(q, out, kv, ctx_lens, prefix_len, gamma, params):
     _check_device(q, out, *kv, ctx_lens, prefix_len)
 
 
+def _strides(t, n):
+    """Element strides of the first n axes for the library, which reads 0 as "dense": an axis of one entry has none to
+    tell, and a broadcast axis cannot be told."""
+    if any(t.stride(i) == 0 and t.shape[i] > 1 for i in range(n)):
+        raise ValueError("a broadcast axis (stride 0) is not supported")
+    return [t.stride(i) if t.shape[i] > 1 else 0 for i in range(n)]
+
+
 def _check_device(*tensors):
     """The library launches on the current device: every tensor has to live there."""
     here = torch.cuda.current_device() if torch.cuda.is_available() else None
@@ -434,8 +457,11 @@ def rapid_verify_attention_prefix(q, k_prefix, v_prefix, prefix_len, k_cache, v_
         raise ValueError("k_prefix and v_prefix must share shape [Hkv, Pmax, D] and strides")
     if k_prefix.stride(2) != 1 or k_prefix.shape[0] != k_cache.shape[1] or k_prefix.shape[2] != q.shape[3]:
         raise ValueError("the prefix must have the cache's KV heads and a contiguous head_dim")
-    shape = _attn_shape(q, k_cache)
-    prefix = _PrefixKv(k_prefix.shape[1], k_prefix.stride(0), k_prefix.stride(1))
+    B, _, Hq, D = q.shape
+    if k_cache.shape[0] != B or k_cache.shape[3] != D or k_cache.stride(3) != 1:
+        raise ValueError("k_cache and v_cache must be [B, Hkv, Lmax, D] of q's batch and a contiguous head_dim")
+    shape = _AttnShape(B, Hq, k_cache.shape[1], D, k_cache.shape[2], *_strides(k_cache, 3))
+    prefix = _PrefixKv(k_prefix.shape[1], *_strides(k_prefix, 2))
     _check(load_library().rapid_verify_attention_prefix(
         _p(q), _p(k_prefix), _p(v_prefix), ctypes.byref(prefix), _p(prefix_len), _p(k_cache), _p(v_cache), _p(ctx_lens),
         gamma, _p(out), ctypes.byref(shape), _attn_params(params), _p(workspace), _nbytes(workspace),
@@ -460,7 +486,7 @@ def rapid_verify_attention_prefix_paged(q, k_pool, v_pool, block_table, prefix_l
         raise ValueError("q and k_pool disagree on head_dim")
     mb = block_table.shape[1]
     shape = _AttnShape(B, Hq, Hkv, D, mb * bs, 0, 0, 0)
-    paged = _PagedKv(bs, nb, mb, 0, k_pool.stride(0), k_pool.stride(1), k_pool.stride(2))
+    paged = _PagedKv(bs, nb, mb, 0, *_strides(k_pool, 3))
     _check(load_library().rapid_verify_attention_prefix_paged(
         _p(q), _p(k_pool), _p(v_pool), _p(block_table), ctypes.byref(paged), _p(prefix_len), _p(ctx_lens), gamma,
         _p(out), ctypes.byref(shape), _attn_params(params), _p(workspace), _nbytes(workspace), _stream_ptr(stream)))
@@ -609,6 +635,101 @@ def rapid_kv_append_paged(k_new, v_new, k_pool, v_pool, block_table, ctx_lens, g
     _check(load_library().rapid_kv_append_paged(_p(k_new), _p(v_new), _p(k_pool), _p(v_pool), _p(block_table),
                                                 ctypes.byref(paged), _p(ctx_lens), gamma, B, Hkv, D,
                                                 _p(status_word), _stream_ptr(stream)))
+
+
+def kv_fill_workspace_bytes(B, Hkv) -> int:
+    """Scratch of rapid_kv_fill_fp8."""
+    return int(load_library().rapid_kv_fill_workspace_bytes(int(B), int(Hkv)))
+
+
+def _fp8_cache_shape(k_cache, v_cache, k_scale, v_scale) -> _AttnShape:
+    if k_cache.element_size() != 1 or v_cache.element_size() != 1:
+        raise TypeError("k_cache / v_cache must hold one-byte E4M3 codes")
+    if k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32:
+        raise TypeError("k_scale / v_scale must be float32")
+    if k_cache.dim() != 4 or k_cache.stride() != v_cache.stride() or k_cache.shape != v_cache.shape or k_cache.stride(3) != 1:
+        raise ValueError("k_cache and v_cache must share shape [B, Hkv, Lmax, D] and strides with a contiguous head_dim")
+    B, Hkv, Lmax, D = k_cache.shape
+    if k_scale.shape != (B, Hkv) or v_scale.shape != (B, Hkv) or not (k_scale.is_contiguous() and v_scale.is_contiguous()):
+        raise ValueError("k_scale / v_scale must be dense [B, Hkv]")
+    return _AttnShape(B, Hkv, Hkv, D, Lmax, *_strides(k_cache, 3))
+
+
+def _new_rows(k_new, v_new, k_cache) -> _KvRows:
+    if k_new.dtype != torch.bfloat16 or v_new.dtype != torch.bfloat16:
+        raise TypeError("k_new / v_new must be bfloat16")
+    if k_new.dim() != 4 or k_new.shape != v_new.shape or k_new.stride() != v_new.stride() or k_new.stride(3) != 1:
+        raise ValueError("k_new and v_new must share shape [B, T, Hkv, D] and strides with a contiguous head_dim")
+    B, _, Hkv, D = k_new.shape
+    if (B, Hkv, D) != (k_cache.shape[0], k_cache.shape[1], k_cache.shape[3]):
+        raise ValueError("the new rows and the cache disagree on batch, KV heads or head_dim")
+    return _KvRows(*_strides(k_new, 3))
+
+
+def _lens(t, B, name):
+    if t is not None and (t.dtype != torch.int32 or t.numel() != B or not t.is_contiguous()):
+        raise TypeError(f"{name} must be dense int32 [B]")
+
+
+def rapid_kv_fill_fp8(k_new, v_new, n_tokens, k_cache, v_cache, k_scale, v_scale, ctx_lens_out, workspace,
+                      headroom: int = 0, stream=None) -> None:
+    """Quantises a prompt's rows k_new / v_new [B, T, Hkv, D] (bf16, may be strided; n_tokens [B] of them count, or all
+    for None) into the E4M3 cache k_cache / v_cache [B, Hkv, Lmax, D] and writes its power-of-two scales [B, Hkv]."""
+    shape = _fp8_cache_shape(k_cache, v_cache, k_scale, v_scale)
+    rows = _new_rows(k_new, v_new, k_cache)
+    _lens(n_tokens, shape.B, "n_tokens")
+    _lens(ctx_lens_out, shape.B, "ctx_lens_out")
+    _check_device(k_new, v_new, n_tokens, k_cache, v_cache, k_scale, v_scale, ctx_lens_out)
+    _check(load_library().rapid_kv_fill_fp8(_p(k_new), _p(v_new), ctypes.byref(rows), k_new.shape[1], _p(n_tokens),
+                                            _p(k_cache), _p(v_cache), _p(k_scale), _p(v_scale), _p(ctx_lens_out),
+                                            int(headroom), ctypes.byref(shape), _p(workspace), _nbytes(workspace),
+                                            _stream_ptr(stream)))
+
+
+def rapid_kv_append_fp8(k_new, v_new, k_cache, v_cache, k_scale, v_scale, ctx_lens, ctx_lens_out, gamma, status_word,
+                        stream=None) -> None:
+    """Quantises a step's rows k_new / v_new [B, gamma+1, Hkv, D] (bf16) into the E4M3 cache at ctx_lens with the
+    scales in place; ctx_lens_out (None, another tensor, or ctx_lens itself) receives ctx_lens + gamma + 1."""
+    shape = _fp8_cache_shape(k_cache, v_cache, k_scale, v_scale)
+    rows = _new_rows(k_new, v_new, k_cache)
+    if k_new.shape[1] != gamma + 1:
+        raise ValueError("k_new and v_new must be [B, gamma+1, Hkv, D]")
+    _lens(ctx_lens, shape.B, "ctx_lens")
+    _lens(ctx_lens_out, shape.B, "ctx_lens_out")
+    _check_device(k_new, v_new, k_cache, v_cache, k_scale, v_scale, ctx_lens, ctx_lens_out, status_word)
+    _check(load_library().rapid_kv_append_fp8(_p(k_new), _p(v_new), ctypes.byref(rows), _p(k_cache), _p(v_cache),
+                                              _p(k_scale), _p(v_scale), _p(ctx_lens), _p(ctx_lens_out), int(gamma),
+                                              ctypes.byref(shape), _p(status_word), _stream_ptr(stream)))
+
+
+def rapid_kv_read_fp8(k_cache, v_cache, k_scale, v_scale, ctx_lens, chunk_idx, chunk_tokens, k_out, v_out, out_lens,
+                      status_word, stream=None) -> None:
+    """Chunks of an E4M3 cache, one behind the other, into the bf16 cache k_out / v_out [B, Hkv, Lout, D].  chunk_idx
+    [B, n] names them (-1: none), as rapid_retrieval_select returns them; None: all chunks the output has room for."""
+    shape = _fp8_cache_shape(k_cache, v_cache, k_scale, v_scale)
+    if k_out.dtype != torch.bfloat16 or v_out.dtype != torch.bfloat16:
+        raise TypeError("k_out / v_out must be bfloat16")
+    if k_out.dim() != 4 or k_out.shape != v_out.shape or k_out.stride() != v_out.stride() or k_out.stride(3) != 1 \
+            or (k_out.shape[0], k_out.shape[1], k_out.shape[3]) != (shape.B, shape.Hkv, shape.D):
+        raise ValueError("k_out and v_out must be [B, Hkv, Lout, D] with equal strides and a contiguous head_dim")
+    _lens(ctx_lens, shape.B, "ctx_lens")
+    _lens(out_lens, shape.B, "out_lens")
+    if chunk_tokens <= 0:
+        raise ValueError("chunk_tokens must be positive")
+    if chunk_idx is None:
+        n = -(-min(k_out.shape[2], shape.Lmax) // chunk_tokens)
+    else:
+        if chunk_idx.dtype != torch.int32:
+            raise TypeError("chunk_idx must be int32")
+        if chunk_idx.dim() != 2 or chunk_idx.shape[0] != shape.B or not chunk_idx.is_contiguous():
+            raise ValueError("chunk_idx must be dense [B, n_chunks]")
+        n = chunk_idx.shape[1]
+    out = _AttnShape(shape.B, shape.Hkv, shape.Hkv, shape.D, k_out.shape[2], *_strides(k_out, 3))
+    _check_device(k_cache, v_cache, k_scale, v_scale, ctx_lens, chunk_idx, k_out, v_out, out_lens, status_word)
+    _check(load_library().rapid_kv_read_fp8(_p(k_cache), _p(v_cache), _p(k_scale), _p(v_scale), _p(ctx_lens),
+                                            ctypes.byref(shape), _p(chunk_idx), n, int(chunk_tokens), _p(k_out),
+                                            _p(v_out), ctypes.byref(out), _p(out_lens), _p(status_word),
+                                            _stream_ptr(stream)))
 
 
 def rapid_step_commit(ctx_lens, accept_len, gamma, status_word, stream=None) -> None:

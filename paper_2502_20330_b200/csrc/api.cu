@@ -180,6 +180,36 @@ int rapid_kv_append_paged(const void* k_new, const void* v_new, void* k_pool, vo
     return RAPID_OK;
 }
 
+size_t rapid_kv_fill_workspace_bytes(int B, int Hkv) { return kv_fill_workspace_bytes(B, Hkv); }
+
+int rapid_kv_fill_fp8(const void* k_new, const void* v_new, const rapid_kv_rows* rows, int T,
+                      const int32_t* n_tokens, void* k_cache, void* v_cache, float* k_scale, float* v_scale,
+                      int32_t* ctx_lens_out, int headroom, const rapid_attn_shape* shape, void* workspace,
+                      size_t workspace_bytes, void* cuda_stream) {
+    clear_error();
+    return launch_kv_fill_fp8(k_new, v_new, rows, T, n_tokens, k_cache, v_cache, k_scale, v_scale, ctx_lens_out, headroom,
+                              shape, workspace, workspace_bytes, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int rapid_kv_append_fp8(const void* k_new, const void* v_new, const rapid_kv_rows* rows, void* k_cache,
+                        void* v_cache, const float* k_scale, const float* v_scale, const int32_t* ctx_lens,
+                        int32_t* ctx_lens_out, int gamma, const rapid_attn_shape* shape, int32_t* status_word,
+                        void* cuda_stream) {
+    clear_error();
+    return launch_kv_append_fp8(k_new, v_new, rows, k_cache, v_cache, k_scale, v_scale, ctx_lens, ctx_lens_out, gamma, shape,
+                                status_word, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int rapid_kv_read_fp8(const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
+                      const int32_t* ctx_lens, const rapid_attn_shape* shape, const int32_t* chunk_idx,
+                      int n_chunks, int chunk_tokens, void* k_out, void* v_out,
+                      const rapid_attn_shape* out_shape, int32_t* out_lens, int32_t* status_word,
+                      void* cuda_stream) {
+    clear_error();
+    return launch_kv_read_fp8(k_cache, v_cache, k_scale, v_scale, ctx_lens, shape, chunk_idx, n_chunks, chunk_tokens, k_out,
+                              v_out, out_shape, out_lens, status_word, static_cast<cudaStream_t>(cuda_stream));
+}
+
 int rapid_step_commit(int32_t* ctx_lens, const int32_t* accept_len, int gamma, int B,
                       int32_t* status_word, void* cuda_stream) {
     clear_error();

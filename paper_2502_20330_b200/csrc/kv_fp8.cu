@@ -1,0 +1,641 @@
+// The FP8 KV cache around the verify step: quantising rows as they are written (a prompt's, a step's) and reading
+// chunks of it back in bf16.  The cache is the one rapid_verify_attention_fp8 reads: E4M3 codes
+// [B, Hkv, Lmax, D] and one fp32 scale per (sequence, KV head) for K and one for V; x = scale * decode(code).
+//
+//   fill     scale = 2^headroom * the smallest power of two with amax <= 448 * scale, over the prompt's rows of the
+//            (sequence, KV head); code = E4M3(x / scale), to nearest even.  With a power of two the division is exact
+//            (one rounding, the code's own) and so is the read-back (a code has 4 significant bits, bf16 8); codes
+//            being floating-point it costs no precision, only up to one binade at the small end of the range.
+//   append   code = E4M3(clamp(x / scale, +-448)) with the scales in place
+//   read     bf16(scale * decode(code)), the product in fp32
+//
+// All are bound by memory (2 + 1 bytes an element) or, for a step's few rows, by latency.
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+#include <math.h>
+
+#include "common.cuh"
+
+namespace rapid {
+
+namespace {
+
+constexpr float kE4m3Max = 448.f;
+
+struct RowsIn {  // rows to be written: [B, T, Hkv, D] bf16 by element strides, D contiguous
+    const __nv_bfloat16* k;
+    const __nv_bfloat16* v;
+    long long sb, st, sh;
+};
+struct Cache8 {
+    uint8_t* k;
+    uint8_t* v;
+    long long sb, sh, sl, Lmax;
+};
+
+// 8 bf16 of a row -> 8 codes.  What lies beyond the largest code saturates, infinities included; NaN stays NaN.
+// POW2: the scale is a power of two and `inv` its reciprocal.
+template <bool POW2>
+__device__ __forceinline__ uint2 quantise8(const uint4& v, float scale, float inv, bool& clipped) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    uint32_t c[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float lo = __uint_as_float(w[i] << 16), hi = __uint_as_float(w[i] & 0xffff0000u);
+        lo = POW2 ? lo * inv : __fdiv_rn(lo, scale);
+        hi = POW2 ? hi * inv : __fdiv_rn(hi, scale);
+        clipped |= fabsf(lo) > kE4m3Max || fabsf(hi) > kE4m3Max;
+        c[i] = __nv_cvt_float2_to_fp8x2(make_float2(lo, hi), __NV_SATFINITE, __NV_E4M3);
+    }
+    return make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
+}
+
+// ---- append -----------------------------------------------------------------------------------------------------
+// A step's R rows.  Thread = 8 elements; the length, the scale and the rows are requested together, so that a call
+// of a few rows is one round trip.  ctx_out (if any) is another array than ctx here; a caller's in-place update is
+// a second kernel, because every block has to have read the length first.
+__global__ void __launch_bounds__(128) kv_append_fp8_kernel(RowsIn in, Cache8 c, const float* __restrict__ k_scale,
+                                                            const float* __restrict__ v_scale, const int32_t* ctx,
+                                                            int32_t* ctx_out, int R, int Hkv, int D, int32_t* status) {
+    const int b = blockIdx.y;
+    const bool is_v = blockIdx.z;
+    const int per_row = D / 8, per_tok = Hkv * per_row;
+    const int n = R * per_tok;
+    const int i = blockIdx.x * 128 + threadIdx.x, at = min(i, n - 1);
+    const int t = at / per_tok, rem = at - t * per_tok;
+    const int h = rem / per_row, d = (rem - h * per_row) * 8;
+    griddep_wait();
+    griddep_launch_dependents();
+    const uint4 x = __ldg(reinterpret_cast<const uint4*>((is_v ? in.v : in.k) + b * in.sb + t * in.st + h * in.sh + d));
+    const float scale = (is_v ? v_scale : k_scale)[b * Hkv + h];
+    const long long L = ctx[b];
+    const bool fits = L >= 0 && L + R <= c.Lmax;
+    if (i == 0 && !is_v) {
+        if (!fits) atomicOr(status, RAPID_STATUS_BAD_CTX_LEN);
+        if (ctx_out) ctx_out[b] = (int32_t)(fits ? L + R : L);
+    }
+    if (!fits || i >= n) return;
+    bool clipped = false;
+    const uint2 code = quantise8<false>(x, scale, 0.f, clipped);
+    *reinterpret_cast<uint2*>((is_v ? c.v : c.k) + b * c.sb + h * c.sh + (L + t) * c.sl + d) = code;
+    if (clipped) atomicOr(status, RAPID_STATUS_FP8_SATURATED);
+}
+
+__global__ void kv_append_fp8_lens_kernel(int32_t* ctx, int B, int R, long long Lmax) {
+    griddep_wait();
+    griddep_launch_dependents();
+    const int b = blockIdx.x * blockDim.x + threadIdx.x;
+    if (b >= B) return;
+    const long long L = ctx[b];
+    if (L >= 0 && L + R <= Lmax) ctx[b] = (int32_t)(L + R);
+}
+
+// ---- fill -------------------------------------------------------------------------------------------------------
+
+// Exponent of the scale for a largest magnitude given as bf16 bits (7 fraction bits): 448 = 1.75 * 2^8.
+// An infinity counts as the largest finite value; the scale stays a normal number with a normal reciprocal.
+__device__ __forceinline__ int scale_exponent(uint32_t amax_bits, int headroom) {
+    const uint32_t a = min(amax_bits, 0x7f7fu);
+    if (a == 0) return 0;
+    const int e = (int)(a >> 7) - 127 - 8 + ((a & 0x7f) > 0x60 ? 1 : 0) + headroom;
+    return max(-126, min(126, e));
+}
+__device__ __forceinline__ float pow2(int e) { return __int_as_float((e + 127) << 23); }
+
+// Running maximum of |x| over pairs of bf16 (a NaN takes no part).
+__device__ __forceinline__ __nv_bfloat162 absmax(__nv_bfloat162 m, const uint4& v) {
+    const __nv_bfloat162* p = reinterpret_cast<const __nv_bfloat162*>(&v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = __hmax2(m, __habs2(p[i]));
+    return m;
+}
+__device__ __forceinline__ uint32_t absmax_bits(__nv_bfloat162 m) {
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(&m);
+    return max(w & 0x7fffu, (w >> 16) & 0x7fffu);
+}
+
+struct FillArgs {
+    RowsIn in;
+    Cache8 c;
+    const int32_t* n_tokens;  // [B], or NULL: T each
+    float* k_scale;
+    float* v_scale;
+    int32_t* ctx_out;
+    int32_t* status;
+    int B, Hkv, D, T, headroom;
+    int row_shift;  // log2 of a row's chunks of 8 elements, or -1 if that is no power of two
+};
+
+__device__ __forceinline__ int row_of(int chunk, int per_row, int shift) { return shift >= 0 ? chunk >> shift : chunk / per_row; }
+
+// Rows of sequence b, or -1 if it cannot be written.
+__device__ __forceinline__ int fill_rows(const FillArgs& a, int b) {
+    const int n = a.n_tokens ? a.n_tokens[b] : a.T;
+    return n < 0 || n > a.T || n > a.c.Lmax ? -1 : n;
+}
+// What one block per (sequence, K or V, KV head) writes besides the codes.
+__device__ __forceinline__ void fill_scalars(const FillArgs& a, int b, bool is_v, int h, int n, float scale) {
+    if (n >= 0) (is_v ? a.v_scale : a.k_scale)[b * a.Hkv + h] = scale;
+    if (!is_v && h == 0) {
+        if (n < 0) atomicOr(a.status, RAPID_STATUS_BAD_CTX_LEN);
+        else if (a.ctx_out) a.ctx_out[b] = n;
+    }
+}
+
+// Short prompts: one cluster per (sequence, K or V, KV head) holds all of its rows in registers, so they are read
+// once: loads, the largest magnitude over block and cluster (a word of each CTA's shared memory that its peers
+// push to), codes.  CTA r of the cluster takes chunks r * 256 * N .. ; a chunk is 8 elements.
+constexpr int kFillThreads = 256;
+constexpr int kFillCluster = 8;
+
+template <int N>
+__global__ void __launch_bounds__(kFillThreads) kv_fill_cluster_kernel(const FillArgs a) {
+    __shared__ uint32_t peers[kFillCluster];
+    __shared__ uint32_t warps[kFillThreads / 32];
+    const int rank = blockIdx.x, unit = blockIdx.y;  // (grid x = cluster)
+    const int h = unit % a.Hkv, rest = unit / a.Hkv;
+    const bool is_v = rest & 1;
+    const int b = rest >> 1;
+    const int per_row = a.D / 8;
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");  // (a peer's shared memory is written to once it runs)
+    griddep_wait();
+    griddep_launch_dependents();
+    const int n = fill_rows(a, b);
+    const int chunks = max(n, 0) * per_row;
+    const __nv_bfloat16* src = (is_v ? a.in.v : a.in.k) + b * a.in.sb + h * a.in.sh;
+    const int first = rank * kFillThreads * N + threadIdx.x;
+    uint4 x[N];
+    int row[N], col[N];
+    __nv_bfloat162 m = __float2bfloat162_rn(0.f);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int ch = first + i * kFillThreads;
+        row[i] = row_of(ch, per_row, a.row_shift);
+        col[i] = (ch - row[i] * per_row) * 8;
+        x[i] = ch < chunks ? __ldg(reinterpret_cast<const uint4*>(src + row[i] * a.in.st + col[i])) : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) m = absmax(m, x[i]);
+    uint32_t top = __reduce_max_sync(0xffffffffu, absmax_bits(m));
+    if ((threadIdx.x & 31) == 0) warps[threadIdx.x >> 5] = top;
+    __syncthreads();
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (threadIdx.x < kFillCluster) {  // thread p pushes the block's value to CTA p of the cluster
+#pragma unroll
+        for (int w = 0; w < kFillThreads / 32; ++w) top = max(top, warps[w]);
+        uint32_t there;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(smem_u32(&peers[rank])), "r"((int)threadIdx.x));
+        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(there), "r"(top) : "memory");
+    }
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    top = 0;
+#pragma unroll
+    for (int p = 0; p < kFillCluster; ++p) top = max(top, peers[p]);
+    const int e = scale_exponent(top, a.headroom);
+    if (rank == 0 && threadIdx.x == 0) fill_scalars(a, b, is_v, h, n, pow2(e));
+    const float inv = pow2(-e);
+    bool clipped = false;
+    uint8_t* dst = (is_v ? a.c.v : a.c.k) + b * a.c.sb + h * a.c.sh;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (first + i * kFillThreads < chunks)
+            *reinterpret_cast<uint2*>(dst + row[i] * a.c.sl + col[i]) = quantise8<true>(x[i], 0.f, inv, clipped);
+    if (clipped) atomicOr(a.status, RAPID_STATUS_FP8_SATURATED);
+}
+
+// Long prompts: the rows do not fit on chip, so they are read twice, the second time out of L2.  The units
+// (sequence, K or V, KV head) are worked off in groups that L2 holds; work items are handed out by a ticket counter
+// in the order  maxima of group 0 | maxima of group 1 and codes of group 0, alternating | ... .  An item that
+// writes codes waits until the maxima of its group are in: those items were all handed out before it to blocks
+// that wait for nothing, so the wait ends whatever the number of blocks that run at a time (and it is bounded).
+struct FillPlan {
+    int group_heads, groups;   // KV heads of a group, groups in all
+    int item_rows, items;      // rows of an item, items of a group (item = row chunk * group_heads + head)
+    uint32_t* words;           // ticket, then per group the count of finished maxima items, then per unit the maximum
+};
+__device__ __forceinline__ uint32_t ld_acquire(const uint32_t* p) {
+    uint32_t v;
+    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+
+__global__ void kv_fill_clear_kernel(uint32_t* words, int n) {
+    griddep_wait();
+    griddep_launch_dependents();
+    for (int i = threadIdx.x; i < n; i += blockDim.x) words[i] = 0;
+}
+
+template <int UN>
+__global__ void __launch_bounds__(kFillThreads) kv_fill_kernel(const FillArgs a, const FillPlan p) {
+    __shared__ uint32_t warps[kFillThreads / 32];
+    __shared__ uint32_t sh_ticket[2], sh_amax;
+    uint32_t* ticket = p.words;
+    uint32_t* done = p.words + 1;
+    uint32_t* amax = done + p.groups;
+    const int per_row = a.D / 8;
+    const int groups_per = (a.Hkv + p.group_heads - 1) / p.group_heads;  // groups of a (sequence, K or V)
+    const uint32_t total = (uint32_t)(p.groups + 1) * 2u * p.items;
+    griddep_wait();
+    griddep_launch_dependents();
+    bool clipped = false;
+    if (threadIdx.x == 0) sh_ticket[0] = atomicAdd(ticket, 1u);
+    __syncthreads();
+    for (int turn = 0;; turn ^= 1) {
+        const uint32_t tk = sh_ticket[turn];
+        if (tk >= total) break;
+        if (threadIdx.x == 0) sh_ticket[turn ^ 1] = atomicAdd(ticket, 1u);  // the next one, meanwhile
+        const uint32_t step = tk / (2u * p.items), r = tk - step * 2u * p.items;
+        const bool codes = r & 1;
+        const int group = (int)step - (codes ? 1 : 0), item = (int)(r >> 1);
+        const int rest = group < 0 ? 0 : group / groups_per;
+        const bool is_v = rest & 1;
+        const int b = rest >> 1;
+        const int chunk = item / p.group_heads;
+        const int h = (group - rest * groups_per) * p.group_heads + item - chunk * p.group_heads;
+        const bool work = group >= 0 && group < p.groups && h < a.Hkv;
+        const int n = work ? fill_rows(a, b) : -1;
+        const int row0 = chunk * p.item_rows, rows = min(p.item_rows, max(n, 0) - row0);
+        const int unit = rest * a.Hkv + h;
+        const __nv_bfloat16* src = (is_v ? a.in.v : a.in.k) + b * a.in.sb + h * a.in.sh;
+        if (!codes) {
+            if (rows > 0) {
+                __nv_bfloat162 m = __float2bfloat162_rn(0.f);
+                const int chunks = rows * per_row;
+                for (int i0 = threadIdx.x; i0 < chunks; i0 += kFillThreads * UN) {
+                    uint4 x[UN];
+#pragma unroll
+                    for (int u = 0; u < UN; ++u) {
+                        const int i = i0 + u * kFillThreads, row = row_of(i, per_row, a.row_shift);
+                        x[u] = i < chunks ? __ldg(reinterpret_cast<const uint4*>(src + (row0 + row) * a.in.st + (i - row * per_row) * 8))
+                                          : make_uint4(0, 0, 0, 0);
+                    }
+#pragma unroll
+                    for (int u = 0; u < UN; ++u) m = absmax(m, x[u]);
+                }
+                const uint32_t top = __reduce_max_sync(0xffffffffu, absmax_bits(m));
+                if ((threadIdx.x & 31) == 0) warps[threadIdx.x >> 5] = top;
+            }
+            __syncthreads();
+            if (threadIdx.x == 0 && group >= 0 && group < p.groups) {
+                if (rows > 0) {
+                    uint32_t top = 0;
+#pragma unroll
+                    for (int w = 0; w < kFillThreads / 32; ++w) top = max(top, warps[w]);
+                    atomicMax(amax + unit, top);
+                    __threadfence();
+                }
+                atomicAdd(done + group, 1u);
+            }
+        } else {
+            if (threadIdx.x == 0 && work) {
+                const long long t0 = clock64();
+                bool ready = true;
+                while (ld_acquire(done + group) < (uint32_t)p.items) {
+                    if (clock64() - t0 > kWaitCycleLimit) {
+                        ready = false;
+                        atomicOr(a.status, RAPID_STATUS_PIPELINE_TIMEOUT);
+                        break;
+                    }
+                    __nanosleep(100);
+                }
+                sh_amax = ready ? ld_acquire(amax + unit) : 0x10000u;
+            }
+            __syncthreads();
+            if (work && sh_amax <= 0xffffu) {
+                const int e = scale_exponent(sh_amax, a.headroom);
+                if (chunk == 0 && threadIdx.x == 0) fill_scalars(a, b, is_v, h, n, pow2(e));
+                if (rows > 0) {
+                    const float inv = pow2(-e);
+                    uint8_t* dst = (is_v ? a.c.v : a.c.k) + b * a.c.sb + h * a.c.sh;
+                    const int chunks = rows * per_row;
+                    for (int i0 = threadIdx.x; i0 < chunks; i0 += kFillThreads * UN) {
+                        uint4 x[UN];
+#pragma unroll
+                        for (int u = 0; u < UN; ++u) {
+                            const int i = i0 + u * kFillThreads, row = row_of(i, per_row, a.row_shift);
+                            if (i < chunks) x[u] = __ldcs(reinterpret_cast<const uint4*>(src + (row0 + row) * a.in.st + (i - row * per_row) * 8));
+                        }
+#pragma unroll
+                        for (int u = 0; u < UN; ++u) {
+                            const int i = i0 + u * kFillThreads, row = row_of(i, per_row, a.row_shift);
+                            if (i < chunks)
+                                __stcs(reinterpret_cast<uint2*>(dst + (row0 + row) * a.c.sl + (i - row * per_row) * 8),
+                                       quantise8<true>(x[u], 0.f, inv, clipped));
+                        }
+                    }
+                }
+            }
+        }
+        __syncthreads();  // (warps, sh_amax and the ticket of this turn are free again; the next ticket is there)
+    }
+    if (clipped) atomicOr(a.status, RAPID_STATUS_FP8_SATURATED);
+}
+
+// ---- read back --------------------------------------------------------------------------------------------------
+// Chunks of the cache into a bf16 cache, one behind the other.  A block takes 16 KB of codes of one (sequence, K or
+// V, KV head, chunk); where its rows go depends on the chunks before (a partial one is shorter, -1 is none), which
+// the block adds up while its codes are on their way.
+struct ReadArgs {
+    Cache8 c;
+    const float* k_scale;
+    const float* v_scale;
+    const int32_t* ctx;
+    const int32_t* idx;  // [B, n_chunks], or NULL: 0, 1, 2, ...
+    __nv_bfloat16* k_out;
+    __nv_bfloat16* v_out;
+    int32_t* out_lens;
+    int32_t* status;
+    long long ob, oh, ol, Lout;  // strides of the output, its capacity
+    int B, Hkv, D, n_chunks, chunk;
+};
+constexpr int kReadThreads = 256;
+constexpr int kReadUnroll = 4;  // 16-byte loads in flight per thread
+
+// Rows that chunk number i of sequence b holds.
+__device__ __forceinline__ int chunk_rows(const ReadArgs& a, int ctx, int i) {
+    if (i < 0) return 0;
+    const long long from = (long long)i * a.chunk;
+    return (int)max(0LL, min((long long)a.chunk, ctx - from));
+}
+
+__global__ void __launch_bounds__(kReadThreads) kv_read_fp8_kernel(const ReadArgs a) {
+    __shared__ int warps[kReadThreads / 32];
+    const int j = blockIdx.y;  // which of the chunks
+    const int h = blockIdx.z % a.Hkv, rest = blockIdx.z / a.Hkv;
+    const bool is_v = rest & 1;
+    const int b = rest >> 1;
+    const int per_row = a.D / 16;
+    griddep_wait();
+    griddep_launch_dependents();
+    const int given = a.ctx[b];
+    const int ctx = (int)max(0LL, min((long long)given, a.c.Lmax));
+    const int number = a.idx ? a.idx[(size_t)b * a.n_chunks + j] : j;
+    const int rows = chunk_rows(a, ctx, number);
+    const int first = blockIdx.x * kReadThreads * kReadUnroll + threadIdx.x;
+    const uint8_t* src = (is_v ? a.c.v : a.c.k) + b * a.c.sb + h * a.c.sh;
+    uint4 x[kReadUnroll];
+    int row[kReadUnroll], col[kReadUnroll];
+#pragma unroll
+    for (int u = 0; u < kReadUnroll; ++u) {
+        const int i = first + u * kReadThreads;
+        row[u] = i / per_row;
+        col[u] = (i - row[u] * per_row) * 16;
+        if (row[u] < rows)
+            x[u] = __ldcs(reinterpret_cast<const uint4*>(src + ((long long)number * a.chunk + row[u]) * a.c.sl + col[u]));
+    }
+    const float scale = (is_v ? a.v_scale : a.k_scale)[b * a.Hkv + h];
+    // the rows before this chunk's
+    long long before = 0;
+    const bool teller = blockIdx.x == 0 && h == 0 && !is_v && j == a.n_chunks - 1;
+    if (a.idx) {
+        int s = 0;
+        for (int i = threadIdx.x; i < j; i += kReadThreads) s += chunk_rows(a, ctx, a.idx[(size_t)b * a.n_chunks + i]);
+        s = __reduce_add_sync(0xffffffffu, s);
+        if ((threadIdx.x & 31) == 0) warps[threadIdx.x >> 5] = s;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kReadThreads / 32; ++w) before += warps[w];
+    } else {
+        before = min((long long)ctx, (long long)j * a.chunk);
+    }
+    if (threadIdx.x == 0) {
+        if (teller) {
+            a.out_lens[b] = (int32_t)min(before + rows, a.Lout);
+            if (given != ctx) atomicOr(a.status, RAPID_STATUS_BAD_CTX_LEN);
+        }
+        if (blockIdx.x == 0 && h == 0 && !is_v && (number < -1 || (number >= 0 && rows == 0 && a.idx) || before + rows > a.Lout))
+            atomicOr(a.status, RAPID_STATUS_BAD_CTX_LEN);
+    }
+    __nv_bfloat16* dst = (is_v ? a.v_out : a.k_out) + b * a.ob + h * a.oh;
+#pragma unroll
+    for (int u = 0; u < kReadUnroll; ++u) {
+        const long long to = before + row[u];
+        if (row[u] >= rows || to >= a.Lout) continue;
+        const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+        uint32_t o[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const __half2_raw r = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[i >> 1] >> (16 * (i & 1))), __NV_E4M3);
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&r));
+            o[i] = pack_bf16x2(f.x * scale, f.y * scale);
+        }
+        uint4* out = reinterpret_cast<uint4*>(dst + to * a.ol + col[u]);
+        __stcs(out, make_uint4(o[0], o[1], o[2], o[3]));
+        __stcs(out + 1, make_uint4(o[4], o[5], o[6], o[7]));
+    }
+}
+
+// ---- host side --------------------------------------------------------------------------------------------------
+
+bool cache8_of(const char* who, const rapid_attn_shape* s, void* k, void* v, Cache8& c) {
+    if (s->B <= 0 || s->Hkv <= 0 || s->Lmax <= 0 || s->D <= 0 || s->Lmax > 0x7fffffffLL) {
+        set_error("%s: invalid shape", who);
+        return false;
+    }
+    c.k = static_cast<uint8_t*>(k);
+    c.v = static_cast<uint8_t*>(v);
+    c.sl = s->kv_stride_l ? s->kv_stride_l : s->D;
+    c.sh = s->kv_stride_h ? s->kv_stride_h : s->Lmax * c.sl;
+    c.sb = s->kv_stride_b ? s->kv_stride_b : s->Hkv * c.sh;
+    c.Lmax = s->Lmax;
+    return true;
+}
+// Whether strides and pointers allow 16-byte accesses of codes and of bf16 rows.
+bool cache8_aligned(const char* who, int D, const Cache8& c) {
+    if (D % 16 || c.sl < D || c.sl % 16 || c.sh % 16 || c.sb % 16 || c.sh <= 0 || c.sb <= 0 || (((uintptr_t)c.k | (uintptr_t)c.v) & 15)) {
+        set_error("%s: head_dim and the cache's strides must be positive multiples of 16, its pointers 16-byte aligned", who);
+        return false;
+    }
+    return true;
+}
+bool rows_of(const char* who, const rapid_kv_rows* r, int T, int Hkv, int D, const void* k, const void* v, RowsIn& in) {
+    in.k = static_cast<const __nv_bfloat16*>(k);
+    in.v = static_cast<const __nv_bfloat16*>(v);
+    in.sh = r && r->stride_h ? r->stride_h : D;
+    in.st = r && r->stride_t ? r->stride_t : (long long)Hkv * D;
+    in.sb = r && r->stride_b ? r->stride_b : (long long)T * Hkv * D;
+    if (in.sh % 8 || in.st % 8 || in.sb % 8 || in.sh <= 0 || in.st <= 0 || in.sb <= 0 || (((uintptr_t)k | (uintptr_t)v) & 15)) {
+        set_error("%s: the rows' strides must be positive multiples of 8 elements, their pointers 16-byte aligned", who);
+        return false;
+    }
+    return true;
+}
+
+}  // namespace
+
+int launch_kv_append_fp8(const void* k_new, const void* v_new, const rapid_kv_rows* rows, void* k_cache, void* v_cache,
+                         const float* k_scale, const float* v_scale, const int32_t* ctx_lens, int32_t* ctx_lens_out,
+                         int gamma, const rapid_attn_shape* shape, int32_t* status_word, cudaStream_t stream) {
+    const char* who = "rapid_kv_append_fp8";
+    if (!k_new || !v_new || !k_cache || !v_cache || !k_scale || !v_scale || !ctx_lens || !shape || !status_word) {
+        set_error("%s: NULL argument", who);
+        return RAPID_ERR_INVALID_ARG;
+    }
+    Cache8 c;
+    if (!cache8_of(who, shape, k_cache, v_cache, c)) return RAPID_ERR_INVALID_ARG;
+    const rapid_attn_shape& s = *shape;
+    if (gamma < 0 || s.B > 65535 || ((int64_t)gamma + 1) * s.Hkv * s.D > 0x7fffffffLL - 1024) {
+        set_error("%s: gamma must not be negative, B at most 65535 and a sequence's new rows below 2^31 elements", who);
+        return RAPID_ERR_INVALID_ARG;
+    }
+    const int R = gamma + 1;
+    RowsIn in;
+    if (!cache8_aligned(who, s.D, c) || !rows_of(who, rows, R, s.Hkv, s.D, k_new, v_new, in)) return RAPID_ERR_UNSUPPORTED;
+    const bool in_place = ctx_lens_out == ctx_lens;
+    const int chunks = R * s.Hkv * (s.D / 8);
+    RAPID_CUDA_CHECK(launch_dependent(kv_append_fp8_kernel, dim3((chunks + 127) / 128, s.B, 2), dim3(128), 0, stream, in, c, k_scale,
+                                      v_scale, ctx_lens, in_place ? nullptr : ctx_lens_out, R, s.Hkv, s.D, status_word));
+    count_launch(1);
+    if (in_place) {
+        RAPID_CUDA_CHECK(launch_dependent(kv_append_fp8_lens_kernel, dim3((s.B + 127) / 128), dim3(128), 0, stream, ctx_lens_out,
+                                          s.B, R, (long long)s.Lmax));
+        count_launch(1);
+    }
+    return RAPID_OK;
+}
+
+// Words of scratch of a fill: ticket, a count per group (at most one group per unit), a maximum per unit.
+size_t kv_fill_workspace_bytes(int B, int Hkv) {
+    if (B <= 0 || Hkv <= 0) return 0;
+    return kWorkspaceHeaderBytes + align_up((1 + 2 * (size_t)2 * B * Hkv) * sizeof(uint32_t), 256);
+}
+
+int launch_kv_fill_fp8(const void* k_new, const void* v_new, const rapid_kv_rows* rows, int T, const int32_t* n_tokens,
+                       void* k_cache, void* v_cache, float* k_scale, float* v_scale, int32_t* ctx_lens_out, int headroom,
+                       const rapid_attn_shape* shape, void* workspace, size_t workspace_bytes, cudaStream_t stream) {
+    const char* who = "rapid_kv_fill_fp8";
+    if (!k_new || !v_new || !k_cache || !v_cache || !k_scale || !v_scale || !shape) {
+        set_error("%s: NULL argument", who);
+        return RAPID_ERR_INVALID_ARG;
+    }
+    FillArgs a = {};
+    if (!cache8_of(who, shape, k_cache, v_cache, a.c)) return RAPID_ERR_INVALID_ARG;
+    const rapid_attn_shape& s = *shape;
+    if (T <= 0 || headroom < 0 || headroom > 8) {
+        set_error("%s: T must be positive and headroom in [0, 8]", who);
+        return RAPID_ERR_INVALID_ARG;
+    }
+    const int64_t units = 2 * (int64_t)s.B * s.Hkv;
+    if (units > 65535 || (int64_t)T * s.D > 0x7fffffffLL - 65536) {
+        set_error("%s: 2 * B * Hkv at most 65535, T * D below 2^31", who);
+        return RAPID_ERR_UNSUPPORTED;
+    }
+    if (!cache8_aligned(who, s.D, a.c) || !rows_of(who, rows, T, s.Hkv, s.D, k_new, v_new, a.in)) return RAPID_ERR_UNSUPPORTED;
+    if (!workspace || workspace_bytes < kv_fill_workspace_bytes(s.B, s.Hkv) || ((uintptr_t)workspace & 255)) {
+        set_error("%s: workspace of %zu bytes needed (256-byte aligned), got %zu", who, kv_fill_workspace_bytes(s.B, s.Hkv),
+                  workspace_bytes);
+        return RAPID_ERR_WORKSPACE;
+    }
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    a.n_tokens = n_tokens;
+    a.k_scale = k_scale;
+    a.v_scale = v_scale;
+    a.ctx_out = ctx_lens_out;
+    a.status = reinterpret_cast<int32_t*>(ws);
+    a.B = s.B;
+    a.Hkv = s.Hkv;
+    a.D = s.D;
+    a.T = T;
+    a.headroom = headroom;
+    a.row_shift = -1;
+    for (int i = 0; i < 16; ++i)
+        if (s.D == 8 << i) a.row_shift = i;
+    const int64_t chunks = (int64_t)T * (s.D / 8);
+    const int64_t per_n = (int64_t)kFillThreads * kFillCluster;
+    if (chunks <= 8 * per_n) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(kFillCluster, (unsigned)units);
+        cfg.blockDim = dim3(kFillThreads);
+        cfg.stream = stream;
+        cudaLaunchAttribute attr[2];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = kFillCluster;
+        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 2;
+        if (chunks <= per_n) RAPID_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kv_fill_cluster_kernel<1>, a));
+        else if (chunks <= 2 * per_n) RAPID_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kv_fill_cluster_kernel<2>, a));
+        else if (chunks <= 4 * per_n) RAPID_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kv_fill_cluster_kernel<4>, a));
+        else RAPID_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kv_fill_cluster_kernel<8>, a));
+        count_launch(1);
+        return RAPID_OK;
+    }
+    constexpr int64_t kGroupBytes = 32 << 20, kItemBytes = 64 << 10;
+    FillPlan p;
+    const int64_t unit_bytes = (int64_t)T * s.D * 2;
+    p.group_heads = (int)(kGroupBytes / unit_bytes < 1 ? 1 : kGroupBytes / unit_bytes > s.Hkv ? s.Hkv : kGroupBytes / unit_bytes);
+    p.groups = 2 * s.B * ((s.Hkv + p.group_heads - 1) / p.group_heads);
+    p.item_rows = (int)(kItemBytes / (s.D * 2) > 0 ? kItemBytes / (s.D * 2) : 1);
+    p.items = (T + p.item_rows - 1) / p.item_rows * p.group_heads;
+    if (((int64_t)p.groups + 1) * 2 * p.items > 0x7fffffffLL) {
+        set_error("%s: too many rows in one call", who);
+        return RAPID_ERR_UNSUPPORTED;
+    }
+    p.words = reinterpret_cast<uint32_t*>(ws + kWorkspaceHeaderBytes);
+    int dev = 0, sms = 0;
+    RAPID_CUDA_CHECK(cudaGetDevice(&dev));
+    RAPID_CUDA_CHECK(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+    RAPID_CUDA_CHECK(launch_dependent(kv_fill_clear_kernel, dim3(1), dim3(256), 0, stream, p.words, (int)(1 + p.groups + units)));
+    RAPID_CUDA_CHECK(launch_dependent(kv_fill_kernel<8>, dim3(sms * 4), dim3(kFillThreads), 0, stream, a, p));
+    count_launch(2);
+    return RAPID_OK;
+}
+
+int launch_kv_read_fp8(const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
+                       const int32_t* ctx_lens, const rapid_attn_shape* shape, const int32_t* chunk_idx, int n_chunks,
+                       int chunk_tokens, void* k_out, void* v_out, const rapid_attn_shape* out_shape, int32_t* out_lens,
+                       int32_t* status_word, cudaStream_t stream) {
+    const char* who = "rapid_kv_read_fp8";
+    if (!k_cache || !v_cache || !k_scale || !v_scale || !ctx_lens || !shape || !k_out || !v_out || !out_shape || !out_lens || !status_word) {
+        set_error("%s: NULL argument", who);
+        return RAPID_ERR_INVALID_ARG;
+    }
+    ReadArgs a = {};
+    Cache8 o;  // (the output's geometry goes through the same defaults)
+    if (!cache8_of(who, shape, const_cast<void*>(k_cache), const_cast<void*>(v_cache), a.c) || !cache8_of(who, out_shape, k_out, v_out, o))
+        return RAPID_ERR_INVALID_ARG;
+    const rapid_attn_shape& s = *shape;
+    if (n_chunks <= 0 || chunk_tokens <= 0 || out_shape->B != s.B || out_shape->Hkv != s.Hkv || out_shape->D != s.D) {
+        set_error("%s: n_chunks and chunk_tokens must be positive and the output of the cache's B, Hkv and D", who);
+        return RAPID_ERR_INVALID_ARG;
+    }
+    if (!cache8_aligned(who, s.D, a.c)) return RAPID_ERR_UNSUPPORTED;
+    if (o.sl < s.D || o.sl % 8 || o.sh % 8 || o.sb % 8 || o.sh <= 0 || o.sb <= 0 || (((uintptr_t)k_out | (uintptr_t)v_out) & 15)) {
+        set_error("%s: the output's strides must be positive multiples of 8 elements, its pointers 16-byte aligned", who);
+        return RAPID_ERR_UNSUPPORTED;
+    }
+    const int64_t units = 2 * (int64_t)s.B * s.Hkv;
+    if (units > 65535 || n_chunks > 65535 || (int64_t)chunk_tokens * s.D > 0x7fffffffLL - 65536) {
+        set_error("%s: 2 * B * Hkv and n_chunks at most 65535, chunk_tokens * D below 2^31", who);
+        return RAPID_ERR_UNSUPPORTED;
+    }
+    a.k_scale = k_scale;
+    a.v_scale = v_scale;
+    a.ctx = ctx_lens;
+    a.idx = chunk_idx;
+    a.k_out = static_cast<__nv_bfloat16*>(k_out);
+    a.v_out = static_cast<__nv_bfloat16*>(v_out);
+    a.out_lens = out_lens;
+    a.status = status_word;
+    a.ob = o.sb;
+    a.oh = o.sh;
+    a.ol = o.sl;
+    a.Lout = o.Lmax;
+    a.B = s.B;
+    a.Hkv = s.Hkv;
+    a.D = s.D;
+    a.n_chunks = n_chunks;
+    a.chunk = chunk_tokens;
+    // no chunk is longer than the cache
+    const int64_t longest = chunk_tokens < s.Lmax ? chunk_tokens : s.Lmax;
+    const int64_t per_block = (int64_t)kReadThreads * kReadUnroll;
+    const int64_t blocks = (longest * (s.D / 16) + per_block - 1) / per_block;
+    RAPID_CUDA_CHECK(launch_dependent(kv_read_fp8_kernel, dim3((unsigned)blocks, n_chunks, (unsigned)units), dim3(kReadThreads), 0,
+                                      stream, a));
+    count_launch(1);
+    return RAPID_OK;
+}
+
+}  // namespace rapid
