@@ -4,6 +4,7 @@ from __future__ import annotations
 import ctypes
 import os
 from dataclasses import dataclass
+from functools import lru_cache
 from typing import Optional
 
 import torch
@@ -234,6 +235,86 @@ def _stream_ptr(stream) -> int:
     return int(stream.cuda_stream)
 
 
+# The calls of a decode loop that is not captured in a graph cost the host more than the device: a step's append is
+# 1.6 us of kernel.  The wrappers of the prefix attention and of the FP8 cache therefore look at each tensor once, keep what
+# follows from shapes and strides alone by those (never by a tensor's address or identity), and pass addresses as plain ints.
+_BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
+
+
+def _here(stream, *tensors) -> int:
+    """The stream to launch on; every tensor (or None) has to be on the current device, which the library uses."""
+    dev = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -2
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError("every tensor must be on the current CUDA device")
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+
+
+def _told(shape, stride):
+    """Element strides for the library, which reads 0 as "dense": an axis of one entry has none to tell, and a broadcast
+    axis cannot be told.  The last axis has to be contiguous."""
+    if stride[-1] != 1 and shape[-1] != 1:
+        raise ValueError("head_dim must be contiguous")
+    if any(st == 0 and n > 1 for n, st in zip(shape, stride)):
+        raise ValueError("a broadcast axis (stride 0) is not supported")
+    return [st if n > 1 else 0 for n, st in zip(shape[:-1], stride[:-1])]
+
+
+@lru_cache(maxsize=512)
+def _prefix_geometry(q, kp, kps, k, kst, gamma):
+    """(attention shape, prefix geometry) of a call with a prefix of its own."""
+    if len(q) != 4 or q[1] != gamma + 1:
+        raise ValueError("q and out must be dense [B, gamma+1, Hq, D]")
+    if len(k) != 4 or k[0] != q[0] or k[3] != q[3]:
+        raise ValueError("k_cache and v_cache must be [B, Hkv, Lmax, D] of q's batch and head_dim")
+    if len(kp) != 3 or kp[0] != k[1] or kp[2] != q[3]:
+        raise ValueError("k_prefix and v_prefix must be [Hkv, Pmax, D] with the cache's KV heads and head_dim")
+    return _AttnShape(q[0], q[2], k[1], q[3], k[2], *_told(k, kst)), _PrefixKv(kp[1], *_told(kp, kps))
+
+
+@lru_cache(maxsize=512)
+def _prefix_paged_geometry(q, k, kst, table, gamma):
+    """(attention shape, pool geometry) of a paged call."""
+    if len(q) != 4 or q[1] != gamma + 1:
+        raise ValueError("q and out must be dense [B, gamma+1, Hq, D]")
+    if len(k) != 4 or k[3] != q[3]:
+        raise ValueError("k_pool and v_pool must be [num_blocks, Hkv, block_size, D] of q's head_dim")
+    if len(table) != 2 or table[0] != q[0]:
+        raise ValueError("block_table must be dense [B, max_blocks_per_seq]")
+    return (_AttnShape(q[0], q[2], k[1], q[3], table[1] * k[2], 0, 0, 0),
+            _PagedKv(k[2], k[0], table[1], 0, *_told(k, kst)))
+
+
+@lru_cache(maxsize=512)
+def _cache8_geometry(k, kst):
+    if len(k) != 4:
+        raise ValueError("k_cache and v_cache must be [B, Hkv, Lmax, D]")
+    return _AttnShape(k[0], k[1], k[1], k[3], k[2], *_told(k, kst))
+
+
+@lru_cache(maxsize=512)
+def _rows_geometry(new, nst, k):
+    if len(new) != 4 or (new[0], new[2], new[3]) != (k[0], k[1], k[3]):
+        raise ValueError("the new rows must be [B, T, Hkv, D] of the cache's batch, KV heads and head_dim")
+    return _KvRows(*_told(new, nst))
+
+
+def _alike(a, b, what):
+    shape, stride = a.shape, a.stride()
+    if b.shape != shape or b.stride() != stride:
+        raise ValueError(what + " must share shape and strides")
+    return shape, stride
+
+
+def _lens(t, B, name):
+    if t is not None and (t.dtype is not _I32 or t.numel() != B or not t.is_contiguous()):
+        raise TypeError(name + " must be dense int32 [B]")
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
+
+
 def _p(t: Optional[torch.Tensor]):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
@@ -414,35 +495,19 @@ def prefix_attention_workspace_bytes(B, Hq, Hkv, D, gamma) -> int:
     return int(load_library().rapid_prefix_attention_workspace_bytes(ctypes.byref(s), gamma))
 
 
-def _check_prefix_call(q, out, kv, ctx_lens, prefix_len, gamma, params):
-    if any(t.dtype != torch.bfloat16 for t in (q, out, *kv)) or ctx_lens.dtype != torch.int32 \
-            or prefix_len.dtype != torch.int32:
-        raise TypeError("q, out and the caches must be bfloat16, ctx_lens and prefix_len int32")
-    if q.dim() != 4 or not (q.is_contiguous() and out.is_contiguous()) or q.shape[1] != gamma + 1 or out.shape != q.shape:
+def _prefix_outputs(q, out, ctx_lens, prefix_len, params):
+    if out.dtype is not _BF16 or ctx_lens.dtype is not _I32 or prefix_len.dtype is not _I32:
+        raise TypeError("out must be bfloat16, ctx_lens and prefix_len int32")
+    if not (q.is_contiguous() and out.is_contiguous()) or out.shape != q.shape:
         raise ValueError("q and out must be dense [B, gamma+1, Hq, D]")
     if ctx_lens.numel() != q.shape[0] or not ctx_lens.is_contiguous() or prefix_len.numel() != 1:
         raise ValueError("ctx_lens must be dense [B] and prefix_len hold one length")
-    if params is not None:
-        for t, n in ((params.lse_out, q.numel() // q.shape[3]), (params.out_f32, q.numel())):
-            if t is not None and (t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous()):
-                raise ValueError("lse_out must be dense float32 [B, gamma+1, Hq] and out_f32 [B, gamma+1, Hq, D]")
-    _check_device(q, out, *kv, ctx_lens, prefix_len)
-
-
-def _strides(t, n):
-    """Element strides of the first n axes for the library, which reads 0 as "dense": an axis of one entry has none to
-    tell, and a broadcast axis cannot be told."""
-    if any(t.stride(i) == 0 and t.shape[i] > 1 for i in range(n)):
-        raise ValueError("a broadcast axis (stride 0) is not supported")
-    return [t.stride(i) if t.shape[i] > 1 else 0 for i in range(n)]
-
-
-def _check_device(*tensors):
-    """The library launches on the current device: every tensor has to live there."""
-    here = torch.cuda.current_device() if torch.cuda.is_available() else None
-    for t in tensors:
-        if t is not None and (not t.is_cuda or t.device.index != here):
-            raise ValueError("every tensor must be on the current CUDA device")
+    if params is None:
+        return None, None
+    for t, n in ((params.lse_out, q.numel() // q.shape[3]), (params.out_f32, q.numel())):
+        if t is not None and (t.dtype is not _F32 or t.numel() != n or not t.is_contiguous()):
+            raise ValueError("lse_out must be dense float32 [B, gamma+1, Hq] and out_f32 [B, gamma+1, Hq, D]")
+    return params.lse_out, params.out_f32
 
 
 def rapid_verify_attention_prefix(q, k_prefix, v_prefix, prefix_len, k_cache, v_cache, ctx_lens, gamma, out, workspace,
@@ -450,46 +515,33 @@ def rapid_verify_attention_prefix(q, k_prefix, v_prefix, prefix_len, k_cache, v_
     """Verify attention of a batch over a prefix that is stored once (k_prefix / v_prefix [Hkv, Pmax, D], of which
     prefix_len [1] keys count) and each sequence's own keys (k_cache / v_cache [B, Hkv, Lmax, D], ctx_lens [B] of
     them, the gamma+1 newest included).  bf16; caches may be strided with a contiguous head_dim."""
-    _check_prefix_call(q, out, (k_prefix, v_prefix, k_cache, v_cache), ctx_lens, prefix_len, gamma, params)
-    if k_cache.stride() != v_cache.stride() or k_cache.shape != v_cache.shape or k_cache.dim() != 4:
-        raise ValueError("k_cache and v_cache must share shape [B, Hkv, Lmax, D] and strides")
-    if k_prefix.stride() != v_prefix.stride() or k_prefix.shape != v_prefix.shape or k_prefix.dim() != 3:
-        raise ValueError("k_prefix and v_prefix must share shape [Hkv, Pmax, D] and strides")
-    if k_prefix.stride(2) != 1 or k_prefix.shape[0] != k_cache.shape[1] or k_prefix.shape[2] != q.shape[3]:
-        raise ValueError("the prefix must have the cache's KV heads and a contiguous head_dim")
-    B, _, Hq, D = q.shape
-    if k_cache.shape[0] != B or k_cache.shape[3] != D or k_cache.stride(3) != 1:
-        raise ValueError("k_cache and v_cache must be [B, Hkv, Lmax, D] of q's batch and a contiguous head_dim")
-    shape = _AttnShape(B, Hq, k_cache.shape[1], D, k_cache.shape[2], *_strides(k_cache, 3))
-    prefix = _PrefixKv(k_prefix.shape[1], *_strides(k_prefix, 2))
+    if not (q.dtype is k_prefix.dtype is v_prefix.dtype is k_cache.dtype is v_cache.dtype is _BF16):
+        raise TypeError("q and the caches must be bfloat16")
+    shape, prefix = _prefix_geometry(q.shape, *_alike(k_prefix, v_prefix, "k_prefix and v_prefix"),
+                                     *_alike(k_cache, v_cache, "k_cache and v_cache"), gamma)
+    extra = _prefix_outputs(q, out, ctx_lens, prefix_len, params)
+    st = _here(stream, q, k_prefix, v_prefix, prefix_len, k_cache, v_cache, ctx_lens, out, workspace, *extra)
     _check(load_library().rapid_verify_attention_prefix(
-        _p(q), _p(k_prefix), _p(v_prefix), ctypes.byref(prefix), _p(prefix_len), _p(k_cache), _p(v_cache), _p(ctx_lens),
-        gamma, _p(out), ctypes.byref(shape), _attn_params(params), _p(workspace), _nbytes(workspace),
-        _stream_ptr(stream)))
+        q.data_ptr(), k_prefix.data_ptr(), v_prefix.data_ptr(), ctypes.byref(prefix), prefix_len.data_ptr(),
+        k_cache.data_ptr(), v_cache.data_ptr(), ctx_lens.data_ptr(), gamma, out.data_ptr(), ctypes.byref(shape),
+        _attn_params(params), workspace.data_ptr(), _nbytes(workspace), st))
 
 
 def rapid_verify_attention_prefix_paged(q, k_pool, v_pool, block_table, prefix_len, ctx_lens, gamma, out, workspace,
                                         params: Optional[AttnParams] = None, stream=None) -> None:
     """rapid_verify_attention_paged for sequences whose first prefix_len [1] keys lie in the same blocks: those are
     read once for the batch, through row 0 of block_table.  ctx_lens counts all keys, the prefix included."""
-    _check_prefix_call(q, out, (k_pool, v_pool), ctx_lens, prefix_len, gamma, params)
-    if k_pool.stride() != v_pool.stride() or k_pool.shape != v_pool.shape or k_pool.dim() != 4 or k_pool.stride(3) != 1:
-        raise ValueError("k_pool and v_pool must share shape and strides, with a contiguous head_dim")
-    if block_table.dtype != torch.int32:
-        raise TypeError("block_table must be int32")
-    B, _, Hq, D = q.shape
-    if not block_table.is_contiguous() or block_table.dim() != 2 or block_table.shape[0] != B:
+    if not (q.dtype is k_pool.dtype is v_pool.dtype is _BF16) or block_table.dtype is not _I32:
+        raise TypeError("q and the pools must be bfloat16, block_table int32")
+    if not block_table.is_contiguous():
         raise ValueError("block_table must be dense [B, max_blocks_per_seq]")
-    _check_device(block_table)
-    nb, Hkv, bs, Dk = k_pool.shape
-    if Dk != D:
-        raise ValueError("q and k_pool disagree on head_dim")
-    mb = block_table.shape[1]
-    shape = _AttnShape(B, Hq, Hkv, D, mb * bs, 0, 0, 0)
-    paged = _PagedKv(bs, nb, mb, 0, *_strides(k_pool, 3))
+    shape, paged = _prefix_paged_geometry(q.shape, *_alike(k_pool, v_pool, "k_pool and v_pool"), block_table.shape, gamma)
+    extra = _prefix_outputs(q, out, ctx_lens, prefix_len, params)
+    st = _here(stream, q, k_pool, v_pool, block_table, prefix_len, ctx_lens, out, workspace, *extra)
     _check(load_library().rapid_verify_attention_prefix_paged(
-        _p(q), _p(k_pool), _p(v_pool), _p(block_table), ctypes.byref(paged), _p(prefix_len), _p(ctx_lens), gamma,
-        _p(out), ctypes.byref(shape), _attn_params(params), _p(workspace), _nbytes(workspace), _stream_ptr(stream)))
+        q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), block_table.data_ptr(), ctypes.byref(paged),
+        prefix_len.data_ptr(), ctx_lens.data_ptr(), gamma, out.data_ptr(), ctypes.byref(shape), _attn_params(params),
+        workspace.data_ptr(), _nbytes(workspace), st))
 
 
 def rapid_draft_sample(draft_logits, uniforms, temperature, out_token, out_logq, workspace, out_row_stats=None,
@@ -642,94 +694,86 @@ def kv_fill_workspace_bytes(B, Hkv) -> int:
     return int(load_library().rapid_kv_fill_workspace_bytes(int(B), int(Hkv)))
 
 
-def _fp8_cache_shape(k_cache, v_cache, k_scale, v_scale) -> _AttnShape:
+def _cache8(k_cache, v_cache, k_scale, v_scale):
+    """(shape of the cache, its geometry for the library)"""
     if k_cache.element_size() != 1 or v_cache.element_size() != 1:
         raise TypeError("k_cache / v_cache must hold one-byte E4M3 codes")
-    if k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32:
+    if not (k_scale.dtype is v_scale.dtype is _F32):
         raise TypeError("k_scale / v_scale must be float32")
-    if k_cache.dim() != 4 or k_cache.stride() != v_cache.stride() or k_cache.shape != v_cache.shape or k_cache.stride(3) != 1:
-        raise ValueError("k_cache and v_cache must share shape [B, Hkv, Lmax, D] and strides with a contiguous head_dim")
-    B, Hkv, Lmax, D = k_cache.shape
-    if k_scale.shape != (B, Hkv) or v_scale.shape != (B, Hkv) or not (k_scale.is_contiguous() and v_scale.is_contiguous()):
+    shape, stride = _alike(k_cache, v_cache, "k_cache and v_cache")
+    geometry = _cache8_geometry(shape, stride)
+    if k_scale.shape != shape[:2] or v_scale.shape != shape[:2] or not (k_scale.is_contiguous() and v_scale.is_contiguous()):
         raise ValueError("k_scale / v_scale must be dense [B, Hkv]")
-    return _AttnShape(B, Hkv, Hkv, D, Lmax, *_strides(k_cache, 3))
+    return shape, geometry
 
 
-def _new_rows(k_new, v_new, k_cache) -> _KvRows:
-    if k_new.dtype != torch.bfloat16 or v_new.dtype != torch.bfloat16:
+def _new_rows(k_new, v_new, cache_shape):
+    if not (k_new.dtype is v_new.dtype is _BF16):
         raise TypeError("k_new / v_new must be bfloat16")
-    if k_new.dim() != 4 or k_new.shape != v_new.shape or k_new.stride() != v_new.stride() or k_new.stride(3) != 1:
-        raise ValueError("k_new and v_new must share shape [B, T, Hkv, D] and strides with a contiguous head_dim")
-    B, _, Hkv, D = k_new.shape
-    if (B, Hkv, D) != (k_cache.shape[0], k_cache.shape[1], k_cache.shape[3]):
-        raise ValueError("the new rows and the cache disagree on batch, KV heads or head_dim")
-    return _KvRows(*_strides(k_new, 3))
-
-
-def _lens(t, B, name):
-    if t is not None and (t.dtype != torch.int32 or t.numel() != B or not t.is_contiguous()):
-        raise TypeError(f"{name} must be dense int32 [B]")
+    shape, stride = _alike(k_new, v_new, "k_new and v_new")
+    return shape, _rows_geometry(shape, stride, cache_shape)
 
 
 def rapid_kv_fill_fp8(k_new, v_new, n_tokens, k_cache, v_cache, k_scale, v_scale, ctx_lens_out, workspace,
                       headroom: int = 0, stream=None) -> None:
     """Quantises a prompt's rows k_new / v_new [B, T, Hkv, D] (bf16, may be strided; n_tokens [B] of them count, or all
     for None) into the E4M3 cache k_cache / v_cache [B, Hkv, Lmax, D] and writes its power-of-two scales [B, Hkv]."""
-    shape = _fp8_cache_shape(k_cache, v_cache, k_scale, v_scale)
-    rows = _new_rows(k_new, v_new, k_cache)
-    _lens(n_tokens, shape.B, "n_tokens")
-    _lens(ctx_lens_out, shape.B, "ctx_lens_out")
-    _check_device(k_new, v_new, n_tokens, k_cache, v_cache, k_scale, v_scale, ctx_lens_out)
-    _check(load_library().rapid_kv_fill_fp8(_p(k_new), _p(v_new), ctypes.byref(rows), k_new.shape[1], _p(n_tokens),
-                                            _p(k_cache), _p(v_cache), _p(k_scale), _p(v_scale), _p(ctx_lens_out),
-                                            int(headroom), ctypes.byref(shape), _p(workspace), _nbytes(workspace),
-                                            _stream_ptr(stream)))
+    cache, geometry = _cache8(k_cache, v_cache, k_scale, v_scale)
+    new, rows = _new_rows(k_new, v_new, cache)
+    _lens(n_tokens, cache[0], "n_tokens")
+    _lens(ctx_lens_out, cache[0], "ctx_lens_out")
+    st = _here(stream, k_new, v_new, n_tokens, k_cache, v_cache, k_scale, v_scale, ctx_lens_out, workspace)
+    _check(load_library().rapid_kv_fill_fp8(
+        k_new.data_ptr(), v_new.data_ptr(), ctypes.byref(rows), new[1], _addr(n_tokens), k_cache.data_ptr(),
+        v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), _addr(ctx_lens_out), headroom, ctypes.byref(geometry),
+        workspace.data_ptr(), _nbytes(workspace), st))
 
 
 def rapid_kv_append_fp8(k_new, v_new, k_cache, v_cache, k_scale, v_scale, ctx_lens, ctx_lens_out, gamma, status_word,
                         stream=None) -> None:
     """Quantises a step's rows k_new / v_new [B, gamma+1, Hkv, D] (bf16) into the E4M3 cache at ctx_lens with the
     scales in place; ctx_lens_out (None, another tensor, or ctx_lens itself) receives ctx_lens + gamma + 1."""
-    shape = _fp8_cache_shape(k_cache, v_cache, k_scale, v_scale)
-    rows = _new_rows(k_new, v_new, k_cache)
-    if k_new.shape[1] != gamma + 1:
+    cache, geometry = _cache8(k_cache, v_cache, k_scale, v_scale)
+    new, rows = _new_rows(k_new, v_new, cache)
+    if new[1] != gamma + 1:
         raise ValueError("k_new and v_new must be [B, gamma+1, Hkv, D]")
-    _lens(ctx_lens, shape.B, "ctx_lens")
-    _lens(ctx_lens_out, shape.B, "ctx_lens_out")
-    _check_device(k_new, v_new, k_cache, v_cache, k_scale, v_scale, ctx_lens, ctx_lens_out, status_word)
-    _check(load_library().rapid_kv_append_fp8(_p(k_new), _p(v_new), ctypes.byref(rows), _p(k_cache), _p(v_cache),
-                                              _p(k_scale), _p(v_scale), _p(ctx_lens), _p(ctx_lens_out), int(gamma),
-                                              ctypes.byref(shape), _p(status_word), _stream_ptr(stream)))
+    _lens(ctx_lens, cache[0], "ctx_lens")
+    _lens(ctx_lens_out, cache[0], "ctx_lens_out")
+    st = _here(stream, k_new, v_new, k_cache, v_cache, k_scale, v_scale, ctx_lens, ctx_lens_out, status_word)
+    _check(load_library().rapid_kv_append_fp8(
+        k_new.data_ptr(), v_new.data_ptr(), ctypes.byref(rows), k_cache.data_ptr(), v_cache.data_ptr(),
+        k_scale.data_ptr(), v_scale.data_ptr(), ctx_lens.data_ptr(), _addr(ctx_lens_out), gamma, ctypes.byref(geometry),
+        status_word.data_ptr(), st))
 
 
 def rapid_kv_read_fp8(k_cache, v_cache, k_scale, v_scale, ctx_lens, chunk_idx, chunk_tokens, k_out, v_out, out_lens,
                       status_word, stream=None) -> None:
     """Chunks of an E4M3 cache, one behind the other, into the bf16 cache k_out / v_out [B, Hkv, Lout, D].  chunk_idx
     [B, n] names them (-1: none), as rapid_retrieval_select returns them; None: all chunks the output has room for."""
-    shape = _fp8_cache_shape(k_cache, v_cache, k_scale, v_scale)
-    if k_out.dtype != torch.bfloat16 or v_out.dtype != torch.bfloat16:
+    cache, geometry = _cache8(k_cache, v_cache, k_scale, v_scale)
+    if not (k_out.dtype is v_out.dtype is _BF16):
         raise TypeError("k_out / v_out must be bfloat16")
-    if k_out.dim() != 4 or k_out.shape != v_out.shape or k_out.stride() != v_out.stride() or k_out.stride(3) != 1 \
-            or (k_out.shape[0], k_out.shape[1], k_out.shape[3]) != (shape.B, shape.Hkv, shape.D):
-        raise ValueError("k_out and v_out must be [B, Hkv, Lout, D] with equal strides and a contiguous head_dim")
-    _lens(ctx_lens, shape.B, "ctx_lens")
-    _lens(out_lens, shape.B, "out_lens")
+    shape, stride = _alike(k_out, v_out, "k_out and v_out")
+    out = _cache8_geometry(shape, stride)
+    if (shape[0], shape[1], shape[3]) != (cache[0], cache[1], cache[3]):
+        raise ValueError("k_out and v_out must be [B, Hkv, Lout, D] of the cache's batch, KV heads and head_dim")
+    _lens(ctx_lens, cache[0], "ctx_lens")
+    _lens(out_lens, cache[0], "out_lens")
     if chunk_tokens <= 0:
         raise ValueError("chunk_tokens must be positive")
     if chunk_idx is None:
-        n = -(-min(k_out.shape[2], shape.Lmax) // chunk_tokens)
+        n = -(-min(shape[2], cache[2]) // chunk_tokens)
     else:
-        if chunk_idx.dtype != torch.int32:
+        if chunk_idx.dtype is not _I32:
             raise TypeError("chunk_idx must be int32")
-        if chunk_idx.dim() != 2 or chunk_idx.shape[0] != shape.B or not chunk_idx.is_contiguous():
+        if chunk_idx.dim() != 2 or chunk_idx.shape[0] != cache[0] or not chunk_idx.is_contiguous():
             raise ValueError("chunk_idx must be dense [B, n_chunks]")
         n = chunk_idx.shape[1]
-    out = _AttnShape(shape.B, shape.Hkv, shape.Hkv, shape.D, k_out.shape[2], *_strides(k_out, 3))
-    _check_device(k_cache, v_cache, k_scale, v_scale, ctx_lens, chunk_idx, k_out, v_out, out_lens, status_word)
-    _check(load_library().rapid_kv_read_fp8(_p(k_cache), _p(v_cache), _p(k_scale), _p(v_scale), _p(ctx_lens),
-                                            ctypes.byref(shape), _p(chunk_idx), n, int(chunk_tokens), _p(k_out),
-                                            _p(v_out), ctypes.byref(out), _p(out_lens), _p(status_word),
-                                            _stream_ptr(stream)))
+    st = _here(stream, k_cache, v_cache, k_scale, v_scale, ctx_lens, chunk_idx, k_out, v_out, out_lens, status_word)
+    _check(load_library().rapid_kv_read_fp8(
+        k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), ctx_lens.data_ptr(),
+        ctypes.byref(geometry), _addr(chunk_idx), n, chunk_tokens, k_out.data_ptr(), v_out.data_ptr(), ctypes.byref(out),
+        out_lens.data_ptr(), status_word.data_ptr(), st))
 
 
 def rapid_step_commit(ctx_lens, accept_len, gamma, status_word, stream=None) -> None:
