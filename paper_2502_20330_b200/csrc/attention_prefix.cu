@@ -112,7 +112,8 @@ struct Plan {
 __device__ __forceinline__ int share_start(int total, int n, float r, int i) {
     return i >= n ? total : min(total, (int)((float)i * r));
 }
-// x / d for 0 <= x < 2^23 (a tile index of one sequence or one pass over the prefix, at most 2^31 / 128).
+// x / d for 0 <= x < 2^31 and a quotient below 2^16 (a KV head, a team): the approximate quotient, off by less than
+// 2^16 * 2^-21, is cut to within one of the true one.
 __device__ __forceinline__ int small_div(int x, int d) {
     int q = (int)__fdividef((float)x, (float)d);
     if (q * d > x) --q;
@@ -376,6 +377,19 @@ __device__ __noinline__ void scale_o(uint32_t tO, float factor) {
         tmem_st_x16(tO + 16 * i, o);
     }
     tmem_wait_st();
+}
+
+// Zeroes a row's probabilities in a block but for the first `keep`: exp2_poly leaves 2^-125 where the score is -inf,
+// and V there may be anything finite.  (In registers, before P is written, it costs every block: 150.4 us for 146.9.)
+__device__ __noinline__ void keep_p(uint32_t tS, int keep) {
+    uint32_t x[32];
+    tmem_wait_st();
+    tmem_ld_x32(tS, x);
+    tmem_wait_ld();
+#pragma unroll
+    for (int k = 0; k < 32; ++k)
+        if (2 * k + 1 >= keep) x[k] &= 2 * k >= keep ? 0u : 0xffffu;
+    tmem_st_x32(tS, x);
 }
 
 template <int D>
@@ -668,7 +682,7 @@ prefix_attn_split_kernel(const __grid_constant__ CUtensorMap tmKp, const __grid_
 #pragma unroll
                     for (int k = 0; k < kBlock; k += 2)
                         mx[(k >> 1) & 3] = max3(mx[(k >> 1) & 3], __uint_as_float(x[k]), __uint_as_float(x[k + 1]));
-                    const float top = ceilf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c);
+                    const float top = ceilf(max3(max3(mx[0], mx[1], mx[2]), mx[3], mx[3]) * c);
                     // no reference yet, or scores that outgrow it
                     const bool move = row_valid && !(top <= m_ref + kJump) && top != -INFINITY;
                     if (__any_sync(0xffffffffu, move)) {
@@ -702,6 +716,7 @@ prefix_attn_split_kernel(const __grid_constant__ CUtensorMap tmKp, const __grid_
                         pk[k >> 1] = pack_bf16x2(p0, p1);
                     }
                     tmem_st_x32(tS, pk);
+                    if (key0 + kBlock - 1 > all_see) keep_p(tS, lim - key0 + 1);
                     float s0, s1;
                     f32x2_split(f32x2_add(acc[0], acc[1]), s0, s1);
                     l_run += s0 + s1;
@@ -846,7 +861,7 @@ prefix_attn_merge_kernel(const __grid_constant__ PrefixArgs a, __nv_bfloat16* ou
         }
         float top = m;
 #pragma unroll
-        for (int u = 0; u < UN; ++u) top = fmaxf(top, ms[u]);
+        for (int u = 0; u < UN; ++u) top = max3(top, ms[u], ms[u]);
         const float keep = m == -INFINITY ? 0.f : exp2f(m - top);
         m = top;
         l *= keep;
@@ -877,7 +892,7 @@ prefix_attn_merge_kernel(const __grid_constant__ PrefixArgs a, __nv_bfloat16* ou
     if (row0 + row >= total_rows) return;
     float M = -INFINITY, L = 0.f;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) M = fmaxf(M, sh_m[k][row]);
+    for (int k = 0; k < 8; ++k) M = max3(M, sh_m[k][row], sh_m[k][row]);
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
