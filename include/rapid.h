@@ -650,7 +650,8 @@ int rapid_kv_append_fp8(const void* k_new, const void* v_new, const rapid_kv_row
  *   ctx_lens  : device int32 [B], tokens in the cache; out of [0, Lmax]: clamped, sets RAPID_STATUS_BAD_CTX_LEN
  *   chunk_idx : device int32 [B, n_chunks]: chunk i holds positions [i * chunk_tokens, (i+1) * chunk_tokens), as far
  *               as ctx_lens[b] reaches; -1 is no chunk; any other that holds nothing sets RAPID_STATUS_BAD_CTX_LEN.
- *               The same chunk may be named twice.  NULL: chunks 0 .. n_chunks - 1
+ *               The same chunk may be named twice; all together hold less than 2^31 tokens.  NULL: chunks
+ *               0 .. n_chunks - 1
  *   k_out, v_out, out_shape : device bf16 cache, geometry as in rapid_verify_attention; what would go beyond its
  *               Lmax is left out and sets RAPID_STATUS_BAD_CTX_LEN; rows behind the last written are left as they were
  *   out_lens  : device int32 [B], rows written per KV head

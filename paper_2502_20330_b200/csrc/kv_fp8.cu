@@ -617,6 +617,12 @@ int launch_kv_read_fp8(const void* k_cache, const void* v_cache, const float* k_
         set_error("%s: 2 * B * Hkv and n_chunks at most 65535, chunk_tokens * D below 2^31", who);
         return RAPID_ERR_UNSUPPORTED;
     }
+    // no chunk is longer than the cache; the rows of the chunks named are added up in 32 bits
+    const int64_t longest = chunk_tokens < s.Lmax ? chunk_tokens : s.Lmax;
+    if (chunk_idx && longest * n_chunks > 0x7fffffffLL) {
+        set_error("%s: the chunks named must hold less than 2^31 tokens", who);
+        return RAPID_ERR_UNSUPPORTED;
+    }
     a.k_scale = k_scale;
     a.v_scale = v_scale;
     a.ctx = ctx_lens;
@@ -634,8 +640,6 @@ int launch_kv_read_fp8(const void* k_cache, const void* v_cache, const float* k_
     a.D = s.D;
     a.n_chunks = n_chunks;
     a.chunk = chunk_tokens;
-    // no chunk is longer than the cache
-    const int64_t longest = chunk_tokens < s.Lmax ? chunk_tokens : s.Lmax;
     const int64_t per_block = (int64_t)kReadThreads * kReadUnroll;
     const int64_t blocks = (longest * (s.D / 16) + per_block - 1) / per_block;
     RAPID_CUDA_CHECK(launch_dependent(kv_read_fp8_kernel, dim3((unsigned)blocks, n_chunks, (unsigned)units), dim3(kReadThreads), 0,
