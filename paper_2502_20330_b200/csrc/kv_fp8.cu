@@ -34,18 +34,29 @@ struct Cache8 {
 };
 
 // 8 bf16 of a row -> 8 codes.  What lies beyond the largest code saturates, infinities included; NaN stays NaN.
-// POW2: the scale is a power of two and `inv` its reciprocal.
-template <bool POW2>
-__device__ __forceinline__ uint2 quantise8(const uint4& v, float scale, float inv, bool& clipped) {
+__device__ __forceinline__ uint2 quantise8(const uint4& v, float scale, bool& clipped) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
     uint32_t c[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        float lo = __uint_as_float(w[i] << 16), hi = __uint_as_float(w[i] & 0xffff0000u);
-        lo = POW2 ? lo * inv : __fdiv_rn(lo, scale);
-        hi = POW2 ? hi * inv : __fdiv_rn(hi, scale);
+        const float lo = __fdiv_rn(__uint_as_float(w[i] << 16), scale), hi = __fdiv_rn(__uint_as_float(w[i] & 0xffff0000u), scale);
         clipped |= fabsf(lo) > kE4m3Max || fabsf(hi) > kE4m3Max;
         c[i] = __nv_cvt_float2_to_fp8x2(make_float2(lo, hi), __NV_SATFINITE, __NV_E4M3);
+    }
+    return make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
+}
+// The same for a scale that is a power of two, `inv` its reciprocal (twice in 64 bits): two products an instruction.
+__device__ __forceinline__ uint2 quantise8_pow2(const uint4& v, uint64_t inv) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    uint32_t c[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint64_t x;
+        float2 y;
+        asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "r"(w[i] << 16), "r"(w[i] & 0xffff0000u));
+        asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(x) : "l"(inv));
+        asm("mov.b64 {%0, %1}, %2;" : "=f"(y.x), "=f"(y.y) : "l"(x));
+        c[i] = __nv_cvt_float2_to_fp8x2(y, __NV_SATFINITE, __NV_E4M3);
     }
     return make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
 }
@@ -76,7 +87,7 @@ __global__ void __launch_bounds__(128) kv_append_fp8_kernel(RowsIn in, Cache8 c,
     }
     if (!fits || i >= n) return;
     bool clipped = false;
-    const uint2 code = quantise8<false>(x, scale, 0.f, clipped);
+    const uint2 code = quantise8(x, scale, clipped);
     *reinterpret_cast<uint2*>((is_v ? c.v : c.k) + b * c.sb + h * c.sh + (L + t) * c.sl + d) = code;
     if (clipped) atomicOr(status, RAPID_STATUS_FP8_SATURATED);
 }
@@ -101,6 +112,7 @@ __device__ __forceinline__ int scale_exponent(uint32_t amax_bits, int headroom) 
     return max(-126, min(126, e));
 }
 __device__ __forceinline__ float pow2(int e) { return __int_as_float((e + 127) << 23); }
+__device__ __forceinline__ uint64_t pow2_twice(int e) { return (uint64_t)((uint32_t)(e + 127) << 23) * 0x100000001ull; }
 
 // Running maximum of |x| over pairs of bf16 (a NaN takes no part).
 __device__ __forceinline__ __nv_bfloat162 absmax(__nv_bfloat162 m, const uint4& v) {
@@ -123,10 +135,7 @@ struct FillArgs {
     int32_t* ctx_out;
     int32_t* status;
     int B, Hkv, D, T, headroom;
-    int row_shift;  // log2 of a row's chunks of 8 elements, or -1 if that is no power of two
 };
-
-__device__ __forceinline__ int row_of(int chunk, int per_row, int shift) { return shift >= 0 ? chunk >> shift : chunk / per_row; }
 
 // Rows of sequence b, or -1 if it cannot be written.
 __device__ __forceinline__ int fill_rows(const FillArgs& a, int b) {
@@ -134,8 +143,10 @@ __device__ __forceinline__ int fill_rows(const FillArgs& a, int b) {
     return n < 0 || n > a.T || n > a.c.Lmax ? -1 : n;
 }
 // What one block per (sequence, K or V, KV head) writes besides the codes.
-__device__ __forceinline__ void fill_scalars(const FillArgs& a, int b, bool is_v, int h, int n, float scale) {
+// (With such a scale nothing but an infinity saturates.)
+__device__ __forceinline__ void fill_scalars(const FillArgs& a, int b, bool is_v, int h, int n, uint32_t amax, float scale) {
     if (n >= 0) (is_v ? a.v_scale : a.k_scale)[b * a.Hkv + h] = scale;
+    if (amax > 0x7f7fu) atomicOr(a.status, RAPID_STATUS_FP8_SATURATED);
     if (!is_v && h == 0) {
         if (n < 0) atomicOr(a.status, RAPID_STATUS_BAD_CTX_LEN);
         else if (a.ctx_out) a.ctx_out[b] = n;
@@ -144,38 +155,33 @@ __device__ __forceinline__ void fill_scalars(const FillArgs& a, int b, bool is_v
 
 // Short prompts: one cluster per (sequence, K or V, KV head) holds all of its rows in registers, so they are read
 // once: loads, the largest magnitude over block and cluster (a word of each CTA's shared memory that its peers
-// push to), codes.  CTA r of the cluster takes chunks r * 256 * N .. ; a chunk is 8 elements.
+// push to), codes.  A thread goes down one column of chunks of 8 elements (see kv_fill_kernel), N rows `down` apart;
+// CTA r of the cluster takes rows r * down * N .. .
 constexpr int kFillThreads = 256;
 constexpr int kFillCluster = 8;
 constexpr int kFillResident = 4;  // blocks of the two-pass kernel on an SM
-constexpr int kFillLag = 2;       // its groups between maxima and codes
+constexpr int kFillLag = 1;       // its groups between maxima and codes
 
-template <int N>
-__global__ void __launch_bounds__(kFillThreads) kv_fill_cluster_kernel(const FillArgs a) {
+template <int N, int THREADS>
+__global__ void __launch_bounds__(THREADS) kv_fill_cluster_kernel(const FillArgs a) {
     __shared__ uint32_t peers[kFillCluster];
-    __shared__ uint32_t warps[kFillThreads / 32];
+    __shared__ uint32_t warps[THREADS / 32];
     const int rank = blockIdx.x, unit = blockIdx.y;  // (grid x = cluster)
     const int h = unit % a.Hkv, rest = unit / a.Hkv;
     const bool is_v = rest & 1;
     const int b = rest >> 1;
-    const int per_row = a.D / 8;
+    const int per_row = a.D / 8, down = THREADS / per_row, my = threadIdx.x / per_row;
     asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");  // (a peer's shared memory is written to once it runs)
     griddep_wait();
     griddep_launch_dependents();
     const int n = fill_rows(a, b);
-    const int chunks = max(n, 0) * per_row;
-    const __nv_bfloat16* src = (is_v ? a.in.v : a.in.k) + b * a.in.sb + h * a.in.sh;
-    const int first = rank * kFillThreads * N + threadIdx.x;
+    const int row0 = my < down ? rank * down * N + my : a.T, col = (threadIdx.x - my * per_row) * 8;
+    const __nv_bfloat16* src = (is_v ? a.in.v : a.in.k) + b * a.in.sb + h * a.in.sh + row0 * a.in.st + col;
     uint4 x[N];
-    int row[N], col[N];
     __nv_bfloat162 m = __float2bfloat162_rn(0.f);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int ch = first + i * kFillThreads;
-        row[i] = row_of(ch, per_row, a.row_shift);
-        col[i] = (ch - row[i] * per_row) * 8;
-        x[i] = ch < chunks ? __ldg(reinterpret_cast<const uint4*>(src + row[i] * a.in.st + col[i])) : make_uint4(0, 0, 0, 0);
-    }
+    for (int i = 0; i < N; ++i)
+        x[i] = row0 + i * down < n ? __ldg(reinterpret_cast<const uint4*>(src + i * (down * a.in.st))) : make_uint4(0, 0, 0, 0);
 #pragma unroll
     for (int i = 0; i < N; ++i) m = absmax(m, x[i]);
     uint32_t top = __reduce_max_sync(0xffffffffu, absmax_bits(m));
@@ -184,7 +190,7 @@ __global__ void __launch_bounds__(kFillThreads) kv_fill_cluster_kernel(const Fil
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     if (threadIdx.x < kFillCluster) {  // thread p pushes the block's value to CTA p of the cluster
 #pragma unroll
-        for (int w = 0; w < kFillThreads / 32; ++w) top = max(top, warps[w]);
+        for (int w = 0; w < THREADS / 32; ++w) top = max(top, warps[w]);
         uint32_t there;
         asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(smem_u32(&peers[rank])), "r"((int)threadIdx.x));
         asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(there), "r"(top) : "memory");
@@ -194,30 +200,29 @@ __global__ void __launch_bounds__(kFillThreads) kv_fill_cluster_kernel(const Fil
 #pragma unroll
     for (int p = 0; p < kFillCluster; ++p) top = max(top, peers[p]);
     const int e = scale_exponent(top, a.headroom);
-    if (rank == 0 && threadIdx.x == 0) fill_scalars(a, b, is_v, h, n, pow2(e));
-    const float inv = pow2(-e);
-    bool clipped = false;
-    uint8_t* dst = (is_v ? a.c.v : a.c.k) + b * a.c.sb + h * a.c.sh;
+    if (rank == 0 && threadIdx.x == 0) fill_scalars(a, b, is_v, h, n, top, pow2(e));
+    const uint64_t inv = pow2_twice(-e);
+    uint8_t* dst = (is_v ? a.c.v : a.c.k) + b * a.c.sb + h * a.c.sh + row0 * a.c.sl + col;
 #pragma unroll
     for (int i = 0; i < N; ++i)
-        if (first + i * kFillThreads < chunks)
-            *reinterpret_cast<uint2*>(dst + row[i] * a.c.sl + col[i]) = quantise8<true>(x[i], 0.f, inv, clipped);
-    if (clipped) atomicOr(a.status, RAPID_STATUS_FP8_SATURATED);
+        if (row0 + i * down < n) *reinterpret_cast<uint2*>(dst + i * (down * a.c.sl)) = quantise8_pow2(x[i], inv);
 }
 
 // Long prompts: the rows do not fit on chip, so they are read twice, the second time out of L2.  The units
 // (sequence, K or V, KV head) are worked off in groups that L2 holds; work items are handed out by a ticket counter:
-// in step s the maxima of group s and the codes of group s - 2, alternating.  An item that writes codes waits until
+// in step s the maxima of group s and the codes of group s - 1, alternating.  An item that writes codes waits until
 // the maxima of its group are in: those items were all handed out before it, each to a block that had finished all
 // it held, so the wait ends whatever the number of blocks that run at a time (and it is bounded).  That is also why
 // no ticket is taken ahead: a block that holds a maximum while it waits for others stalls them (285 us for 8 heads
-// of 131,072 rows of 128, K and V; 229 without).  Items of 128 KB rather than 64, and four loads a thread in flight
-// with 32 warps an SM rather than eight with fewer: 212; a lag of two groups rather than one, 208.  The same block
-// for both passes over an item: 211.  The maxima alone take 98 us, the codes alone 140; DRAM carries each row once
-// (640 MB read, 264 written), and what the second pass waits for is L2.
+// of 131,072 rows of 128, K and V; 229 without).
+//   The rest of the way from there to 172: four 16-byte loads a thread in flight with 32 warps an SM rather than
+// eight with fewer (212), a lag of one group; a thread that goes down one column, so that a load costs one
+// addition, and products in pairs (178); as many items as make one step one wave of the grid, rather than items of
+// 128 KB.  The same block for both passes over an item gained nothing.  DRAM carries each row once; what
+// is left over the 123 us that takes is the second pass's share of L2 and the waves' ends.
 struct FillPlan {
-    int group_heads, groups;   // KV heads of a group, groups in all
-    int item_rows, items;      // rows of an item, items of a group (item = row chunk * group_heads + head)
+    int group_units, groups;   // units of a group, groups in all
+    int item_rows, items;      // rows of an item, items of a group (item = row chunk * group_units + unit)
     uint32_t* words;           // ticket, then per group the count of finished maxima items, then per unit the maximum
 };
 __device__ __forceinline__ uint32_t ld_acquire(const uint32_t* p) {
@@ -239,12 +244,15 @@ __global__ void __launch_bounds__(kFillThreads, kFillResident) kv_fill_kernel(co
     uint32_t* ticket = p.words;
     uint32_t* done = p.words + 1;
     uint32_t* amax = done + p.groups;
+    // A thread goes down a column of chunks of 8 elements, `down` rows at a step; threads that make no whole row are
+    // idle (they begin behind the last row), and rows wider than the block have several columns for each.
     const int per_row = a.D / 8;
-    const int groups_per = (a.Hkv + p.group_heads - 1) / p.group_heads;  // groups of a (sequence, K or V)
+    const int down = max(1, kFillThreads / per_row), my = threadIdx.x / per_row;
+    const int my_col = threadIdx.x - my * per_row, my_row = my < down ? my : p.item_rows;
+    const long long in_step = down * a.in.st, out_step = down * a.c.sl;
     const uint32_t total = (uint32_t)(p.groups + kFillLag) * 2u * p.items;
     griddep_wait();
     griddep_launch_dependents();
-    bool clipped = false;
     for (;;) {
         if (threadIdx.x == 0) sh_ticket = atomicAdd(ticket, 1u);
         __syncthreads();
@@ -253,30 +261,27 @@ __global__ void __launch_bounds__(kFillThreads, kFillResident) kv_fill_kernel(co
         const uint32_t step = tk / (2u * p.items), r = tk - step * 2u * p.items;
         const bool codes = r & 1;
         const int group = (int)step - (codes ? kFillLag : 0), item = (int)(r >> 1);
-        const int rest = group < 0 ? 0 : group / groups_per;
+        const int chunk = item / p.group_units, unit = group * p.group_units + item - chunk * p.group_units;
+        const bool work = group >= 0 && unit < 2 * a.B * a.Hkv;
+        const int rest = work ? unit / a.Hkv : 0, h = work ? unit - rest * a.Hkv : 0;
         const bool is_v = rest & 1;
         const int b = rest >> 1;
-        const int chunk = item / p.group_heads;
-        const int h = (group - rest * groups_per) * p.group_heads + item - chunk * p.group_heads;
-        const bool work = group >= 0 && group < p.groups && h < a.Hkv;
         const int n = work ? fill_rows(a, b) : -1;
         const int row0 = chunk * p.item_rows, rows = min(p.item_rows, max(n, 0) - row0);
-        const int unit = rest * a.Hkv + h;
         const __nv_bfloat16* src = (is_v ? a.in.v : a.in.k) + b * a.in.sb + h * a.in.sh;
         if (!codes) {
             if (rows > 0) {
                 __nv_bfloat162 m = __float2bfloat162_rn(0.f);
-                const int chunks = rows * per_row;
-                for (int i0 = threadIdx.x; i0 < chunks; i0 += kFillThreads * UN) {
-                    uint4 x[UN];
+                for (int col = my_col; col < per_row; col += kFillThreads) {
+                    const __nv_bfloat16* at = src + (long long)(row0 + my_row) * a.in.st + col * 8;
+                    for (int r = my_row; r < rows; r += down * UN, at += UN * in_step) {
+                        uint4 x[UN];
 #pragma unroll
-                    for (int u = 0; u < UN; ++u) {
-                        const int i = i0 + u * kFillThreads, row = row_of(i, per_row, a.row_shift);
-                        x[u] = i < chunks ? __ldg(reinterpret_cast<const uint4*>(src + (row0 + row) * a.in.st + (i - row * per_row) * 8))
-                                          : make_uint4(0, 0, 0, 0);
+                        for (int u = 0; u < UN; ++u)
+                            x[u] = r + u * down < rows ? __ldg(reinterpret_cast<const uint4*>(at + u * in_step)) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                        for (int u = 0; u < UN; ++u) m = absmax(m, x[u]);
                     }
-#pragma unroll
-                    for (int u = 0; u < UN; ++u) m = absmax(m, x[u]);
                 }
                 const uint32_t top = __reduce_max_sync(0xffffffffu, absmax_bits(m));
                 if ((threadIdx.x & 31) == 0) warps[threadIdx.x >> 5] = top;
@@ -309,32 +314,26 @@ __global__ void __launch_bounds__(kFillThreads, kFillResident) kv_fill_kernel(co
             __syncthreads();
             if (work && sh_amax <= 0xffffu) {
                 const int e = scale_exponent(sh_amax, a.headroom);
-                if (chunk == 0 && threadIdx.x == 0) fill_scalars(a, b, is_v, h, n, pow2(e));
-                if (rows > 0) {
-                    const float inv = pow2(-e);
-                    uint8_t* dst = (is_v ? a.c.v : a.c.k) + b * a.c.sb + h * a.c.sh;
-                    const int chunks = rows * per_row;
-                    for (int i0 = threadIdx.x; i0 < chunks; i0 += kFillThreads * UN) {
+                if (chunk == 0 && threadIdx.x == 0) fill_scalars(a, b, is_v, h, n, sh_amax, pow2(e));
+                const uint64_t inv = pow2_twice(-e);
+                uint8_t* dst = (is_v ? a.c.v : a.c.k) + b * a.c.sb + h * a.c.sh;
+                for (int col = my_col; col < per_row; col += kFillThreads) {
+                    const __nv_bfloat16* at = src + (long long)(row0 + my_row) * a.in.st + col * 8;
+                    uint8_t* to = dst + (long long)(row0 + my_row) * a.c.sl + col * 8;
+                    for (int r = my_row; r < rows; r += down * UN, at += UN * in_step, to += UN * out_step) {
                         uint4 x[UN];
 #pragma unroll
-                        for (int u = 0; u < UN; ++u) {
-                            const int i = i0 + u * kFillThreads, row = row_of(i, per_row, a.row_shift);
-                            if (i < chunks) x[u] = __ldcs(reinterpret_cast<const uint4*>(src + (row0 + row) * a.in.st + (i - row * per_row) * 8));
-                        }
+                        for (int u = 0; u < UN; ++u)
+                            if (r + u * down < rows) x[u] = __ldcs(reinterpret_cast<const uint4*>(at + u * in_step));
 #pragma unroll
-                        for (int u = 0; u < UN; ++u) {
-                            const int i = i0 + u * kFillThreads, row = row_of(i, per_row, a.row_shift);
-                            if (i < chunks)
-                                __stcs(reinterpret_cast<uint2*>(dst + (row0 + row) * a.c.sl + (i - row * per_row) * 8),
-                                       quantise8<true>(x[u], 0.f, inv, clipped));
-                        }
+                        for (int u = 0; u < UN; ++u)
+                            if (r + u * down < rows) __stcs(reinterpret_cast<uint2*>(to + u * out_step), quantise8_pow2(x[u], inv));
                     }
                 }
             }
         }
         __syncthreads();  // (warps, sh_amax and sh_ticket are free again)
     }
-    if (clipped) atomicOr(a.status, RAPID_STATUS_FP8_SATURATED);
 }
 
 // ---- read back --------------------------------------------------------------------------------------------------
@@ -543,15 +542,15 @@ int launch_kv_fill_fp8(const void* k_new, const void* v_new, const rapid_kv_rows
     a.D = s.D;
     a.T = T;
     a.headroom = headroom;
-    a.row_shift = -1;
-    for (int i = 0; i < 16; ++i)
-        if (s.D == 8 << i) a.row_shift = i;
-    const int64_t chunks = (int64_t)T * (s.D / 8);
-    const int64_t per_n = (int64_t)kFillThreads * kFillCluster;
-    if (chunks <= 8 * per_n) {
+    // Rows that a cluster holds with one a thread.  Eight a thread of 512, 2,048 rows of 128, are the most that is faster
+    // than two passes (8 heads: 5.5 us for 8.7, and 49.7 for 53.8 at 16 sequences; with 16 a thread 14.4 for 12.7 at
+    // 4,096 rows).  Six a thread rather than eight where they do: 4.0 us for 4.8 at 1,100 rows.
+    const int per_row = s.D / 8;
+    const int64_t rows_256 = (int64_t)kFillCluster * (256 / per_row), rows_512 = (int64_t)kFillCluster * (512 / per_row);
+    if (T <= 8 * rows_512) {
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(kFillCluster, (unsigned)units);
-        cfg.blockDim = dim3(kFillThreads);
+        cfg.blockDim = dim3(T <= 8 * rows_256 ? 256 : 512);
         cfg.stream = stream;
         cudaLaunchAttribute attr[2];
         attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -561,30 +560,38 @@ int launch_kv_fill_fp8(const void* k_new, const void* v_new, const rapid_kv_rows
         attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
         cfg.attrs = attr;
         cfg.numAttrs = 2;
-        if (chunks <= per_n) RAPID_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kv_fill_cluster_kernel<1>, a));
-        else if (chunks <= 2 * per_n) RAPID_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kv_fill_cluster_kernel<2>, a));
-        else if (chunks <= 4 * per_n) RAPID_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kv_fill_cluster_kernel<4>, a));
-        else RAPID_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kv_fill_cluster_kernel<8>, a));
+        if (T <= rows_256) RAPID_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kv_fill_cluster_kernel<1, 256>, a));
+        else if (T <= 2 * rows_256) RAPID_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kv_fill_cluster_kernel<2, 256>, a));
+        else if (T <= 4 * rows_256) RAPID_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kv_fill_cluster_kernel<4, 256>, a));
+        else if (T <= 8 * rows_256) RAPID_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kv_fill_cluster_kernel<8, 256>, a));
+        else if (T <= 6 * rows_512) RAPID_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kv_fill_cluster_kernel<6, 512>, a));
+        else RAPID_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kv_fill_cluster_kernel<8, 512>, a));
         count_launch(1);
         return RAPID_OK;
     }
-    constexpr int64_t kGroupBytes = 32 << 20, kItemBytes = 128 << 10;
+    int dev = 0, sms = 0;
+    RAPID_CUDA_CHECK(cudaGetDevice(&dev));
+    RAPID_CUDA_CHECK(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+    const int grid = sms * kFillResident;
+    // Groups of equal size of at most 32 MB (or one unit): with the group before it, half of L2.  A step's items,
+    // the maxima of a group and the codes of another, are one wave of the grid.
+    constexpr int64_t kGroupBytes = 32 << 20;
     FillPlan p;
     const int64_t unit_bytes = (int64_t)T * s.D * 2;
-    p.group_heads = (int)(kGroupBytes / unit_bytes < 1 ? 1 : kGroupBytes / unit_bytes > s.Hkv ? s.Hkv : kGroupBytes / unit_bytes);
-    p.groups = 2 * s.B * ((s.Hkv + p.group_heads - 1) / p.group_heads);
-    p.item_rows = (int)(kItemBytes / (s.D * 2) > 0 ? kItemBytes / (s.D * 2) : 1);
-    p.items = (T + p.item_rows - 1) / p.item_rows * p.group_heads;
+    const int64_t most = kGroupBytes / unit_bytes < 1 ? 1 : kGroupBytes / unit_bytes;
+    p.groups = (int)((units + most - 1) / most);
+    p.group_units = (int)((units + p.groups - 1) / p.groups);
+    p.groups = (int)((units + p.group_units - 1) / p.group_units);
+    const int chunks_of_unit = grid / 2 / p.group_units > 1 ? grid / 2 / p.group_units : 1;
+    p.item_rows = (T + chunks_of_unit - 1) / chunks_of_unit;
+    p.items = (T + p.item_rows - 1) / p.item_rows * p.group_units;
     if (((int64_t)p.groups + kFillLag) * 2 * p.items > 0x7fffffffLL) {
         set_error("%s: too many rows in one call", who);
         return RAPID_ERR_UNSUPPORTED;
     }
     p.words = reinterpret_cast<uint32_t*>(ws + kWorkspaceHeaderBytes);
-    int dev = 0, sms = 0;
-    RAPID_CUDA_CHECK(cudaGetDevice(&dev));
-    RAPID_CUDA_CHECK(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
     RAPID_CUDA_CHECK(launch_dependent(kv_fill_clear_kernel, dim3(1), dim3(256), 0, stream, p.words, (int)(1 + p.groups + units)));
-    RAPID_CUDA_CHECK(launch_dependent(kv_fill_kernel<4>, dim3(sms * kFillResident), dim3(kFillThreads), 0, stream, a, p));
+    RAPID_CUDA_CHECK(launch_dependent(kv_fill_kernel<4>, dim3(grid), dim3(kFillThreads), 0, stream, a, p));
     count_launch(2);
     return RAPID_OK;
 }

@@ -254,3 +254,38 @@ def test_fills_at_a_time_on_workspaces_of_their_own():
     for i, g in enumerate(got):
         assert all(torch.equal(a, b) for a, b in zip(g, want[i % 2]))
     assert all(R.workspace_status(ws) == 0 for ws in wss)
+
+
+@pytest.mark.parametrize("B,T,Hkv,D,counts", [
+    (1, 1024, 2, 128, None), (2, 1025, 2, 128, (1025, 1024)),    # the last rows and the first of each number of rows a thread
+    (2, 1536, 1, 128, (1536, 1)), (1, 1537, 2, 128, None),
+    (2, 2048, 2, 128, (2048, 2041)), (2, 2049, 1, 128, (2049, 0)),  # the last that is read once, the first that is read twice
+    (3, 333, 2, 80, (333, 25, 0)), (2, 6000, 2, 80, (6000, 5999)),  # ten threads to a row: some have none
+    (1, 700, 3, 48, None),
+    (1, 9, 1, 2048, None), (1, 300, 1, 2048, None),              # a row as wide as a block
+    (2, 40, 1, 4112, (40, 3)),                                   # wider
+    (40, 2300, 1, 64, tuple(57 * i for i in range(40))),         # groups of several sequences
+    (3, 20000, 3, 128, (20000, 1, 12345)),                       # groups that end inside a sequence
+])
+def test_fills_at_the_sizes_where_the_form_changes(B, T, Hkv, D, counts):
+    """Codes and scales from their definition in 64 bits (x / scale is exact there, and so is torch's rounding to E4M3)."""
+    import paper_2502_20330_b200 as R
+    xs = [_rnd(B, T, Hkv, D, seed=200 + i) * torch.logspace(-3, 3, Hkv, device="cuda").bfloat16()[:, None] for i in range(2)]
+    n = None if counts is None else _lens(*counts)
+    cache = [torch.full((B, Hkv, T + 3, D), 77, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    scales = [torch.full((B, Hkv), -1.0, device="cuda") for _ in range(2)]
+    ctx = _lens(*[-5] * B)
+    ws = R.new_workspace(R.kv_fill_workspace_bytes(B, Hkv))
+    R.rapid_kv_fill_fp8(*xs, n, *cache, *scales, ctx, ws)
+    assert R.workspace_status(ws) == 0
+    counts = counts or (T,) * B
+    assert ctx.tolist() == list(counts)
+    for x, c, s in zip(xs, cache, scales):
+        for b, rows in enumerate(counts):
+            head = x[b, :rows].transpose(0, 1).double()                             # [Hkv, rows, D]
+            top = head.abs().amax((1, 2)) if rows else torch.zeros(Hkv, dtype=torch.float64, device="cuda")
+            want = torch.where(top > 0, torch.exp2(torch.ceil(torch.log2(top / 448))), torch.ones_like(top))
+            assert torch.equal(s[b].double(), want)
+            codes = (head / want[:, None, None]).float().to(torch.float8_e4m3fn).view(torch.uint8)
+            assert torch.equal(c[b, :, :rows], codes)
+            assert (c[b, :, rows:] == 77).all()
