@@ -337,9 +337,11 @@ __global__ void __launch_bounds__(kFillThreads, kFillResident) kv_fill_kernel(co
 }
 
 // ---- read back --------------------------------------------------------------------------------------------------
-// Chunks of the cache into a bf16 cache, one behind the other.  A block takes 16 KB of codes of one (sequence, K or
+// Chunks of the cache into a bf16 cache, one behind the other.  A block takes 8 KB of codes of one (sequence, K or
 // V, KV head, chunk); where its rows go depends on the chunks before (a partial one is shorter, -1 is none), which
-// the block adds up while its codes are on their way.
+// the block adds up while its codes are on their way.  Bound by HBM: 131,072 rows of 8 heads of 128, K and V, in 104 us,
+// ten chunks of 512 in 7.1 (119 and 8.7 with 16 codes a thread, whose two stores fill a sector by halves; 106 and
+// 7.2 with blocks of 256 threads).
 struct ReadArgs {
     Cache8 c;
     const float* k_scale;
@@ -352,9 +354,10 @@ struct ReadArgs {
     int32_t* status;
     long long ob, oh, ol, Lout;  // strides of the output, its capacity
     int B, Hkv, D, n_chunks, chunk;
+    int wide;  // blocks that share a row: 1, or more where it is wider than one
 };
-constexpr int kReadThreads = 256;
-constexpr int kReadUnroll = 4;  // 16-byte loads in flight per thread
+constexpr int kReadThreads = 128;
+constexpr int kReadUnroll = 8;  // 8-byte loads in flight per thread
 
 // Rows that chunk number i of sequence b holds.
 __device__ __forceinline__ int chunk_rows(const ReadArgs& a, int ctx, int i) {
@@ -369,25 +372,22 @@ __global__ void __launch_bounds__(kReadThreads) kv_read_fp8_kernel(const ReadArg
     const int h = blockIdx.z % a.Hkv, rest = blockIdx.z / a.Hkv;
     const bool is_v = rest & 1;
     const int b = rest >> 1;
-    const int per_row = a.D / 16;
+    // A thread goes down one column of 8 codes, so that a warp's stores of 16 bytes a lane lie side by side.
+    const int per_row = a.D / 8, down = max(1, kReadThreads / per_row), my = threadIdx.x / per_row;
+    const int block = blockIdx.x / a.wide, part = blockIdx.x - block * a.wide;
+    const int my_col = (part * kReadThreads + threadIdx.x - my * per_row) * 8, row0 = block * (down * kReadUnroll) + my;
     griddep_wait();
     griddep_launch_dependents();
     const int given = a.ctx[b];
     const int ctx = (int)max(0LL, min((long long)given, a.c.Lmax));
     const int number = a.idx ? a.idx[(size_t)b * a.n_chunks + j] : j;
     const int rows = chunk_rows(a, ctx, number);
-    const int first = blockIdx.x * kReadThreads * kReadUnroll + threadIdx.x;
-    const uint8_t* src = (is_v ? a.c.v : a.c.k) + b * a.c.sb + h * a.c.sh;
-    uint4 x[kReadUnroll];
-    int row[kReadUnroll], col[kReadUnroll];
+    const int end = my < down && my_col < a.D ? rows : 0;  // (threads that make no whole row are idle)
+    const uint8_t* src = (is_v ? a.c.v : a.c.k) + b * a.c.sb + h * a.c.sh + ((long long)number * a.chunk + row0) * a.c.sl + my_col;
+    uint2 x[kReadUnroll];
 #pragma unroll
-    for (int u = 0; u < kReadUnroll; ++u) {
-        const int i = first + u * kReadThreads;
-        row[u] = i / per_row;
-        col[u] = (i - row[u] * per_row) * 16;
-        if (row[u] < rows)
-            x[u] = __ldcs(reinterpret_cast<const uint4*>(src + ((long long)number * a.chunk + row[u]) * a.c.sl + col[u]));
-    }
+    for (int u = 0; u < kReadUnroll; ++u)
+        if (row0 + u * down < end) x[u] = __ldcs(reinterpret_cast<const uint2*>(src + u * (down * a.c.sl)));
     const float scale = (is_v ? a.v_scale : a.k_scale)[b * a.Hkv + h];
     // the rows before this chunk's
     long long before = 0;
@@ -411,22 +411,18 @@ __global__ void __launch_bounds__(kReadThreads) kv_read_fp8_kernel(const ReadArg
         if (blockIdx.x == 0 && h == 0 && !is_v && (number < -1 || (number >= 0 && rows == 0 && a.idx) || before + rows > a.Lout))
             atomicOr(a.status, RAPID_STATUS_BAD_CTX_LEN);
     }
-    __nv_bfloat16* dst = (is_v ? a.v_out : a.k_out) + b * a.ob + h * a.oh;
+    __nv_bfloat16* dst = (is_v ? a.v_out : a.k_out) + b * a.ob + h * a.oh + (before + row0) * a.ol + my_col;
 #pragma unroll
     for (int u = 0; u < kReadUnroll; ++u) {
-        const long long to = before + row[u];
-        if (row[u] >= rows || to >= a.Lout) continue;
-        const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
-        uint32_t o[8];
+        if (row0 + u * down >= end || before + row0 + u * down >= a.Lout) continue;
+        uint32_t o[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const __half2_raw r = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[i >> 1] >> (16 * (i & 1))), __NV_E4M3);
+        for (int i = 0; i < 4; ++i) {
+            const __half2_raw r = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)((i & 2 ? x[u].y : x[u].x) >> (16 * (i & 1))), __NV_E4M3);
             const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&r));
             o[i] = pack_bf16x2(f.x * scale, f.y * scale);
         }
-        uint4* out = reinterpret_cast<uint4*>(dst + to * a.ol + col[u]);
-        __stcs(out, make_uint4(o[0], o[1], o[2], o[3]));
-        __stcs(out + 1, make_uint4(o[4], o[5], o[6], o[7]));
+        __stcs(reinterpret_cast<uint4*>(dst + u * (down * a.ol)), make_uint4(o[0], o[1], o[2], o[3]));
     }
 }
 
@@ -647,8 +643,9 @@ int launch_kv_read_fp8(const void* k_cache, const void* v_cache, const float* k_
     a.D = s.D;
     a.n_chunks = n_chunks;
     a.chunk = chunk_tokens;
-    const int64_t per_block = (int64_t)kReadThreads * kReadUnroll;
-    const int64_t blocks = (longest * (s.D / 16) + per_block - 1) / per_block;
+    a.wide = (s.D / 8 + kReadThreads - 1) / kReadThreads;
+    const int64_t rows_of_block = kReadUnroll * (a.wide > 1 ? 1 : kReadThreads / (s.D / 8));
+    const int64_t blocks = (longest + rows_of_block - 1) / rows_of_block * a.wide;
     RAPID_CUDA_CHECK(launch_dependent(kv_read_fp8_kernel, dim3((unsigned)blocks, n_chunks, (unsigned)units), dim3(kReadThreads), 0,
                                       stream, a));
     count_launch(1);

@@ -289,3 +289,22 @@ def test_fills_at_the_sizes_where_the_form_changes(B, T, Hkv, D, counts):
             codes = (head / want[:, None, None]).float().to(torch.float8_e4m3fn).view(torch.uint8)
             assert torch.equal(c[b, :, :rows], codes)
             assert (c[b, :, rows:] == 77).all()
+
+
+@pytest.mark.parametrize("D", [16, 48, 80, 2048, 2064, 4112])
+def test_reading_rows_of_odd_widths(D):
+    import paper_2502_20330_b200 as R
+    B, Hkv, L, chunk = 2, 2, 150, 32
+    codes = [torch.randint(0, 120, (B, Hkv, L, D), dtype=torch.uint8, device="cuda") for _ in range(2)]   # no NaN code
+    scales = [torch.rand(B, Hkv, device="cuda") + 0.5 for _ in range(2)]
+    ctx, idx = _lens(150, 70), _lens(4, 0, -1, 1, 2, 0, 0, 0).view(2, 4)
+    out = [torch.full((B, Hkv, 130, D), 3.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    n, word = _lens(0, 0), torch.zeros(1, dtype=torch.int32, device="cuda")
+    R.rapid_kv_read_fp8(*codes, *scales, ctx, idx, chunk, *out, n, word)
+    assert n.tolist() == [22 + 32 + 32, 6 + 96] and word.item() == 0
+    rows = [[r for c in cs if c >= 0 for r in range(c * chunk, min(m, (c + 1) * chunk))] for cs, m in zip(idx.tolist(), (150, 70))]
+    for c, s, o in zip(codes, scales, out):
+        for b in range(B):
+            x = c[b, :, rows[b]].view(torch.float8_e4m3fn).float() * s[b][:, None, None]
+            assert torch.equal(o[b, :, :len(rows[b])], x.bfloat16())
+            assert (o[b, :, len(rows[b]):] == 3).all()
