@@ -4,6 +4,7 @@
 #include <string.h>
 
 #include "common.cuh"
+#include "prefix_kv8.cuh"
 
 namespace rapid {
 

@@ -38,6 +38,7 @@
 #include <math.h>
 
 #include "common.cuh"
+#include "prefix_kv8.cuh"
 #include "tcgen05.cuh"
 
 namespace rapid {

@@ -51,7 +51,7 @@ inline cudaError_t launch_dependent(void (*kernel)(KArgs...), dim3 grid, dim3 bl
 }
 #endif
 
-// internal launchers shared by the entry points (defined in attention.cu / attention_prefix.cu / kv_fp8.cu / accept.cu / retrieval.cu)
+// internal launchers shared by the entry points (defined in attention.cu / accept.cu)
 int launch_verify_attention(const void* q, const void* k_cache, const void* v_cache,
                             const int32_t* ctx_lens, int gamma, void* out,
                             const rapid_attn_shape* shape, const rapid_attn_params* params,
@@ -71,25 +71,6 @@ int launch_retrieval_select(const float* chunk_emb, const float* query_emb, cons
                             int32_t* sel_count, int32_t* status_word, cudaStream_t stream);
 int launch_merge_partials(const float* o_parts, const float* lse_parts, int P, int64_t rows, int D, void* out,
                           float* out_f32, float* lse_out, cudaStream_t stream);
-size_t prefix_attention_workspace_bytes(const rapid_attn_shape* s, int gamma);
-// paged == nullptr: prefix K/V apart from the own caches; else both in the pools k_cache / v_cache
-int launch_verify_attention_prefix(const void* q, const void* k_prefix, const void* v_prefix,
-                                   const rapid_prefix_kv* prefix, const int32_t* prefix_len, const void* k_cache,
-                                   const void* v_cache, const rapid_paged_kv* paged, const int32_t* block_table,
-                                   const int32_t* ctx_lens, int gamma, void* out, const rapid_attn_shape* shape,
-                                   const rapid_attn_params* params, void* workspace, size_t workspace_bytes,
-                                   cudaStream_t stream);
-size_t kv_fill_workspace_bytes(int B, int Hkv);
-int launch_kv_fill_fp8(const void* k_new, const void* v_new, const rapid_kv_rows* rows, int T, const int32_t* n_tokens,
-                       void* k_cache, void* v_cache, float* k_scale, float* v_scale, int32_t* ctx_lens_out, int headroom,
-                       const rapid_attn_shape* shape, void* workspace, size_t workspace_bytes, cudaStream_t stream);
-int launch_kv_append_fp8(const void* k_new, const void* v_new, const rapid_kv_rows* rows, void* k_cache, void* v_cache,
-                         const float* k_scale, const float* v_scale, const int32_t* ctx_lens, int32_t* ctx_lens_out,
-                         int gamma, const rapid_attn_shape* shape, int32_t* status_word, cudaStream_t stream);
-int launch_kv_read_fp8(const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
-                       const int32_t* ctx_lens, const rapid_attn_shape* shape, const int32_t* chunk_idx, int n_chunks,
-                       int chunk_tokens, void* k_out, void* v_out, const rapid_attn_shape* out_shape, int32_t* out_lens,
-                       int32_t* status_word, cudaStream_t stream);
 int launch_accept(const float* target_logits, const float* draft_logits,
                   const int32_t* draft_tokens, const float* uniforms, float eta,
                   int32_t* out_accept_len, int32_t* out_next_token,

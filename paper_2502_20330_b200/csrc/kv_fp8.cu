@@ -15,6 +15,7 @@
 #include <math.h>
 
 #include "common.cuh"
+#include "prefix_kv8.cuh"
 
 namespace rapid {
 
