@@ -29,7 +29,17 @@
 // row tile, then all).
 //
 // Bound: up to 256 rows per KV head (one pair) a K/V tile of 64 KB is read for every 256 x 128 scores, and HBM
-// is the limit; from two pairs on the tensor cores and the exponentials are.
+// is the limit; from two pairs on the tensor cores and the exponentials are.  Measured (two kernels, calls in a row in
+// a graph, D = 128, bf16):
+//     8 requests of 1 row over 32K + up to 1,000 keys, 32 heads over 8       38 us   3.9 TB/s of the keys read once
+//     7 requests of 9 rows over 128K + up to 2,048, 32 over 8               145 us   4.0 TB/s and 0.94 PFLOP/s
+//    32 requests of 5 rows over 60K + up to 4,000, 28 over 4                157 us   0.90 PFLOP/s
+//    48 requests of 1 row over 8K + up to 1,500, paged in 64, 32 over 8      53 us   3.6 TB/s
+//    16 requests of 9 rows over 32K + up to 3,000, paged in 256, 64 over 8  175 us   0.92 PFLOP/s
+// and up to a fifth more for the large ones while they run for seconds (the clock falls to 1.5 - 1.6 GHz under the
+// power cap).  In those the tensor core is at work 68 - 76 % of the time: a QK^T of N = 64 takes one and a half times
+// its products, because it reads its 128 x 16 A operand from shared memory for 64 columns only.  N = 128 would not,
+// but leaves no second S (above).  The exponentials take 35 % of the special-function unit, issue slots 49 %.
 //
 // Waits are bounded as everywhere in this library; see mbar_wait_bounded.  A parity wait tells a phase from its
 // neighbours only, so every barrier here is one that at a wait is in the phase waited for or just past it.
@@ -539,7 +549,8 @@ prefix_attn_split_kernel(const __grid_constant__ CUtensorMap tmKp, const __grid_
         // ---------------- MMA issuers: a thread for each stream ----------------
         // It issues both products of its stream, because the tensor core works off a thread's instructions in
         // order: the QK^T that refills one half of S goes out behind the PV that reads P from it, with no wait
-        // in between.  It runs up to two blocks ahead of PV.
+        // in between.  It runs up to two blocks ahead of PV.  One thread of the warp is here alone: what is called in this
+        // branch is inlined, no function is.
         if (elect_one()) {
             constexpr uint32_t idesc_qk = umma_idesc_bf16(128, kBlock, 0, 0);
             constexpr uint32_t idesc_pv = umma_idesc_bf16(128, D, 0, 1);
@@ -801,8 +812,9 @@ prefix_attn_split_kernel(const __grid_constant__ CUtensorMap tmKp, const __grid_
 // (one per team whose range touches the KV head) and those of the row's own sequence.  A block takes 32
 // rows of a KV head (lane = row: slots are stored so that this reads whole lines) and 16 columns; its warps
 // take the slots w, w + 8, ... each, all loads of four slots in flight at once, and meet in shared memory.
-// Latency is what counts here (the call's partials are some 20 MB, in L2): one round trip for the ranges, one or
-// two for the slots.  The order of the sums is fixed: results do not depend on timing.
+// Latency is what counts here (the call's partials are up to some 20 MB, in L2): one round trip for the ranges, one or
+// two for the slots (8 - 27 us with events around it; the launch and its first reads overlap the split kernel's end).
+// The order of the sums is fixed: results do not depend on timing.
 template <int D>
 __global__ void __launch_bounds__(256)
 prefix_attn_merge_kernel(const __grid_constant__ PrefixArgs a, __nv_bfloat16* out, float* lse_out, float* out_f32) {
