@@ -383,8 +383,9 @@ __global__ void __launch_bounds__(kReadThreads) kv_read_fp8_kernel(const ReadArg
     const int ctx = (int)max(0LL, min((long long)given, a.c.Lmax));
     const int number = a.idx ? a.idx[(size_t)b * a.n_chunks + j] : j;
     const int rows = chunk_rows(a, ctx, number);
+    const long long from = rows > 0 ? (long long)number * a.chunk : 0;
     const int end = my < down && my_col < a.D ? rows : 0;  // (threads that make no whole row are idle)
-    const uint8_t* src = (is_v ? a.c.v : a.c.k) + b * a.c.sb + h * a.c.sh + ((long long)number * a.chunk + row0) * a.c.sl + my_col;
+    const uint8_t* src = (is_v ? a.c.v : a.c.k) + b * a.c.sb + h * a.c.sh + (from + row0) * a.c.sl + my_col;
     uint2 x[kReadUnroll];
 #pragma unroll
     for (int u = 0; u < kReadUnroll; ++u)
