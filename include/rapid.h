@@ -654,7 +654,7 @@ int rapid_kv_append_fp8(const void* k_new, const void* v_new, const rapid_kv_row
  *               0 .. n_chunks - 1
  *   k_out, v_out, out_shape : device bf16 cache, geometry as in rapid_verify_attention; what would go beyond its
  *               Lmax is left out and sets RAPID_STATUS_BAD_CTX_LEN; rows behind the last written are left as they were
- *   out_lens  : device int32 [B], rows written per KV head
+ *   out_lens  : device int32 [B], rows written per KV head; not ctx_lens itself
  * k_scale, v_scale fp32 [B, Hkv]; D % 16 == 0.  The output must not overlap the cache.
  */
 int rapid_kv_read_fp8(const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,

@@ -622,6 +622,10 @@ int launch_kv_read_fp8(const void* k_cache, const void* v_cache, const float* k_
         set_error("%s: 2 * B * Hkv and n_chunks at most 65535, chunk_tokens * D below 2^31", who);
         return RAPID_ERR_UNSUPPORTED;
     }
+    if (out_lens == ctx_lens) {
+        set_error("%s: out_lens must not be ctx_lens, which blocks still read when it is written", who);
+        return RAPID_ERR_INVALID_ARG;
+    }
     // no chunk is longer than the cache; the rows of the chunks named are added up in 32 bits
     const int64_t longest = chunk_tokens < s.Lmax ? chunk_tokens : s.Lmax;
     if (chunk_idx && longest * n_chunks > 0x7fffffffLL) {

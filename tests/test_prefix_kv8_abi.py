@@ -3,6 +3,7 @@ refusal of the C ABI.  A refused call launches nothing and looks at no device me
 import ctypes
 import os
 import subprocess
+from concurrent.futures import ThreadPoolExecutor
 
 import pytest
 
@@ -10,6 +11,14 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 INVALID, UNSUPPORTED, WORKSPACE = 1, 2, 3
 PTR = 1 << 20            # aligned to anything asked for; never read
 BIG = 1 << 40            # workspace bytes: enough for any shape here
+
+
+_elsewhere = ThreadPoolExecutor(1)
+
+
+def _refused(b, call, change):
+    """(code, message) of a call on another thread: the message of the last error is the thread's own."""
+    return _elsewhere.submit(lambda: (call(b, **change), b.last_error())).result()
 
 
 @pytest.fixture(scope="module")
@@ -99,8 +108,8 @@ def _paged(b, block_size=64, num_blocks=10, max_blocks=16, strides=(0, 0, 0), ta
     (dict(params=dict(plan=PTR)), UNSUPPORTED), (dict(params=dict(out_f32=PTR + 4)), UNSUPPORTED),
 ])
 def test_prefix_attention_refuses(b, change, code):
-    assert _prefix(b, **change) == code
-    assert b.last_error().startswith("rapid_verify_attention_prefix:")
+    got, message = _refused(b, _prefix, change)
+    assert got == code and message.startswith("rapid_verify_attention_prefix:")
 
 
 @pytest.mark.parametrize("change,code", [
@@ -110,8 +119,8 @@ def test_prefix_attention_refuses(b, change, code):
     (dict(strides=(4, 0, 0)), UNSUPPORTED), (dict(ws_bytes=1024), WORKSPACE), (dict(D=80), UNSUPPORTED),
 ])
 def test_paged_prefix_attention_refuses(b, change, code):
-    assert _paged(b, **change) == code
-    assert b.last_error().startswith("rapid_verify_attention_prefix_paged:")
+    got, message = _refused(b, _paged, change)
+    assert got == code and message.startswith("rapid_verify_attention_prefix_paged:")
 
 
 def _fill(b, kn=PTR, vn=PTR, rows=None, T=64, n=PTR, k=PTR, v=PTR, ks=PTR, vs=PTR, headroom=0, ws=PTR, ws_bytes=BIG, **shape):
@@ -129,8 +138,8 @@ def _fill(b, kn=PTR, vn=PTR, rows=None, T=64, n=PTR, k=PTR, v=PTR, ks=PTR, vs=PT
     (dict(ws=None), WORKSPACE), (dict(ws=PTR + 64), WORKSPACE), (dict(ws_bytes=256), WORKSPACE),
 ])
 def test_fill_refuses(b, change, code):
-    assert _fill(b, **change) == code
-    assert b.last_error().startswith("rapid_kv_fill_fp8:")
+    got, message = _refused(b, _fill, change)
+    assert got == code and message.startswith("rapid_kv_fill_fp8:")
 
 
 def _append(b, kn=PTR, vn=PTR, rows=None, k=PTR, v=PTR, ks=PTR, vs=PTR, ctx=PTR, gamma=2, status=PTR, **shape):
@@ -146,11 +155,11 @@ def _append(b, kn=PTR, vn=PTR, rows=None, k=PTR, v=PTR, ks=PTR, vs=PTR, ctx=PTR,
     (dict(v=PTR + 4), UNSUPPORTED), (dict(kv_stride_h=1000), UNSUPPORTED),
 ])
 def test_append_refuses(b, change, code):
-    assert _append(b, **change) == code
-    assert b.last_error().startswith("rapid_kv_append_fp8:")
+    got, message = _refused(b, _append, change)
+    assert got == code and message.startswith("rapid_kv_append_fp8:")
 
 
-def _read(b, k=PTR, v=PTR, ks=PTR, vs=PTR, ctx=PTR, idx=PTR, n_chunks=4, chunk=128, ko=PTR, vo=PTR, out=None, lens=PTR, status=PTR, **shape):
+def _read(b, k=PTR, v=PTR, ks=PTR, vs=PTR, ctx=PTR, idx=PTR, n_chunks=4, chunk=128, ko=PTR, vo=PTR, out=None, lens=2 * PTR, status=PTR, **shape):
     o = _shape(b, **(out or {}))
     return b.load_library().rapid_kv_read_fp8(k, v, ks, vs, ctx, ctypes.byref(_shape(b, **shape)), idx, n_chunks, chunk, ko, vo,
                                               ctypes.byref(o), lens, status, None)
@@ -162,8 +171,9 @@ def _read(b, k=PTR, v=PTR, ks=PTR, vs=PTR, ctx=PTR, idx=PTR, n_chunks=4, chunk=1
     (dict(n_chunks=0), INVALID), (dict(out=dict(D=64)), INVALID), (dict(out=dict(Hkv=1)), INVALID), (dict(out=dict(B=1)), INVALID),
     (dict(D=24, out=dict(D=24)), UNSUPPORTED), (dict(ko=PTR + 8), UNSUPPORTED), (dict(k=PTR + 8), UNSUPPORTED),
     (dict(out=dict(kv_stride_l=132)), UNSUPPORTED), (dict(B=20000, out=dict(B=20000)), UNSUPPORTED), (dict(n_chunks=65536), UNSUPPORTED),
+    (dict(lens=PTR), INVALID),                                # the lengths that the call reads
     (dict(n_chunks=65535, chunk=32769, Lmax=1 << 20), UNSUPPORTED),   # rows of the chunks named: beyond 32 bits
 ])
 def test_read_refuses(b, change, code):
-    assert _read(b, **change) == code
-    assert b.last_error().startswith("rapid_kv_read_fp8:")
+    got, message = _refused(b, _read, change)
+    assert got == code and message.startswith("rapid_kv_read_fp8:")
