@@ -154,12 +154,12 @@ __device__ __forceinline__ void fill_scalars(const FillArgs& a, int b, bool is_v
     }
 }
 
-// Short prompts: one cluster per (sequence, K or V, KV head) holds all of its rows in registers, so they are read
-// once: loads, the largest magnitude over block and cluster (a word of each CTA's shared memory that its peers
+// Short prompts: one cluster per (sequence, K or V, KV head), of up to eight CTAs, holds all of its rows in
+// registers, so they are read once: loads, the largest magnitude over block and cluster (a word of each CTA's shared memory that its peers
 // push to), codes.  A thread goes down one column of chunks of 8 elements (see kv_fill_kernel), N rows `down` apart;
 // CTA r of the cluster takes rows r * down * N .. .
 constexpr int kFillThreads = 256;
-constexpr int kFillCluster = 8;
+constexpr int kFillCluster = 8;   // CTAs of a cluster, at most
 constexpr int kFillResident = 4;  // blocks of the two-pass kernel on an SM
 constexpr int kFillLag = 1;       // its groups between maxima and codes
 
@@ -167,7 +167,7 @@ template <int N, int THREADS>
 __global__ void __launch_bounds__(THREADS) kv_fill_cluster_kernel(const FillArgs a) {
     __shared__ uint32_t peers[kFillCluster];
     __shared__ uint32_t warps[THREADS / 32];
-    const int rank = blockIdx.x, unit = blockIdx.y;  // (grid x = cluster)
+    const int rank = blockIdx.x, size = gridDim.x, unit = blockIdx.y;  // (grid x = cluster)
     const int h = unit % a.Hkv, rest = unit / a.Hkv;
     const bool is_v = rest & 1;
     const int b = rest >> 1;
@@ -189,7 +189,7 @@ __global__ void __launch_bounds__(THREADS) kv_fill_cluster_kernel(const FillArgs
     if ((threadIdx.x & 31) == 0) warps[threadIdx.x >> 5] = top;
     __syncthreads();
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-    if (threadIdx.x < kFillCluster) {  // thread p pushes the block's value to CTA p of the cluster
+    if (threadIdx.x < size) {  // thread p pushes the block's value to CTA p of the cluster
 #pragma unroll
         for (int w = 0; w < THREADS / 32; ++w) top = max(top, warps[w]);
         uint32_t there;
@@ -198,8 +198,7 @@ __global__ void __launch_bounds__(THREADS) kv_fill_cluster_kernel(const FillArgs
     }
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     top = 0;
-#pragma unroll
-    for (int p = 0; p < kFillCluster; ++p) top = max(top, peers[p]);
+    for (int p = 0; p < size; ++p) top = max(top, peers[p]);
     const int e = scale_exponent(top, a.headroom);
     if (rank == 0 && threadIdx.x == 0) fill_scalars(a, b, is_v, h, n, top, pow2(e));
     const uint64_t inv = pow2_twice(-e);
@@ -540,36 +539,42 @@ int launch_kv_fill_fp8(const void* k_new, const void* v_new, const rapid_kv_rows
     a.D = s.D;
     a.T = T;
     a.headroom = headroom;
-    // Rows that a cluster holds with one a thread.  Eight a thread of 512, 2,048 rows of 128, are the most that is faster
-    // than two passes (8 heads: 5.5 us for 8.7, and 49.7 for 53.8 at 16 sequences; with 16 a thread 14.4 for 12.7 at
-    // 4,096 rows).  Six a thread rather than eight where they do: 4.0 us for 4.8 at 1,100 rows.
-    const int per_row = s.D / 8;
-    const int64_t rows_256 = (int64_t)kFillCluster * (256 / per_row), rows_512 = (int64_t)kFillCluster * (512 / per_row);
-    if (T <= 8 * rows_512) {
+    int dev = 0, sms = 0;
+    RAPID_CUDA_CHECK(cudaGetDevice(&dev));
+    RAPID_CUDA_CHECK(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+    // Rows that a CTA holds with one a thread.  Eight a thread in clusters of eight CTAs of 512, 2,048 rows of 128, are
+    // the most that is faster than two passes (8 heads: 5.5 us for 8.7, and 49.7 for 53.8 at 16 sequences; with 16 a
+    // thread 14.4 for 12.7 at 4,096 rows).  Six a thread rather than eight where they do: 4.0 us for 4.8 at 1,100 rows.
+    const int per_row = s.D / 8, rows_256 = 256 / per_row, rows_512 = 512 / per_row;
+    if (T <= 8 * kFillCluster * rows_512) {
+        // Few units take all eight CTAs and few rows a thread; where that would be more than two CTAs an SM, as few CTAs as
+        // hold the rows, eight a thread (8 heads: 256 prompts of 64 rows 22 us for 85, 128 of 200 36 for 62, 8 of 500 6.9
+        // for 7.8).
+        int size = kFillCluster;
+        if (units * kFillCluster > 2 * sms)
+            while (size > 1 && T <= 8 * (size / 2) * rows_256) size /= 2;
+        const int64_t one_256 = (int64_t)size * rows_256, one_512 = (int64_t)size * rows_512;
         cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3(kFillCluster, (unsigned)units);
-        cfg.blockDim = dim3(T <= 8 * rows_256 ? 256 : 512);
+        cfg.gridDim = dim3(size, (unsigned)units);
+        cfg.blockDim = dim3(T <= 8 * one_256 ? 256 : 512);
         cfg.stream = stream;
         cudaLaunchAttribute attr[2];
         attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
         attr[0].val.programmaticStreamSerializationAllowed = 1;
         attr[1].id = cudaLaunchAttributeClusterDimension;
-        attr[1].val.clusterDim.x = kFillCluster;
+        attr[1].val.clusterDim.x = size;
         attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
         cfg.attrs = attr;
         cfg.numAttrs = 2;
-        if (T <= rows_256) RAPID_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kv_fill_cluster_kernel<1, 256>, a));
-        else if (T <= 2 * rows_256) RAPID_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kv_fill_cluster_kernel<2, 256>, a));
-        else if (T <= 4 * rows_256) RAPID_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kv_fill_cluster_kernel<4, 256>, a));
-        else if (T <= 8 * rows_256) RAPID_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kv_fill_cluster_kernel<8, 256>, a));
-        else if (T <= 6 * rows_512) RAPID_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kv_fill_cluster_kernel<6, 512>, a));
+        if (T <= one_256) RAPID_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kv_fill_cluster_kernel<1, 256>, a));
+        else if (T <= 2 * one_256) RAPID_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kv_fill_cluster_kernel<2, 256>, a));
+        else if (T <= 4 * one_256) RAPID_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kv_fill_cluster_kernel<4, 256>, a));
+        else if (T <= 8 * one_256) RAPID_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kv_fill_cluster_kernel<8, 256>, a));
+        else if (T <= 6 * one_512) RAPID_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kv_fill_cluster_kernel<6, 512>, a));
         else RAPID_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kv_fill_cluster_kernel<8, 512>, a));
         count_launch(1);
         return RAPID_OK;
     }
-    int dev = 0, sms = 0;
-    RAPID_CUDA_CHECK(cudaGetDevice(&dev));
-    RAPID_CUDA_CHECK(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
     const int grid = sms * kFillResident;
     // Groups of equal size of at most 32 MB (or one unit): with the group before it, half of L2.  A step's items,
     // the maxima of a group and the codes of another, are one wave of the grid.

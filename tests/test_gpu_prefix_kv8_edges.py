@@ -264,6 +264,8 @@ def test_fills_at_a_time_on_workspaces_of_their_own():
     (1, 700, 3, 48, None),
     (1, 9, 1, 2048, None), (1, 300, 1, 2048, None),              # a row as wide as a block
     (2, 40, 1, 4112, (40, 3)),                                   # wider
+    (64, 70, 8, 128, tuple(range(64))), (30, 128, 8, 128, None), (30, 129, 8, 128, None),  # many units: clusters of one CTA, two
+    (30, 257, 8, 64, None), (24, 500, 8, 128, None), (24, 520, 8, 128, None), (20, 170, 8, 80, None),                   # ... of one again, four, eight, two
     (40, 2300, 1, 64, tuple(57 * i for i in range(40))),         # groups of several sequences
     (3, 20000, 3, 128, (20000, 1, 12345)),                       # groups that end inside a sequence
 ])
