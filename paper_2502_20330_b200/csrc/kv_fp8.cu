@@ -159,13 +159,13 @@ __device__ __forceinline__ void fill_scalars(const FillArgs& a, int b, bool is_v
 // push to), codes.  A thread goes down one column of chunks of 8 elements (see kv_fill_kernel), N rows `down` apart;
 // CTA r of the cluster takes rows r * down * N .. .
 constexpr int kFillThreads = 256;
-constexpr int kFillCluster = 8;   // CTAs of a cluster, at most
+constexpr int kFillCluster = 8;   // CTAs of a cluster, at most; 16 where kv_fill_sixteen() says so
 constexpr int kFillResident = 4;  // blocks of the two-pass kernel on an SM
 constexpr int kFillLag = 1;       // its groups between maxima and codes
 
 template <int N, int THREADS>
 __global__ void __launch_bounds__(THREADS) kv_fill_cluster_kernel(const FillArgs a) {
-    __shared__ uint32_t peers[kFillCluster];
+    __shared__ uint32_t peers[16];
     __shared__ uint32_t warps[THREADS / 32];
     const int rank = blockIdx.x, size = gridDim.x, unit = blockIdx.y;  // (grid x = cluster)
     const int h = unit % a.Hkv, rest = unit / a.Hkv;
@@ -502,6 +502,28 @@ size_t kv_fill_workspace_bytes(int B, int Hkv) {
     return kWorkspaceHeaderBytes + align_up((1 + 2 * (size_t)2 * B * Hkv) * sizeof(uint32_t), 256);
 }
 
+// Whether the current device runs clusters of 16 (beyond what every one does); asked once for each.
+static int kv_fill_sixteen(int dev, bool& yes) {
+    static int known[64] = {};  // 1 + answer
+    if (dev < 64 && known[dev]) {
+        yes = known[dev] == 2;
+        return RAPID_OK;
+    }
+    int least = 16;
+    for (auto* f : {kv_fill_cluster_kernel<6, 512>, kv_fill_cluster_kernel<8, 512>}) {
+        RAPID_CUDA_CHECK(cudaFuncSetAttribute(f, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(16);
+        cfg.blockDim = dim3(512);
+        int n = 0;
+        RAPID_CUDA_CHECK(cudaOccupancyMaxPotentialClusterSize(&n, f, &cfg));
+        if (n < least) least = n;
+    }
+    yes = least >= 16;
+    if (dev < 64) known[dev] = yes ? 2 : 1;
+    return RAPID_OK;
+}
+
 int launch_kv_fill_fp8(const void* k_new, const void* v_new, const rapid_kv_rows* rows, int T, const int32_t* n_tokens,
                        void* k_cache, void* v_cache, float* k_scale, float* v_scale, int32_t* ctx_lens_out, int headroom,
                        const rapid_attn_shape* shape, void* workspace, size_t workspace_bytes, cudaStream_t stream) {
@@ -543,15 +565,22 @@ int launch_kv_fill_fp8(const void* k_new, const void* v_new, const rapid_kv_rows
     RAPID_CUDA_CHECK(cudaGetDevice(&dev));
     RAPID_CUDA_CHECK(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
     // Rows that a CTA holds with one a thread.  Eight a thread in clusters of eight CTAs of 512, 2,048 rows of 128, are
-    // the most that is faster than two passes (8 heads: 5.5 us for 8.7, and 49.7 for 53.8 at 16 sequences; with 16 a
+    // the most that is (for any number of units) faster than two passes (8 heads: 5.5 us for 8.7, and 49.7 for 53.8 at 16 sequences; with 16 a
     // thread 14.4 for 12.7 at 4,096 rows).  Six a thread rather than eight where they do: 4.0 us for 4.8 at 1,100 rows.
     const int per_row = s.D / 8, rows_256 = 256 / per_row, rows_512 = 512 / per_row;
-    if (T <= 8 * kFillCluster * rows_512) {
+    // Sixteen CTAs hold twice as much, which pays while there are few units (8 heads: 4,000 rows 10.2 us for 12.5, 2,100
+    // 6.5 for 9.0; four sequences of 4,000 31.1 for 30.8, sixteen 110 for 90).
+    bool sixteen = false;
+    if (T > 8 * kFillCluster * rows_512 && T <= 8 * 16 * rows_512 && units * 16 <= 4 * sms) {
+        const int rc = kv_fill_sixteen(dev, sixteen);
+        if (rc != RAPID_OK) return rc;
+    }
+    if (sixteen || T <= 8 * kFillCluster * rows_512) {
         // Few units take all eight CTAs and few rows a thread; where that would be more than two CTAs an SM, as few CTAs as
         // hold the rows, eight a thread (8 heads: 256 prompts of 64 rows 22 us for 85, 128 of 200 36 for 62, 8 of 500 6.9
         // for 7.8).
-        int size = kFillCluster;
-        if (units * kFillCluster > 2 * sms)
+        int size = sixteen ? 16 : kFillCluster;
+        if (!sixteen && units * kFillCluster > 2 * sms)
             while (size > 1 && T <= 8 * (size / 2) * rows_256) size /= 2;
         const int64_t one_256 = (int64_t)size * rows_256, one_512 = (int64_t)size * rows_512;
         cudaLaunchConfig_t cfg = {};

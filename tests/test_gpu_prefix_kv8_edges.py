@@ -259,7 +259,9 @@ def test_fills_at_a_time_on_workspaces_of_their_own():
 @pytest.mark.parametrize("B,T,Hkv,D,counts", [
     (1, 1024, 2, 128, None), (2, 1025, 2, 128, (1025, 1024)),    # the last rows and the first of each number of rows a thread
     (2, 1536, 1, 128, (1536, 1)), (1, 1537, 2, 128, None),
-    (2, 2048, 2, 128, (2048, 2041)), (2, 2049, 1, 128, (2049, 0)),  # the last that is read once, the first that is read twice
+    (2, 2048, 2, 128, (2048, 2041)), (2, 2049, 1, 128, (2049, 0)),  # eight CTAs' most rows; sixteen's first
+    (1, 4096, 2, 128, None), (2, 3073, 8, 128, (3073, 3000)), (1, 4097, 2, 128, None),  # sixteen's last; the first that is read twice
+    (3, 4000, 8, 128, (4000, 77, 3999)),                         # more units than sixteen CTAs pay for
     (3, 333, 2, 80, (333, 25, 0)), (2, 6000, 2, 80, (6000, 5999)),  # ten threads to a row: some have none
     (1, 700, 3, 48, None),
     (1, 9, 1, 2048, None), (1, 300, 1, 2048, None),              # a row as wide as a block
