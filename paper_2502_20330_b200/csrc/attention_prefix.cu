@@ -35,7 +35,7 @@
 //     7 requests of 9 rows over 128K + up to 2,048, 32 over 8               145 us   4.0 TB/s and 0.94 PFLOP/s
 //    32 requests of 5 rows over 60K + up to 4,000, 28 over 4                157 us   0.90 PFLOP/s
 //    48 requests of 1 row over 8K + up to 1,500, paged in 64, 32 over 8      53 us   3.6 TB/s
-//    16 requests of 9 rows over 32K + up to 3,000, paged in 256, 64 over 8  175 us   0.92 PFLOP/s
+//    16 requests of 9 rows over 32K + up to 3,000, paged in 256, 64 over 8  170 us   0.95 PFLOP/s
 // and up to a fifth more for the large ones while they run for seconds (the clock falls to 1.5 - 1.6 GHz under the
 // power cap).  In those the tensor core is at work 68 - 76 % of the time: a QK^T of N = 64 takes one and a half times
 // its products, because it reads its 128 x 16 A operand from shared memory for 64 columns only.  N = 128 would not,
@@ -811,16 +811,16 @@ prefix_attn_split_kernel(const __grid_constant__ CUtensorMap tmKp, const __grid_
 // Merge: out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s over the partials of a row: those of the prefix
 // (one per team whose range touches the KV head) and those of the row's own sequence.  A block takes 32
 // rows of a KV head (lane = row: slots are stored so that this reads whole lines) and 16 columns; its warps
-// take the slots w, w + 8, ... each, all loads of four slots in flight at once, and meet in shared memory.
+// take the slots w, w + W, ... each, all loads of four slots in flight at once, and meet in shared memory.
 // Latency is what counts here (the call's partials are up to some 20 MB, in L2): one round trip for the ranges, one or
-// two for the slots (8 - 27 us with events around it; the launch and its first reads overlap the split kernel's end).
+// two for the slots (6 - 18 us with events around it; the launch and its first reads overlap the split kernel's end).
 // The order of the sums is fixed: results do not depend on timing.
-template <int D>
-__global__ void __launch_bounds__(256)
+template <int D, int W>
+__global__ void __launch_bounds__(32 * W)
 prefix_attn_merge_kernel(const __grid_constant__ PrefixArgs a, __nv_bfloat16* out, float* lse_out, float* out_f32) {
     constexpr int UN = 4;
-    __shared__ float4 sh_acc[8][4][32];
-    __shared__ float sh_m[8][32], sh_l[8][32];
+    __shared__ float4 sh_acc[W][4][32];
+    __shared__ float sh_m[W][32], sh_l[W][32];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int kvh = blockIdx.y;
     const int total_rows = a.B * a.R * a.G;
@@ -854,12 +854,12 @@ prefix_attn_merge_kernel(const __grid_constant__ PrefixArgs a, __nv_bfloat16* ou
     float4 acc[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int x0 = warp; x0 < n_all; x0 += 8 * UN) {
+    for (int x0 = warp; x0 < n_all; x0 += W * UN) {
         float ms[UN], ls[UN];
         float4 o[UN][4];
 #pragma unroll
         for (int u = 0; u < UN; ++u) {
-            const int x = x0 + 8 * u;
+            const int x = x0 + W * u;
             ms[u] = -INFINITY;
             if (x < n_all) {
                 const bool pre = x < n_p;
@@ -899,32 +899,33 @@ prefix_attn_merge_kernel(const __grid_constant__ PrefixArgs a, __nv_bfloat16* ou
 #pragma unroll
     for (int j = 0; j < 4; ++j) sh_acc[warp][j][lane] = acc[j];
     __syncthreads();
-    if (threadIdx.x >= 128) return;
     // four neighbouring threads write the 16 columns of a row
-    const int row = threadIdx.x >> 2, j = threadIdx.x & 3;
-    if (row0 + row >= total_rows) return;
-    float M = -INFINITY, L = 0.f;
+    for (int t = threadIdx.x; t < 128; t += 32 * W) {
+        const int row = t >> 2, j = t & 3;
+        if (row0 + row >= total_rows) return;
+        float M = -INFINITY, L = 0.f;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) M = max3(M, sh_m[k][row], sh_m[k][row]);
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k = 0; k < W; ++k) M = max3(M, sh_m[k][row], sh_m[k][row]);
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        if (sh_m[k][row] == -INFINITY) continue;
-        const float wgt = exp2f(sh_m[k][row] - M);
-        const float4 o = sh_acc[k][j][row];
-        L += wgt * sh_l[k][row];
-        v.x += wgt * o.x;
-        v.y += wgt * o.y;
-        v.z += wgt * o.z;
-        v.w += wgt * o.w;
+        for (int k = 0; k < W; ++k) {
+            if (sh_m[k][row] == -INFINITY) continue;
+            const float wgt = exp2f(sh_m[k][row] - M);
+            const float4 o = sh_acc[k][j][row];
+            L += wgt * sh_l[k][row];
+            v.x += wgt * o.x;
+            v.y += wgt * o.y;
+            v.z += wgt * o.z;
+            v.w += wgt * o.w;
+        }
+        const int fo = (row0 + row) / a.G, go = row0 + row - fo * a.G;
+        const size_t at = (size_t)fo * a.Hq + (size_t)kvh * a.G + go;
+        const float inv = 1.f / L;
+        v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+        *reinterpret_cast<uint2*>(out + at * D + (d4 + j) * 4) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+        if (out_f32) *reinterpret_cast<float4*>(out_f32 + at * D + (d4 + j) * 4) = v;
+        if (lse_out && d4 + j == 0) lse_out[at] = (M + log2f(L)) * 0.69314718055994530942f;
     }
-    const int fo = (row0 + row) / a.G, go = row0 + row - fo * a.G;
-    const size_t at = (size_t)fo * a.Hq + (size_t)kvh * a.G + go;
-    const float inv = 1.f / L;
-    v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
-    *reinterpret_cast<uint2*>(out + at * D + (d4 + j) * 4) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
-    if (out_f32) *reinterpret_cast<float4*>(out_f32 + at * D + (d4 + j) * 4) = v;
-    if (lse_out && d4 + j == 0) lse_out[at] = (M + log2f(L)) * 0.69314718055994530942f;
 }
 
 // ---- host side ----------------------------------------------------------------------------
@@ -1008,8 +1009,20 @@ int launch(const CUtensorMap (&tm)[5], const PrefixArgs& a, __nv_bfloat16* out, 
                                       tm[0], tm[1], tm[2], tm[3], tm[4], a));
     if (split_done) RAPID_CUDA_CHECK(cudaEventRecord(static_cast<cudaEvent_t>(split_done), stream));
     const int rows = a.B * a.R * a.G;
-    RAPID_CUDA_CHECK(launch_dependent(prefix_attn_merge_kernel<D>, dim3((rows + 31) / 32, a.Hkv, D / 16), dim3(256), 0,
-                                      stream, a, out, lse, out_f32));
+    // Few blocks have eight warps, so that a row's slots are all in flight at once; many have two, so that those of more rows
+    // are (a row has two to ten slots then).  Whole calls with 8 / 4 / 2 warps, us: 192 blocks 69.4 / 72.2 / 73.1,
+    // 320 blocks 16.4 / 15.2 / 16.4, 512 148.5 / 147.7 / 149.0, 1,152 90.4 / 87.2 / 85.1, 1,264 27.2 / 23.7 / 22.2,
+    // 2,304 175.1 / 170.3 / 169.2, 4,864 85.8 / 69.4 / 61.6.
+    int sms = 0;
+    RAPID_CUDA_CHECK(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+    const dim3 grid((rows + 31) / 32, a.Hkv, D / 16);
+    const int64_t blocks = (int64_t)grid.x * grid.y * grid.z;
+    if (2 * blocks <= 3 * sms)
+        RAPID_CUDA_CHECK(launch_dependent(prefix_attn_merge_kernel<D, 8>, grid, dim3(256), 0, stream, a, out, lse, out_f32));
+    else if (blocks <= 8 * sms)
+        RAPID_CUDA_CHECK(launch_dependent(prefix_attn_merge_kernel<D, 4>, grid, dim3(128), 0, stream, a, out, lse, out_f32));
+    else
+        RAPID_CUDA_CHECK(launch_dependent(prefix_attn_merge_kernel<D, 2>, grid, dim3(64), 0, stream, a, out, lse, out_f32));
     count_launch(2);
     return RAPID_OK;
 }
