@@ -83,6 +83,7 @@ struct PrefixArgs {
     int2* prefix_range;          // per KV head: first and last team with tiles of it
     int2* own_range;             // per (sequence, KV head): first and last worker
     int32_t* status;
+    int32_t* plan_sig;           // first word of a verify plan's signature, see ws_layout
     int B, R, G, Hq, Hkv, GR;
     int Pmax, Lmax;              // capacities in keys (paged: both the capacity of a table row)
     int block_size, block_log2, num_blocks, max_blocks, box_rows;
@@ -450,6 +451,7 @@ prefix_attn_split_kernel(const __grid_constant__ CUtensorMap tmKp, const __grid_
     if (warp == 10) tmem_alloc(&tmem_slot, TMEM_COLS);  // the same warp frees it
     griddep_wait();  // lengths are read from here on
     griddep_launch_dependents();
+    if (cta == 0 && threadIdx.x == 32) *a.plan_sig = 0;
     if (threadIdx.x == 0) plan_prefix(a, cta, plan);
     tc_fence_before_sync();
     __syncthreads();
@@ -967,12 +969,18 @@ int make_map(CUtensorMap* map, const void* base, int D, int64_t d1, int64_t d2, 
     return RAPID_OK;
 }
 
+// Scratch.  A caller may use the same workspace for rapid_attention_plan and the calls that follow that plan, whose CTAs and
+// slots are then addressed by what lies behind the signature at the start of it; what is written here would be taken for
+// them.  So the signature's place is kept free of scratch, and every call takes the plan back by its first word (a batch
+// size, never 0): a call that still names the plan finds it stale.
 struct WsLayout {
-    size_t prefix_range, own_range, part_prefix, part_own, total;
+    size_t plan_sig, prefix_range, own_range, part_prefix, part_own, total;
 };
 WsLayout ws_layout(int B, int Hkv, int GR, int np, int D) {
     WsLayout l;
     size_t off = kWorkspaceHeaderBytes;
+    l.plan_sig = off;
+    off += 256;
     l.prefix_range = off;
     off += align_up((size_t)Hkv * sizeof(int2), 256);
     l.own_range = off;
@@ -1166,6 +1174,7 @@ int launch_verify_attention_prefix(const void* q, const void* k_prefix, const vo
     a.prefix_range = reinterpret_cast<int2*>(ws + lay.prefix_range);
     a.own_range = reinterpret_cast<int2*>(ws + lay.own_range);
     a.status = reinterpret_cast<int32_t*>(ws);
+    a.plan_sig = reinterpret_cast<int32_t*>(ws + lay.plan_sig);
     a.B = s.B;
     a.R = R;
     a.G = G;
