@@ -269,9 +269,9 @@ int rapid_verify_attention_fp8(const void* q, const void* k_cache, const void* v
  * this workspace and set params->plan.  A call whose geometry or lengths differ from the plan's
  * sets RAPID_STATUS_STALE_PLAN (checked on the device by every call).  shape's strides and a
  * paged layout do not matter to the plan.  The plan lasts until the workspace is used for another
- * plan, by an attention call without a plan, or by rapid_verify_attention_prefix, its paged form or
- * rapid_kv_fill_fp8, whose scratch takes its place: a call that names it afterwards sets
- * RAPID_STATUS_STALE_PLAN.  (The last of these leaves it in place for short prompts.)
+ * plan, by an attention call without a plan, or by a call of another kind whose scratch takes its
+ * place (rapid_verify_attention_prefix, its paged form, rapid_kv_fill_fp8 but for short prompts,
+ * rapid_accept, rapid_draft_sample): a call that names it afterwards sets RAPID_STATUS_STALE_PLAN.
  */
 int rapid_attention_plan(const int32_t* ctx_lens, int gamma, const rapid_attn_shape* shape,
                          const rapid_attn_params* params, void* workspace, size_t workspace_bytes,

@@ -530,7 +530,12 @@ __global__ void __launch_bounds__(NT, 2048 / NT / 2) accept_fused_kernel(const A
         }
     }
     __syncthreads();
-    if (tid == 0) *a.done = 0;  // ready for the next call on this workspace
+    if (tid == 0) {
+        *a.done = 0;  // ready for the next call on this workspace
+        // The ratios lie where a verify plan in the same workspace has its signature, the candidates where its walks
+        // begin.  Without drafts no ratio was written: the plan is taken back here (its first word is never 0).
+        if (a.gamma == 0) a.ratio[0] = 0.f;
+    }
 }
 
 bool accept_shape_ok(const rapid_accept_shape* s) {

@@ -102,3 +102,23 @@ def test_calls_without_a_plan_share_the_workspace(step):
         got, status = verify(R.PLAN_NONE)
         assert status == 0
         assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("gamma", [0, 3])
+def test_accepting_and_sampling_end_the_plan(step, gamma):
+    import paper_2502_20330_b200 as R
+    verify, _, plan, want, ws, _ = step
+    V = 512
+    logits, draft = torch.randn(B, gamma + 1, V, device="cuda"), torch.randn(B, max(gamma, 1), V, device="cuda")
+    tokens, u = torch.zeros(B, gamma, dtype=torch.int32, device="cuda"), torch.rand(B, gamma + 1, device="cuda")
+    n, tok, logq = _lens(*[0] * B), _lens(*[0] * B), torch.zeros(B, device="cuda")
+    calls = [lambda: R.rapid_accept(logits, draft[:, :gamma].contiguous(), tokens, u, 0.5, n, tok, ws)]
+    if gamma == 0:
+        calls.append(lambda: R.rapid_draft_sample(draft[:, 0].contiguous(), u[:, 0].contiguous(), 1.0, tok, logq, ws))
+    for call in calls:
+        plan()
+        call()
+        assert verify(R.PLAN_READY)[1] == R.STATUS_STALE_PLAN
+        plan()
+        got, status = verify(R.PLAN_READY)
+        assert status == 0 and torch.equal(got, want)
