@@ -357,18 +357,20 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 
 // 2^y0 and 2^y1, y at most 126, without the special-function unit: adding 1.5 * 2^23 leaves n, the whole number
-// next to y, in the low bits of the sum; f = y - n in [-1/2, 1/2] goes through the minimax polynomial of
-// degree 4 of 2^f (Remez exchange on the relative error, 2.7e-6 with fp32 coefficients), and n is added to the
-// exponent.  Below -125 the result is 2^-125.
+// next to y, in the low bits of the sum; f = y - n in [-1/2, 1/2] goes through the polynomial of degree 4 that is 1 at
+// f = 0 and has the least largest relative error to 2^f besides (2.9e-6 with fp32 coefficients; 2.7e-6 without the
+// condition), and n is added to the exponent.  The condition makes the end of the range exact: at y = -127 and below the
+// sum of both exponents is the word 0, so that a score of -inf, of a masked key too, weighs nothing.  From -126 down to there
+// the word is a denormal that is off by at most 2^-127.
 __device__ __forceinline__ void exp2_poly(float& y0, float& y1) {
     constexpr float kMagic = 12582912.f;
-    const uint64_t y = f32x2(fmaxf(y0, -125.f), fmaxf(y1, -125.f));
+    const uint64_t y = f32x2(fmaxf(y0, -127.f), fmaxf(y1, -127.f));
     const uint64_t t = f32x2_add(y, f32x2(kMagic, kMagic));
     const uint64_t f = f32x2_fma(f32x2_add(t, f32x2(-kMagic, -kMagic)), f32x2(-1.f, -1.f), y);
-    uint64_t p = f32x2_fma(f, f32x2(0.009570102207362652f, 0.009570102207362652f), f32x2(0.05591785907745361f, 0.05591785907745361f));
-    p = f32x2_fma(p, f, f32x2(0.240247443318367f, 0.240247443318367f));
-    p = f32x2_fma(p, f, f32x2(0.6931217908859253f, 0.6931217908859253f));
-    p = f32x2_fma(p, f, f32x2(0.9999992847442627f, 0.9999992847442627f));
+    uint64_t p = f32x2_fma(f, f32x2(0.009582852944731712f, 0.009582852944731712f), f32x2(0.055906426161527634f, 0.055906426161527634f));
+    p = f32x2_fma(p, f, f32x2(0.24024099111557007f, 0.24024099111557007f));
+    p = f32x2_fma(p, f, f32x2(0.6931241750717163f, 0.6931241750717163f));
+    p = f32x2_fma(p, f, f32x2(1.f, 1.f));
     float t0, t1;
     f32x2_split(t, t0, t1);
     f32x2_split(p, y0, y1);
@@ -389,19 +391,6 @@ __device__ __noinline__ void scale_o(uint32_t tO, float factor) {
         tmem_st_x16(tO + 16 * i, o);
     }
     tmem_wait_st();
-}
-
-// Zeroes a row's probabilities in a block but for the first `keep`: exp2_poly leaves 2^-125 where the score is -inf,
-// and V there may be anything finite.  (In registers, before P is written, it costs every block: 150.4 us for 146.9.)
-__device__ __noinline__ void keep_p(uint32_t tS, int keep) {
-    uint32_t x[32];
-    tmem_wait_st();
-    tmem_ld_x32(tS, x);
-    tmem_wait_ld();
-#pragma unroll
-    for (int k = 0; k < 32; ++k)
-        if (2 * k + 1 >= keep) x[k] &= 2 * k >= keep ? 0u : 0xffffu;
-    tmem_st_x32(tS, x);
 }
 
 template <int D>
@@ -730,7 +719,6 @@ prefix_attn_split_kernel(const __grid_constant__ CUtensorMap tmKp, const __grid_
                         pk[k >> 1] = pack_bf16x2(p0, p1);
                     }
                     tmem_st_x32(tS, pk);
-                    if (key0 + kBlock - 1 > all_see) keep_p(tS, lim - key0 + 1);
                     float s0, s1;
                     f32x2_split(f32x2_add(acc[0], acc[1]), s0, s1);
                     l_run += s0 + s1;
