@@ -371,10 +371,10 @@ int rapid_verify_attention_paged(const void* q, const void* k_pool, const void* 
  *   workspace          : device, >= rapid_prefix_attention_workspace_bytes(), initialised
  * D is 64 or 128, (Hq/Hkv) * R at most 128, B * Hkv at most 65,535; B * R may be large (thousands of rows
  * per KV head).  A length out of its range is clamped and sets RAPID_STATUS_BAD_CTX_LEN.  lse_out is within
- * 1e-4 of the exact value.  A key of which less than 2^-126 of the weight of its row's first keys is left counts
- * for nothing.  A value that is not finite in a V entry that some row sees reaches every row of that key's tile
- * that the same product holds.  Two kernels per call; lengths are read on the device, so a
- * captured call follows them.
+ * 1e-4 of the exact value.  A key whose weight is below 2^-125 of its row's largest may count for nothing.  Sums
+ * stay finite while the number of keys times the largest |V| is below 2^111.  A value that is not finite in a V
+ * entry that some row sees reaches every row of that key's tile that the same product holds.  Two kernels per
+ * call; lengths are read on the device, so a captured call follows them.
  */
 typedef struct rapid_prefix_kv {
     int64_t Pmax;     /* capacity in keys                     */

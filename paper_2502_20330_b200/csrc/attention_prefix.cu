@@ -62,8 +62,8 @@ constexpr int kHalfBytes = kKeys * 128;  // one 64-column half of a tile of 128 
 constexpr int kPad = 3;                // single-stream tiles that a change of unit costs
 constexpr int kPoly = 3;               // of 8 pairs of exponentials, those that the FMA pipe takes from the special-function unit
 constexpr int kMaxPrefixCtas = 256;
-constexpr float kJump = 40.f;          // a score this far (log2) above a row's reference moves it: probabilities stay below
-                                       // 2^40, far from the end of fp32's and bf16's range in any sum
+constexpr float kJump = 16.f;          // a score this far (log2) above a row's reference moves it: probabilities stay below 2^16 as
+                                       // in the kernels without a prefix, and O below 2^16 |V| a key (at 40 a |V| of 3e26 overflowed)
 
 __host__ __device__ constexpr int k_slots(int D) { return D == 128 ? 2 : 4; }
 __host__ __device__ constexpr int v_slots(int D) { return D == 128 ? 3 : 6; }

@@ -1,4 +1,6 @@
-"""Prefix attention at the ends of bf16's range: keys without weight whose values are the largest there are."""
+"""Prefix attention at the ends of bf16's range: keys without weight whose values are the largest there are, and large values under
+scores that rise along the keys."""
+import numpy as np
 import pytest
 import torch
 
@@ -65,3 +67,28 @@ def test_keys_without_weight_add_nothing_however_large_their_values(D, low):
     assert torch.isfinite(want).all() and size.max() < 100
     assert ((got[0].double() - want).abs() <= 2 * 2 ** -8 * size + 1e-6).all()
     assert (got[2].double() - lse).abs().max() < 1e-4
+
+
+@pytest.mark.parametrize("D,B,num_ctas", [(64, 2, 1), (128, 2, 1), (128, 12, 1), (128, 12, 3)])
+@pytest.mark.parametrize("rise", [12, 36])
+def test_large_values_where_scores_rise_along_the_keys(D, B, num_ctas, rise):
+    """Later keys weigh 2^rise times the earlier ones and V is around 2^95 everywhere: times the keys 2^106, inside the 2^111 that the
+    call allows.  (A CTA takes long runs of tiles here, so that rows come to the later keys with a reference of the earlier.)
+    Tolerance: 2^-8 of sum p |v| for the probabilities and for the output, 2^-11 for the scores' fp32 sums: 128 products of at
+    most 600 in all, 128 * 2^-24 * 600 / sqrt(128) < 2^-11."""
+    P, n, gamma = 640, 400, 4
+    q, kp, vp = _rnd(B, gamma + 1, 8, D, seed=10), _rnd(2, P, D, seed=11), _rnd(2, P, D, seed=12)
+    k, v = _rnd(B, 2, n, D, seed=13), _rnd(B, 2, n, D, seed=14)
+    q[..., 0] = 1
+    by = rise * np.log(2) * D ** 0.5
+    for keys in (kp, k):
+        keys[..., 0] = 0
+        keys[..., 64:, 0] = by / 2
+        keys[..., 256:, 0] = by
+    vp *= 2.0 ** 95
+    v *= 2.0 ** 95
+    lens = [n - 7 * b for b in range(B)]
+    got = _call(q, kp, vp, P, k, v, lens, gamma, num_ctas=num_ctas)
+    want, size, _ = _exact(q, kp, vp, P, k, v, lens)
+    assert ((got[0].double() - want).abs() <= (2 * 2 ** -8 + 2 ** -11) * size).all()
+    assert ((got[1].double() - want).abs() <= (2 ** -8 + 2 ** -11) * size).all()
