@@ -749,7 +749,8 @@ def rapid_kv_append_fp8(k_new, v_new, k_cache, v_cache, k_scale, v_scale, ctx_le
 def rapid_kv_read_fp8(k_cache, v_cache, k_scale, v_scale, ctx_lens, chunk_idx, chunk_tokens, k_out, v_out, out_lens,
                       status_word, stream=None) -> None:
     """Chunks of an E4M3 cache, one behind the other, into the bf16 cache k_out / v_out [B, Hkv, Lout, D].  chunk_idx
-    [B, n] names them (-1: none), as rapid_retrieval_select returns them; None: all chunks the output has room for."""
+    [B, n] names them (-1: none), as rapid_retrieval_select returns them; None: each cache from its start, as far as the output has
+    room (a longer one sets STATUS_BAD_CTX_LEN)."""
     cache, geometry = _cache8(k_cache, v_cache, k_scale, v_scale)
     if not (k_out.dtype is v_out.dtype is _BF16):
         raise TypeError("k_out / v_out must be bfloat16")
@@ -762,7 +763,9 @@ def rapid_kv_read_fp8(k_cache, v_cache, k_scale, v_scale, ctx_lens, chunk_idx, c
     if chunk_tokens <= 0:
         raise ValueError("chunk_tokens must be positive")
     if chunk_idx is None:
-        n = -(-min(shape[2], cache[2]) // chunk_tokens)
+        told = min(shape[2] + 1, cache[2])                      # one token past the output's room, to tell what did not fit
+        chunk_tokens = max(chunk_tokens, -(-told // 65535))     # (a call takes 65,535 chunks; their length has no bearing here)
+        n = -(-told // chunk_tokens)
     else:
         if chunk_idx.dtype is not _I32:
             raise TypeError("chunk_idx must be int32")
