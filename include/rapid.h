@@ -359,7 +359,8 @@ int rapid_verify_attention_paged(const void* q, const void* k_pool, const void* 
  * For every sequence b, query head h (KV head g = h / (Hq/Hkv)) and row i:
  *   out[b,i,h,:] = softmax-weighted sum of the values of the *prefix_len prefix keys (every row sees them all)
  *                  and of the keys 0 <= j <= ctx_lens[b] - R + i of sequence b's own cache.
- * It equals rapid_verify_attention over each sequence's prefix and own keys written one behind the other.
+ * It equals rapid_verify_attention over each sequence's prefix and own keys written one behind the other: fp32
+ * accumulation, bf16 probabilities in the second product, bf16 output.
  *
  *   k_prefix, v_prefix : device [Hkv, Pmax, D] bf16, D contiguous, geometry of `prefix`; entries at positions
  *                        >= *prefix_len are never used, whatever their bits
@@ -371,10 +372,11 @@ int rapid_verify_attention_paged(const void* q, const void* k_pool, const void* 
  *   workspace          : device, >= rapid_prefix_attention_workspace_bytes(), initialised
  * D is 64 or 128, (Hq/Hkv) * R at most 128, B * Hkv at most 65,535; B * R may be large (thousands of rows
  * per KV head).  A length out of its range is clamped and sets RAPID_STATUS_BAD_CTX_LEN.  lse_out is within
- * 1e-4 of the exact value.  A key whose weight is below 2^-125 of its row's largest may count for nothing.  Sums
- * stay finite while the number of keys times the largest |V| is below 2^111.  A value that is not finite in a V
- * entry that some row sees reaches every row of that key's tile that the same product holds.  Two kernels per
- * call; lengths are read on the device, so a captured call follows them.
+ * 1e-4 of the exact value, plus 2^-17 of the row's largest scale * sum_d |q_d k_d| (the scores are fp32 sums).  A key
+ * whose weight is below 2^-125 of its row's largest may count for nothing.  Sums stay finite while the number of
+ * keys times the largest |V| is below 2^111.  A value that is not finite in a V entry that some row sees reaches
+ * every row of that key's tile that the same product holds.  Two kernels per call; lengths are read on the
+ * device, so a captured call follows them.
  */
 typedef struct rapid_prefix_kv {
     int64_t Pmax;     /* capacity in keys                     */
@@ -609,6 +611,8 @@ typedef struct rapid_kv_rows {
  * KV head, over the rows 0 .. n_tokens[b] - 1:
  *   scale = 2^headroom * (the smallest power of two with max |x| <= 448 * scale);  1 where there is nothing but zeros
  *   code  = E4M3(x / scale), to nearest, ties to even
+ * The scale is kept within 2^-126 .. 2^126: rows with a maximum beyond 448 * 2^(126 - headroom) get less headroom (none is
+ * lost up to 6), rows of denormals a larger scale.  The codes go
  * into positions 0 .. n_tokens[b] - 1; the cache behind them is left as it was.  `headroom` (0 .. 8) leaves that many
  * powers of two for later, larger rows (rapid_kv_append_fp8 keeps the scale).  A power of two makes
  * rapid_kv_read_fp8 exact for these codes.  NaN is stored as NaN and takes no part in the maximum; an
@@ -650,12 +654,13 @@ int rapid_kv_append_fp8(const void* k_new, const void* v_new, const rapid_kv_row
  * rapid_retrieval_select chose become the cache that the drafter (or, as the shared prefix of
  * rapid_verify_attention_prefix, a batch of them) attends over (Section 2.3: the drafter runs on the retrieved
  * context); or a whole cache goes back to bf16.
- *   out = bf16(scale * decode(code)), the product in fp32 (exact for the scales of rapid_kv_fill_fp8)
+ *   out = bf16(scale * decode(code)), the product in fp32 (exact for the scales of rapid_kv_fill_fp8, but for what
+ *         lies beyond bf16's range: a value of 248 * 2^120 or more has the code of 2^128 and comes back as an infinity)
  *   ctx_lens  : device int32 [B], tokens in the cache; out of [0, Lmax]: clamped, sets RAPID_STATUS_BAD_CTX_LEN
  *   chunk_idx : device int32 [B, n_chunks]: chunk i holds positions [i * chunk_tokens, (i+1) * chunk_tokens), as far
  *               as ctx_lens[b] reaches; -1 is no chunk; any other that holds nothing sets RAPID_STATUS_BAD_CTX_LEN.
  *               The same chunk may be named twice; all together hold less than 2^31 tokens.  NULL: chunks
- *               0 .. n_chunks - 1
+ *               0 .. n_chunks - 1, whatever the cache holds behind them.  n_chunks is at most 65,535
  *   k_out, v_out, out_shape : device bf16 cache, geometry as in rapid_verify_attention; what would go beyond its
  *               Lmax is left out and sets RAPID_STATUS_BAD_CTX_LEN; rows behind the last written are left as they were
  *   out_lens  : device int32 [B], rows written per KV head; not ctx_lens itself
