@@ -47,6 +47,8 @@
 // mean that the PV of block j - 2 has completed, but say nothing of j - 1.
 #include <math.h>
 
+#include <atomic>
+
 #include "common.cuh"
 #include "prefix_kv8.cuh"
 #include "tcgen05.cuh"
@@ -996,7 +998,7 @@ int launch(const CUtensorMap (&tm)[5], const PrefixArgs& a, __nv_bfloat16* out, 
     static_assert(smem <= 232448 - 1024, "shared memory (dynamic + static)");
     int dev = 0;
     RAPID_CUDA_CHECK(cudaGetDevice(&dev));
-    static bool configured[64] = {};
+    static std::atomic<bool> configured[64];  // (first calls may come from several threads at once; all set the same)
     if (dev >= 64 || !configured[dev]) {
         RAPID_CUDA_CHECK(cudaFuncSetAttribute(prefix_attn_split_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
         if (dev < 64) configured[dev] = true;

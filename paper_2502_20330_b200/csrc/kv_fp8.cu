@@ -14,6 +14,8 @@
 #include <cuda_fp8.h>
 #include <math.h>
 
+#include <atomic>
+
 #include "common.cuh"
 #include "prefix_kv8.cuh"
 
@@ -504,9 +506,9 @@ size_t kv_fill_workspace_bytes(int B, int Hkv) {
 
 // Whether the current device runs clusters of 16 (beyond what every one does); asked once for each.
 static int kv_fill_sixteen(int dev, bool& yes) {
-    static int known[64] = {};  // 1 + answer
-    if (dev < 64 && known[dev]) {
-        yes = known[dev] == 2;
+    static std::atomic<int> known[64];  // 1 + answer (first calls may come from several threads at once)
+    if (const int told = dev < 64 ? known[dev].load() : 0) {
+        yes = told == 2;
         return RAPID_OK;
     }
     int least = 16;
