@@ -31,15 +31,15 @@
 // Bound: up to 256 rows per KV head (one pair) a K/V tile of 64 KB is read for every 256 x 128 scores, and HBM
 // is the limit; from two pairs on the tensor cores and the exponentials are.  Measured (two kernels, calls in a row in
 // a graph, D = 128, bf16):
-//     8 requests of 1 row over 32K + up to 1,000 keys, 32 heads over 8       38 us   3.9 TB/s of the keys read once
-//     7 requests of 9 rows over 128K + up to 2,048, 32 over 8               145 us   4.0 TB/s and 0.94 PFLOP/s
-//    32 requests of 5 rows over 60K + up to 4,000, 28 over 4                157 us   0.90 PFLOP/s
-//    48 requests of 1 row over 8K + up to 1,500, paged in 64, 32 over 8      53 us   3.6 TB/s
-//    16 requests of 9 rows over 32K + up to 3,000, paged in 256, 64 over 8  170 us   0.95 PFLOP/s
-// and up to a fifth more for the large ones while they run for seconds (the clock falls to 1.5 - 1.6 GHz under the
-// power cap).  In those the tensor core is at work 68 - 76 % of the time: a QK^T of N = 64 takes one and a half times
+//     8 requests of 1 row over 32K + up to 1,000 keys, 32 heads over 8       37 us   4.0 TB/s of the keys read once
+//     7 requests of 9 rows over 128K + up to 2,048, 32 over 8               146 us   4.0 TB/s and 0.94 PFLOP/s
+//    32 requests of 5 rows over 60K + up to 4,000, 28 over 4          156 - 172 us   0.91 - 0.83 PFLOP/s, by process
+//    48 requests of 1 row over 8K + up to 1,500, paged in 64, 32 over 8      54 us   3.5 TB/s
+//    16 requests of 9 rows over 32K + up to 3,000, paged in 256, 64 over 8  169 us   0.96 PFLOP/s
+// and up to a quarter more for the large ones while they run for seconds (the clock falls to 1.5 - 1.6 GHz under the
+// power cap).  In those the tensor core is at work 68 - 69 % of the time: a QK^T of N = 64 takes one and a half times
 // its products, because it reads its 128 x 16 A operand from shared memory for 64 columns only.  N = 128 would not,
-// but leaves no second S (above).  The exponentials take 35 % of the special-function unit, issue slots 49 %.
+// but leaves no second S (above).  The exponentials take 36 % of the special-function unit, issue slots 49 %.
 //
 // Waits are bounded as everywhere in this library; see mbar_wait_bounded.  A parity wait tells a phase from its
 // neighbours only, so every barrier here is one that at a wait is in the phase waited for or just past it.
