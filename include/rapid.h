@@ -624,6 +624,7 @@ typedef struct rapid_kv_rows {
  *   k_scale, v_scale : device fp32 [B, Hkv], written
  *   ctx_lens_out : device int32 [B], receives n_tokens[b]; or NULL
  *   workspace    : device, >= rapid_kv_fill_workspace_bytes(), initialised; the status word is its first
+ * 2 * B * Hkv is at most 65,535 and T * D below 2^31 - 65,536.
  */
 size_t rapid_kv_fill_workspace_bytes(int B, int Hkv);
 int rapid_kv_fill_fp8(const void* k_new, const void* v_new, const rapid_kv_rows* rows, int T,
@@ -641,6 +642,7 @@ int rapid_kv_fill_fp8(const void* k_new, const void* v_new, const rapid_kv_rows*
  *   k_scale, v_scale : device fp32 [B, Hkv], positive and finite
  *   ctx_lens     : device int32 [B], tokens in the cache before the call
  *   ctx_lens_out : device int32 [B], receives ctx_lens[b] + R; may be ctx_lens itself (one more kernel); or NULL
+ * B is at most 65,535 and R * Hkv * D below 2^31 - 1,024.
  * A sequence whose cache cannot take R more rows (or with a negative length) is left untouched, its length
  * is passed on as it is, and RAPID_STATUS_BAD_CTX_LEN is set in *status_word.
  */
@@ -664,7 +666,8 @@ int rapid_kv_append_fp8(const void* k_new, const void* v_new, const rapid_kv_row
  *   k_out, v_out, out_shape : device bf16 cache, geometry as in rapid_verify_attention; what would go beyond its
  *               Lmax is left out and sets RAPID_STATUS_BAD_CTX_LEN; rows behind the last written are left as they were
  *   out_lens  : device int32 [B], rows written per KV head; not ctx_lens itself
- * k_scale, v_scale fp32 [B, Hkv]; D % 16 == 0.  The output must not overlap the cache.
+ * k_scale, v_scale fp32 [B, Hkv]; D % 16 == 0; 2 * B * Hkv at most 65,535, chunk_tokens * D below 2^31 - 65,536.  The
+ * output must not overlap the cache.
  */
 int rapid_kv_read_fp8(const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
                       const int32_t* ctx_lens, const rapid_attn_shape* shape, const int32_t* chunk_idx,
