@@ -194,6 +194,13 @@ __global__ void __launch_bounds__(NT, 2048 / NT / 2) accept_fused_kernel(const A
     // CTA says so here and waits for the others just before its first store into a peer.
     cluster.barrier_arrive();
     griddep_wait();  // the logits may come from the kernel just before this one
+    // The ratios lie where a verify plan in the same workspace has its signature, the candidates where its walks begin: the
+    // plan is taken back by its first word, which is never 0, before a dependent can start that reads a settled plan
+    // ahead of its own wait.  (Row 0's ratio is written later by the same cluster.)
+    if (row == 0 && c == 0 && tid == NT - 1) {
+        a.ratio[0] = 0.f;
+        __threadfence();
+    }
     griddep_launch_dependents();
 
     // The draft token and the two logits at it are needed late (step 2), by one thread, on the CTA's
@@ -530,12 +537,7 @@ __global__ void __launch_bounds__(NT, 2048 / NT / 2) accept_fused_kernel(const A
         }
     }
     __syncthreads();
-    if (tid == 0) {
-        *a.done = 0;  // ready for the next call on this workspace
-        // The ratios lie where a verify plan in the same workspace has its signature, the candidates where its walks
-        // begin.  Without drafts no ratio was written: the plan is taken back here (its first word is never 0).
-        if (a.gamma == 0) a.ratio[0] = 0.f;
-    }
+    if (tid == 0) *a.done = 0;  // ready for the next call on this workspace
 }
 
 bool accept_shape_ok(const rapid_accept_shape* s) {

@@ -105,7 +105,8 @@ def test_calls_without_a_plan_share_the_workspace(step):
 
 
 @pytest.mark.parametrize("gamma", [0, 3])
-def test_accepting_and_sampling_end_the_plan(step, gamma):
+@pytest.mark.parametrize("mode", ["PLAN_READY", "PLAN_SETTLED"])
+def test_accepting_and_sampling_end_the_plan(step, gamma, mode):
     import paper_2502_20330_b200 as R
     verify, _, plan, want, ws, _ = step
     V = 512
@@ -118,7 +119,7 @@ def test_accepting_and_sampling_end_the_plan(step, gamma):
     for call in calls:
         plan()
         call()
-        assert verify(R.PLAN_READY)[1] == R.STATUS_STALE_PLAN
+        assert verify(getattr(R, mode))[1] == R.STATUS_STALE_PLAN
         plan()
         got, status = verify(R.PLAN_READY)
         assert status == 0 and torch.equal(got, want)
