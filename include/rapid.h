@@ -676,6 +676,74 @@ int rapid_kv_read_fp8(const void* k_cache, const void* v_cache, const float* k_s
                       void* cuda_stream);
 
 /*
+ * Position rotation (rotary position embedding; the paper's models apply it, its text does not spell it out).  The first
+ * rotary_dim columns of a head are pairs, and pair i of a row is turned by the angle a = p * inv_freq[i], where p is the row's
+ * position on the pair's axis:
+ *   y1 = scale * (x1 cos a - x2 sin a),   y2 = scale * (x1 sin a + x2 cos a)
+ * The other columns stay as they are.  Text has one axis; images and video turn a part of the pairs by time, a part by
+ * height and a part by width (pair_axis says which).  The angle's whole turns are taken off in 64 bits: cos and sin are good
+ * to 1e-6 while |a| < 2^31, whatever the position.  x, inv_freq and the positions are read, y is rounded to bf16 once.
+ */
+typedef struct rapid_rope {
+    const float* inv_freq;    /* device fp32 [rotary_dim / 2]                                                       */
+    int32_t rotary_dim;       /* multiple of 16, at most D; 0 = D                                                   */
+    int32_t interleaved;      /* 0: pair i is columns i and i + rotary_dim / 2;  non-zero: columns 2i and 2i + 1    */
+    float scale;              /* finite; 0 = 1                                                                      */
+    int32_t n_axes;           /* 1 to 4 (0 = 1)                                                                     */
+    const uint8_t* pair_axis; /* HOST [rotary_dim / 2]: the axis of every pair, below n_axes; NULL = axis 0 for all */
+} rapid_rope;
+
+/*
+ * Rotates queries and keys, or either of them.
+ *   q, k         : device bf16, T rows per sequence, geometry of q_rows / k_rows (NULL = dense [B, T, Hq, D] and
+ *                  [B, T, Hkv, D]); one of them may be NULL, and its output then too.  A cache [B, Hkv, L, D] is
+ *                  rows with stride_t = D and stride_h = L * D: keys of retrieved chunks are turned to new places by
+ *                  the differences of the positions, which may be negative
+ *   q_out, k_out : device bf16, geometry of q_out_rows / k_out_rows (strides at least D).  An output may be its input with
+ *                  the same strides; apart from that nothing written may overlap anything read
+ *   positions    : device int32 [n_axes, B, T], dense; any values
+ *   inverse      : non-zero turns by -a: the gradient of the rotation, and for scale 1 its inverse
+ * D is a multiple of 16, at most 256; B, Hq and Hkv at most 65,535.
+ */
+int rapid_rope_apply(const void* q, const rapid_kv_rows* q_rows, void* q_out, const rapid_kv_rows* q_out_rows,
+                     const void* k, const rapid_kv_rows* k_rows, void* k_out, const rapid_kv_rows* k_out_rows, int B,
+                     int T, int Hq, int Hkv, int D, const int32_t* positions, const rapid_rope* rope, int inverse,
+                     void* cuda_stream);
+
+/*
+ * rapid_kv_append for rows that are not rotated yet, for any number of them and for sequences that bring different
+ * numbers: turns the new keys on their way into the cache, writes the values beside them, and turns the queries.  One kernel.
+ *   q            : device bf16, T rows per sequence, geometry of q_rows (NULL = dense [B, T, Hq, D]); or NULL, with q_out
+ *   k_new, v_new : device bf16, T rows per sequence, geometry of `rows` (NULL = dense [B, T, Hkv, D])
+ *   n_tokens     : device int32 [B], rows that count, in [0, T]; or NULL = T each
+ *   q_out        : device bf16 [B, T, Hq, D], dense; may be q where that is dense.  Rows behind n_tokens[b] are left as
+ *                  they were, in q_out as in the cache
+ *   k_cache, v_cache : device bf16, geometry of `shape` (strides honoured)
+ *   ctx_lens     : device int32 [B], tokens in the cache before the call
+ *   ctx_lens_out : device int32 [B], receives ctx_lens[b] + n_tokens[b]; may be ctx_lens itself (one more kernel); or NULL
+ *   positions    : device int32 [n_axes, B, T], dense; NULL = ctx_lens[b] + i (one axis)
+ * A sequence with a count out of range, a negative length or a cache that cannot take its rows is left untouched, its length
+ * is passed on as it is, and RAPID_STATUS_BAD_CTX_LEN is set in *status_word.  Limits as in rapid_rope_apply.
+ */
+int rapid_kv_append_rope(const void* q, const rapid_kv_rows* q_rows, const void* k_new, const void* v_new,
+                         const rapid_kv_rows* rows, int T, const int32_t* n_tokens, void* q_out, void* k_cache,
+                         void* v_cache, const int32_t* ctx_lens, int32_t* ctx_lens_out, const rapid_rope* rope,
+                         const int32_t* positions, const rapid_attn_shape* shape, int32_t* status_word,
+                         void* cuda_stream);
+
+/*
+ * The same into a paged cache (see rapid_paged_kv; block_size need not be a power of two here).  shape->Lmax must equal
+ * max_blocks_per_seq * block_size; shape's strides are ignored.  A position whose entry is outside [0, num_blocks) is
+ * not written and sets RAPID_STATUS_BAD_BLOCK_TABLE; its query is turned all the same.
+ */
+int rapid_kv_append_rope_paged(const void* q, const rapid_kv_rows* q_rows, const void* k_new, const void* v_new,
+                               const rapid_kv_rows* rows, int T, const int32_t* n_tokens, void* q_out, void* k_pool,
+                               void* v_pool, const int32_t* block_table, const rapid_paged_kv* paged,
+                               const int32_t* ctx_lens, int32_t* ctx_lens_out, const rapid_rope* rope,
+                               const int32_t* positions, const rapid_attn_shape* shape, int32_t* status_word,
+                               void* cuda_stream);
+
+/*
  * Closes a verify step (Algorithm 1: accepted drafts become x_j, the rest is discarded): of the R
  * rows appended before the step the cache keeps the last accepted token and the accept_len[b]
  * accepted drafts,  ctx_lens[b] -= gamma - accept_len[b].  (The token sampled by the step is

@@ -5,7 +5,7 @@ import ctypes
 import os
 from dataclasses import dataclass
 from functools import lru_cache
-from typing import Optional
+from typing import Optional, Sequence
 
 import torch
 
@@ -33,6 +33,7 @@ EXPORTS = [
     "rapid_version", "rapid_kernel_launch_count", "rapid_kernel_launch_count_reset",
     "rapid_prefix_attention_workspace_bytes", "rapid_verify_attention_prefix", "rapid_verify_attention_prefix_paged",
     "rapid_kv_fill_workspace_bytes", "rapid_kv_fill_fp8", "rapid_kv_append_fp8", "rapid_kv_read_fp8",
+    "rapid_rope_apply", "rapid_kv_append_rope", "rapid_kv_append_rope_paged",
 ]
 
 
@@ -60,6 +61,11 @@ class _PrefixKv(ctypes.Structure):
 
 class _KvRows(ctypes.Structure):
     _fields_ = [("stride_b", ctypes.c_int64), ("stride_t", ctypes.c_int64), ("stride_h", ctypes.c_int64)]
+
+
+class _Rope(ctypes.Structure):
+    _fields_ = [("inv_freq", ctypes.c_void_p), ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("n_axes", ctypes.c_int32), ("pair_axis", ctypes.c_char_p)]
 
 
 class _AttnParams(ctypes.Structure):
@@ -115,6 +121,15 @@ class AcceptParams:
     ratio_out: Optional[torch.Tensor] = None  # [B,gamma] float32
     draft_row_stats: Optional[torch.Tensor] = None  # [B,gamma,2] float32: rapid_draft_sample's out_row_stats
     draft_logq: Optional[torch.Tensor] = None       # [B,gamma] float32: rapid_draft_sample's out_logq
+
+
+@dataclass
+class Rope:
+    inv_freq: torch.Tensor                   # [rotary_dim / 2] float32, CUDA: pair i turns by position * inv_freq[i]
+    rotary_dim: int = 0                      # columns that are turned; 0 = all of head_dim
+    interleaved: bool = False                # pairs are neighbouring columns, not columns half of rotary_dim apart
+    scale: float = 1.0                       # factor of the turned columns
+    pair_axis: Optional[Sequence[int]] = None  # [rotary_dim / 2]: whose position turns each pair; None = axis 0 for all
 
 
 _lib = None
@@ -198,6 +213,14 @@ def load_library():
         lib.rapid_kv_append_fp8.argtypes = [vp, vp, rows_p, vp, vp, vp, vp, vp, vp, i32, shape_p, vp, vp]
         lib.rapid_kv_read_fp8.restype = i32
         lib.rapid_kv_read_fp8.argtypes = [vp, vp, vp, vp, vp, shape_p, vp, i32, i32, vp, vp, shape_p, vp, vp, vp]
+        rope_p = ctypes.POINTER(_Rope)
+        lib.rapid_rope_apply.restype = i32
+        lib.rapid_rope_apply.argtypes = [vp, rows_p] * 4 + [i32] * 5 + [vp, rope_p, i32, vp]
+        append_rope = [vp, rows_p, vp, vp, rows_p, i32, vp, vp, vp, vp]
+        lib.rapid_kv_append_rope.restype = i32
+        lib.rapid_kv_append_rope.argtypes = append_rope + [vp, vp, rope_p, vp, shape_p, vp, vp]
+        lib.rapid_kv_append_rope_paged.restype = i32
+        lib.rapid_kv_append_rope_paged.argtypes = append_rope + [vp, ctypes.POINTER(_PagedKv), vp, vp, rope_p, vp, shape_p, vp, vp]
         lib.rapid_step_commit.restype = i32
         lib.rapid_step_commit.argtypes = [vp, vp, i32, i32, vp, vp]
         lib.rapid_last_error.restype = ctypes.c_char_p
@@ -777,6 +800,152 @@ def rapid_kv_read_fp8(k_cache, v_cache, k_scale, v_scale, ctx_lens, chunk_idx, c
         k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), ctx_lens.data_ptr(),
         ctypes.byref(geometry), _addr(chunk_idx), n, chunk_tokens, k_out.data_ptr(), v_out.data_ptr(), ctypes.byref(out),
         out_lens.data_ptr(), status_word.data_ptr(), st))
+
+
+@lru_cache(maxsize=512)
+def _row_strides(x, st):
+    return _KvRows(*_told(x, st))
+
+
+@lru_cache(maxsize=512)
+def _pool_geometry(k, kst, table):
+    return _PagedKv(k[2], k[0], table[1], 0, *_told(k, kst))
+
+
+@lru_cache(maxsize=512)
+def _append_geometry(k, kst, Hq, Lmax):
+    return _AttnShape(k[0], Hq, k[1], k[3], Lmax, *_told(k, kst))
+
+
+@lru_cache(maxsize=64)
+def _pair_axes(pair_axis):
+    if any(not 0 <= a < 4 for a in pair_axis):
+        raise ValueError("pair_axis must name axes 0 to 3")
+    return bytes(pair_axis)
+
+
+def _rope(rope, D, positions, B, T):
+    """The library's struct and the positions' address; positions [B, T] for one axis, [n_axes, B, T], or None."""
+    rd = rope.rotary_dim or D
+    f = rope.inv_freq
+    if f.dtype is not _F32 or f.numel() * 2 != rd or not f.is_contiguous():
+        raise ValueError("inv_freq must be dense float32 [rotary_dim / 2]")
+    axes = 1
+    if positions is not None:
+        if positions.dtype is not _I32 or not positions.is_contiguous():
+            raise TypeError("positions must be dense int32")
+        shape = positions.shape
+        if shape[-2:] != (B, T) or len(shape) not in (2, 3):
+            raise ValueError("positions must be [B, T] or [n_axes, B, T]")
+        axes = shape[0] if len(shape) == 3 else 1
+    pairs = None
+    if rope.pair_axis is not None:
+        pairs = _pair_axes(tuple(rope.pair_axis))
+        if len(pairs) * 2 != rd:
+            raise ValueError("pair_axis must hold rotary_dim / 2 axes")
+    return _Rope(f.data_ptr(), rope.rotary_dim, 1 if rope.interleaved else 0, rope.scale, axes, pairs)
+
+
+def _turned(x, y, what):
+    if not (x.dtype is y.dtype is _BF16):
+        raise TypeError(what + " and its output must be bfloat16")
+    if x.dim() != 4 or x.shape != y.shape:
+        raise ValueError(what + " and its output must be [B, T, heads, D]")
+    return x.shape, _row_strides(x.shape, x.stride()), _row_strides(y.shape, y.stride())
+
+
+def rapid_rope_apply(q, q_out, k, k_out, positions, rope: Rope, inverse: bool = False, stream=None) -> None:
+    """Turns q [B, T, Hq, D] and k [B, T, Hkv, D] (bf16, may be strided; either may be None, with its output) by their
+    positions [B, T] or [n_axes, B, T] (int32).  An output may be its input.  ``inverse`` turns back (the gradient)."""
+    if (q is None) != (q_out is None) or (k is None) != (k_out is None) or (q is None and k is None):
+        raise ValueError("q and k need an output each, and one of them has to be given")
+    shape = qr = qor = kr = kor = None
+    Hq = Hkv = 0
+    if q is not None:
+        shape, qr, qor = _turned(q, q_out, "q")
+        Hq = shape[2]
+    if k is not None:
+        ks, kr, kor = _turned(k, k_out, "k")
+        Hkv = ks[2]
+        if shape is not None and (ks[0], ks[1], ks[3]) != (shape[0], shape[1], shape[3]):
+            raise ValueError("q and k disagree on batch, rows or head_dim")
+        shape = ks
+    if positions is None:
+        raise ValueError("positions are required")
+    B, T, _, D = shape
+    r = _rope(rope, D, positions, B, T)
+    st = _here(stream, q, q_out, k, k_out, positions, rope.inv_freq)
+    ref = lambda g: None if g is None else ctypes.byref(g)  # noqa: E731
+    _check(load_library().rapid_rope_apply(_addr(q), ref(qr), _addr(q_out), ref(qor), _addr(k), ref(kr), _addr(k_out), ref(kor),
+                                           B, T, Hq, Hkv, D, positions.data_ptr(), ctypes.byref(r), 1 if inverse else 0, st))
+
+
+def _append_rows(q, k_new, v_new, q_out, n_tokens, ctx_lens, ctx_lens_out):
+    """(B, T, Hq, Hkv, D) and the strides of q and of the new rows"""
+    if not (k_new.dtype is v_new.dtype is _BF16):
+        raise TypeError("k_new / v_new must be bfloat16")
+    shape, stride = _alike(k_new, v_new, "k_new and v_new")
+    if len(shape) != 4:
+        raise ValueError("k_new and v_new must be [B, T, Hkv, D]")
+    B, T, Hkv, D = shape
+    Hq, qr = Hkv, None
+    if (q is None) != (q_out is None):
+        raise ValueError("q needs q_out, and q_out needs q")
+    if q is not None:
+        if not (q.dtype is q_out.dtype is _BF16):
+            raise TypeError("q and q_out must be bfloat16")
+        qs = q.shape
+        if len(qs) != 4 or (qs[0], qs[1], qs[3]) != (B, T, D) or q_out.shape != qs or not q_out.is_contiguous():
+            raise ValueError("q must be [B, T, Hq, D] with the new rows' B, T and D, q_out the same and dense")
+        Hq, qr = qs[2], ctypes.byref(_row_strides(qs, q.stride()))
+    _lens(n_tokens, B, "n_tokens")
+    _lens(ctx_lens, B, "ctx_lens")
+    _lens(ctx_lens_out, B, "ctx_lens_out")
+    return B, T, Hq, Hkv, D, qr, ctypes.byref(_row_strides(shape, stride))
+
+
+def rapid_kv_append_rope(q, k_new, v_new, q_out, k_cache, v_cache, ctx_lens, ctx_lens_out, rope: Rope, status_word,
+                         n_tokens=None, positions=None, stream=None) -> None:
+    """Turns the new rows k_new [B, T, Hkv, D] on their way into the cache [B, Hkv, Lmax, D] at ctx_lens, writes v_new beside
+    them and turns q [B, T, Hq, D] into q_out (bf16; q and the new rows may be strided, q may be None).  n_tokens [B] of the
+    rows count (None: all); positions as in rapid_rope_apply (None: ctx_lens + row); ctx_lens_out (None, another tensor, or
+    ctx_lens itself) receives ctx_lens + n_tokens."""
+    B, T, Hq, Hkv, D, qr, rows = _append_rows(q, k_new, v_new, q_out, n_tokens, ctx_lens, ctx_lens_out)
+    if not (k_cache.dtype is v_cache.dtype is _BF16):
+        raise TypeError("k_cache / v_cache must be bfloat16")
+    cache, stride = _alike(k_cache, v_cache, "k_cache and v_cache")
+    if len(cache) != 4 or (cache[0], cache[1], cache[3]) != (B, Hkv, D):
+        raise ValueError("k_cache and v_cache must be [B, Hkv, Lmax, D] of the new rows' batch, KV heads and head_dim")
+    geometry = _append_geometry(cache, stride, Hq, cache[2])
+    r = _rope(rope, D, positions, B, T)
+    st = _here(stream, q, k_new, v_new, q_out, k_cache, v_cache, ctx_lens, ctx_lens_out, rope.inv_freq, status_word, n_tokens,
+               positions)
+    _check(load_library().rapid_kv_append_rope(
+        _addr(q), qr, k_new.data_ptr(), v_new.data_ptr(), rows, T, _addr(n_tokens), _addr(q_out), k_cache.data_ptr(),
+        v_cache.data_ptr(), ctx_lens.data_ptr(), _addr(ctx_lens_out), ctypes.byref(r), _addr(positions), ctypes.byref(geometry),
+        status_word.data_ptr(), st))
+
+
+def rapid_kv_append_rope_paged(q, k_new, v_new, q_out, k_pool, v_pool, block_table, ctx_lens, ctx_lens_out, rope: Rope,
+                               status_word, n_tokens=None, positions=None, stream=None) -> None:
+    """rapid_kv_append_rope into pools [num_blocks, Hkv, block_size, D] through block_table [B, max_blocks] (int32)."""
+    B, T, Hq, Hkv, D, qr, rows = _append_rows(q, k_new, v_new, q_out, n_tokens, ctx_lens, ctx_lens_out)
+    if not (k_pool.dtype is v_pool.dtype is _BF16) or block_table.dtype is not _I32:
+        raise TypeError("the pools must be bfloat16, block_table int32")
+    pool, stride = _alike(k_pool, v_pool, "k_pool and v_pool")
+    if len(pool) != 4 or (pool[1], pool[3]) != (Hkv, D):
+        raise ValueError("k_pool and v_pool must be [num_blocks, Hkv, block_size, D] of the new rows' KV heads and head_dim")
+    if block_table.dim() != 2 or block_table.shape[0] != B or not block_table.is_contiguous():
+        raise ValueError("block_table must be dense [B, max_blocks_per_seq]")
+    paged = _pool_geometry(pool, stride, block_table.shape)
+    shape = _AttnShape(B, Hq, Hkv, D, block_table.shape[1] * pool[2], 0, 0, 0)
+    r = _rope(rope, D, positions, B, T)
+    st = _here(stream, q, k_new, v_new, q_out, k_pool, v_pool, block_table, ctx_lens, ctx_lens_out, rope.inv_freq, status_word,
+               n_tokens, positions)
+    _check(load_library().rapid_kv_append_rope_paged(
+        _addr(q), qr, k_new.data_ptr(), v_new.data_ptr(), rows, T, _addr(n_tokens), _addr(q_out), k_pool.data_ptr(),
+        v_pool.data_ptr(), block_table.data_ptr(), ctypes.byref(paged), ctx_lens.data_ptr(), _addr(ctx_lens_out),
+        ctypes.byref(r), _addr(positions), ctypes.byref(shape), status_word.data_ptr(), st))
 
 
 def rapid_step_commit(ctx_lens, accept_len, gamma, status_word, stream=None) -> None:

@@ -4,6 +4,7 @@
 #include <string.h>
 
 #include "common.cuh"
+#include "prefill.cuh"
 #include "prefix_kv8.cuh"
 
 namespace rapid {
@@ -209,6 +210,42 @@ int rapid_kv_read_fp8(const void* k_cache, const void* v_cache, const float* k_s
     clear_error();
     return launch_kv_read_fp8(k_cache, v_cache, k_scale, v_scale, ctx_lens, shape, chunk_idx, n_chunks, chunk_tokens, k_out,
                               v_out, out_shape, out_lens, status_word, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int rapid_rope_apply(const void* q, const rapid_kv_rows* q_rows, void* q_out, const rapid_kv_rows* q_out_rows,
+                     const void* k, const rapid_kv_rows* k_rows, void* k_out, const rapid_kv_rows* k_out_rows, int B,
+                     int T, int Hq, int Hkv, int D, const int32_t* positions, const rapid_rope* rope, int inverse,
+                     void* cuda_stream) {
+    clear_error();
+    return launch_rope_apply(q, q_rows, q_out, q_out_rows, k, k_rows, k_out, k_out_rows, B, T, Hq, Hkv, D, positions, rope,
+                             inverse, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int rapid_kv_append_rope(const void* q, const rapid_kv_rows* q_rows, const void* k_new, const void* v_new,
+                         const rapid_kv_rows* rows, int T, const int32_t* n_tokens, void* q_out, void* k_cache,
+                         void* v_cache, const int32_t* ctx_lens, int32_t* ctx_lens_out, const rapid_rope* rope,
+                         const int32_t* positions, const rapid_attn_shape* shape, int32_t* status_word,
+                         void* cuda_stream) {
+    clear_error();
+    return launch_kv_append_rope(q, q_rows, k_new, v_new, rows, T, n_tokens, q_out, k_cache, v_cache, nullptr, nullptr,
+                                 ctx_lens, ctx_lens_out, rope, positions, shape, status_word,
+                                 static_cast<cudaStream_t>(cuda_stream));
+}
+
+int rapid_kv_append_rope_paged(const void* q, const rapid_kv_rows* q_rows, const void* k_new, const void* v_new,
+                               const rapid_kv_rows* rows, int T, const int32_t* n_tokens, void* q_out, void* k_pool,
+                               void* v_pool, const int32_t* block_table, const rapid_paged_kv* paged,
+                               const int32_t* ctx_lens, int32_t* ctx_lens_out, const rapid_rope* rope,
+                               const int32_t* positions, const rapid_attn_shape* shape, int32_t* status_word,
+                               void* cuda_stream) {
+    clear_error();
+    if (!paged || !block_table) {
+        set_error("rapid_kv_append_rope_paged: NULL paged geometry or block table");
+        return RAPID_ERR_INVALID_ARG;
+    }
+    return launch_kv_append_rope(q, q_rows, k_new, v_new, rows, T, n_tokens, q_out, k_pool, v_pool, paged, block_table,
+                                 ctx_lens, ctx_lens_out, rope, positions, shape, status_word,
+                                 static_cast<cudaStream_t>(cuda_stream));
 }
 
 int rapid_step_commit(int32_t* ctx_lens, const int32_t* accept_len, int gamma, int B,
