@@ -410,6 +410,53 @@ int rapid_verify_attention_prefix_paged(const void* q, const void* k_pool, const
                                         size_t workspace_bytes, void* cuda_stream);
 
 /*
+ * Where the new rows of a sequence lie (keys, values, queries): bf16, D contiguous, element strides between sequences / tokens /
+ * KV heads (0 = dense [B, T, Hkv, D]); multiples of 8.
+ */
+typedef struct rapid_kv_rows {
+    int64_t stride_b;
+    int64_t stride_t;
+    int64_t stride_h;
+} rapid_kv_rows;
+
+/*
+ * Attention of many new rows of every sequence over its cache: a prompt, the next piece of one (the cache then holds what
+ * went before), the drafter's retrieved context (Section 2.3), or a long draft.  The rows' own keys have been appended
+ * (rapid_kv_append_rope).  With n = n_tokens[b], row i of sequence b is the query at position p = ctx_lens[b] - n + i, and
+ *   out[b,i,h,:] = softmax-weighted sum of the values of the keys j <= p of KV head h / (Hq/Hkv)
+ * or, with window_keys, of those of them with j > p - window_keys or j < sink_keys (the mask of the streaming drafter, as in
+ * rapid_attn_params; key tiles that no row sees are not read), or, with all_keys_visible, of all ctx_lens[b] keys.
+ *   q            : device bf16, T rows per sequence, geometry of q_rows (NULL = dense [B, T, Hq, D]; strides multiples of 8)
+ *   n_tokens     : device int32 [B], rows that count, in [0, T]; or NULL = T each
+ *   k_cache, v_cache : device bf16, geometry of `shape` (strides honoured); entries at positions >= ctx_lens[b] are
+ *                  never used, whatever their bits
+ *   ctx_lens     : device int32 [B], keys in the cache, the new rows included: in [n, Lmax] (in [0, Lmax] with
+ *                  all_keys_visible)
+ *   out          : device bf16 [B, T, Hq, D], dense; rows behind n_tokens[b] are left as they were, here as in
+ *                  lse_out [B, T, Hq] and out_f32 [B, T, Hq, D] (16-byte aligned)
+ *   params       : host, may be NULL; scale, num_ctas (at most 256), lse_out, out_f32, split_done_event, all_keys_visible,
+ *                  sink_keys, window_keys and wait_cycle_limit apply, anything else set is RAPID_ERR_UNSUPPORTED
+ *   workspace    : device, >= rapid_prefill_attention_workspace_bytes(), initialised
+ * D is 64 or 128, Hq/Hkv at most 128, B and Hkv at most 65,535, and B * Hkv * ceil(T / (2 * floor(128 / (Hq/Hkv)))) at most
+ * 2^24.  A sequence with a count or a length out of range is left out (its rows stay as they were) and sets
+ * RAPID_STATUS_BAD_CTX_LEN.  A row that sees no key is 0, its log-sum-exp -inf.  fp32 accumulation, bf16 probabilities in the
+ * second product; lse_out, the range of V, values that are not finite and keys of next to no weight are as in
+ * rapid_verify_attention_prefix.  Three kernels per call; lengths are read on the device, so a captured call follows them.
+ */
+size_t rapid_prefill_attention_workspace_bytes(const rapid_attn_shape* shape, int T);
+
+int rapid_prefill_attention(const void* q, const rapid_kv_rows* q_rows, int T, const int32_t* n_tokens, const void* k_cache,
+                            const void* v_cache, const int32_t* ctx_lens, void* out, const rapid_attn_shape* shape,
+                            const rapid_attn_params* params, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* The same over a paged cache (see rapid_paged_kv); shape->Lmax, table and bad entries as in rapid_verify_attention_paged. */
+int rapid_prefill_attention_paged(const void* q, const rapid_kv_rows* q_rows, int T, const int32_t* n_tokens,
+                                  const void* k_pool, const void* v_pool, const int32_t* block_table,
+                                  const rapid_paged_kv* paged, const int32_t* ctx_lens, void* out,
+                                  const rapid_attn_shape* shape, const rapid_attn_params* params, void* workspace,
+                                  size_t workspace_bytes, void* cuda_stream);
+
+/*
  * Accept / residual (Algorithm 1, validation loop and residual step;
  * Eq. (new_target); Section 2.4).
  *
@@ -594,16 +641,6 @@ int rapid_kv_append(const void* k_new, const void* v_new, void* k_cache, void* v
 int rapid_kv_append_paged(const void* k_new, const void* v_new, void* k_pool, void* v_pool,
                           const int32_t* block_table, const rapid_paged_kv* paged, int32_t* ctx_lens,
                           int gamma, int B, int Hkv, int D, int32_t* status_word, void* cuda_stream);
-
-/*
- * Where the rows lie that the two calls below quantise: bf16, D contiguous, element strides between sequences / tokens /
- * KV heads (0 = dense [B, T, Hkv, D]); multiples of 8.
- */
-typedef struct rapid_kv_rows {
-    int64_t stride_b;
-    int64_t stride_t;
-    int64_t stride_h;
-} rapid_kv_rows;
 
 /*
  * Writes a prompt's K/V rows into an FP8 E4M3 cache (the one rapid_verify_attention_fp8 reads) and chooses its scales.

@@ -34,6 +34,7 @@ EXPORTS = [
     "rapid_prefix_attention_workspace_bytes", "rapid_verify_attention_prefix", "rapid_verify_attention_prefix_paged",
     "rapid_kv_fill_workspace_bytes", "rapid_kv_fill_fp8", "rapid_kv_append_fp8", "rapid_kv_read_fp8",
     "rapid_rope_apply", "rapid_kv_append_rope", "rapid_kv_append_rope_paged",
+    "rapid_prefill_attention_workspace_bytes", "rapid_prefill_attention", "rapid_prefill_attention_paged",
 ]
 
 
@@ -221,6 +222,13 @@ def load_library():
         lib.rapid_kv_append_rope.argtypes = append_rope + [vp, vp, rope_p, vp, shape_p, vp, vp]
         lib.rapid_kv_append_rope_paged.restype = i32
         lib.rapid_kv_append_rope_paged.argtypes = append_rope + [vp, ctypes.POINTER(_PagedKv), vp, vp, rope_p, vp, shape_p, vp, vp]
+        lib.rapid_prefill_attention_workspace_bytes.restype = sz
+        lib.rapid_prefill_attention_workspace_bytes.argtypes = [shape_p, i32]
+        prefill_tail = [vp, vp, shape_p, ctypes.POINTER(_AttnParams), vp, sz, vp]
+        lib.rapid_prefill_attention.restype = i32
+        lib.rapid_prefill_attention.argtypes = [vp, rows_p, i32, vp, vp, vp] + prefill_tail
+        lib.rapid_prefill_attention_paged.restype = i32
+        lib.rapid_prefill_attention_paged.argtypes = [vp, rows_p, i32, vp, vp, vp, vp, ctypes.POINTER(_PagedKv)] + prefill_tail
         lib.rapid_step_commit.restype = i32
         lib.rapid_step_commit.argtypes = [vp, vp, i32, i32, vp, vp]
         lib.rapid_last_error.restype = ctypes.c_char_p
@@ -946,6 +954,70 @@ def rapid_kv_append_rope_paged(q, k_new, v_new, q_out, k_pool, v_pool, block_tab
         _addr(q), qr, k_new.data_ptr(), v_new.data_ptr(), rows, T, _addr(n_tokens), _addr(q_out), k_pool.data_ptr(),
         v_pool.data_ptr(), block_table.data_ptr(), ctypes.byref(paged), ctx_lens.data_ptr(), _addr(ctx_lens_out),
         ctypes.byref(r), _addr(positions), ctypes.byref(shape), status_word.data_ptr(), st))
+
+
+def prefill_attention_workspace_bytes(B, Hq, Hkv, D, T) -> int:
+    """Scratch of rapid_prefill_attention and rapid_prefill_attention_paged for calls of up to T rows per sequence."""
+    s = _AttnShape(B, Hq, Hkv, D, 1, 0, 0, 0)
+    return int(load_library().rapid_prefill_attention_workspace_bytes(ctypes.byref(s), T))
+
+
+def _prefill_rows(q, out, ctx_lens, n_tokens, params):
+    """(shape of q, its strides, lse_out, out_f32)"""
+    if not (q.dtype is out.dtype is _BF16):
+        raise TypeError("q and out must be bfloat16")
+    shape = q.shape
+    if len(shape) != 4 or out.shape != shape or not out.is_contiguous():
+        raise ValueError("q must be [B, T, Hq, D], out the same and dense")
+    if ctx_lens is None:
+        raise ValueError("ctx_lens are required")
+    _lens(ctx_lens, shape[0], "ctx_lens")
+    _lens(n_tokens, shape[0], "n_tokens")
+    lse = o32 = None
+    if params is not None:
+        lse, o32 = params.lse_out, params.out_f32
+        for t, n in ((lse, q.numel() // shape[3]), (o32, q.numel())):
+            if t is not None and (t.dtype is not _F32 or t.numel() != n or not t.is_contiguous()):
+                raise ValueError("lse_out must be dense float32 [B, T, Hq] and out_f32 [B, T, Hq, D]")
+    return shape, ctypes.byref(_row_strides(shape, q.stride())), lse, o32
+
+
+def rapid_prefill_attention(q, k_cache, v_cache, ctx_lens, out, workspace, n_tokens=None, params: Optional[AttnParams] = None,
+                            stream=None) -> None:
+    """Attention of the n_tokens [B] newest rows of every sequence (None: all T of q [B, T, Hq, D]; may be strided) over its
+    cache [B, Hkv, Lmax, D], of which ctx_lens [B] keys count, the rows' own included: causal, or with params.window_keys /
+    sink_keys or all_keys_visible.  bf16."""
+    if not (k_cache.dtype is v_cache.dtype is _BF16):
+        raise TypeError("k_cache / v_cache must be bfloat16")
+    shape, rows, lse, o32 = _prefill_rows(q, out, ctx_lens, n_tokens, params)
+    cache, stride = _alike(k_cache, v_cache, "k_cache and v_cache")
+    if len(cache) != 4 or cache[0] != shape[0] or cache[3] != shape[3]:
+        raise ValueError("k_cache and v_cache must be [B, Hkv, Lmax, D] of q's batch and head_dim")
+    geometry = _append_geometry(cache, stride, shape[2], cache[2])
+    st = _here(stream, q, k_cache, v_cache, ctx_lens, out, workspace, n_tokens, lse, o32)
+    _check(load_library().rapid_prefill_attention(
+        q.data_ptr(), rows, shape[1], _addr(n_tokens), k_cache.data_ptr(), v_cache.data_ptr(), ctx_lens.data_ptr(), out.data_ptr(),
+        ctypes.byref(geometry), _attn_params(params), workspace.data_ptr(), _nbytes(workspace), st))
+
+
+def rapid_prefill_attention_paged(q, k_pool, v_pool, block_table, ctx_lens, out, workspace, n_tokens=None,
+                                  params: Optional[AttnParams] = None, stream=None) -> None:
+    """rapid_prefill_attention over pools [num_blocks, Hkv, block_size, D] through block_table [B, max_blocks] (int32)."""
+    if not (k_pool.dtype is v_pool.dtype is _BF16) or block_table.dtype is not _I32:
+        raise TypeError("the pools must be bfloat16, block_table int32")
+    shape, rows, lse, o32 = _prefill_rows(q, out, ctx_lens, n_tokens, params)
+    pool, stride = _alike(k_pool, v_pool, "k_pool and v_pool")
+    if len(pool) != 4 or pool[3] != shape[3]:
+        raise ValueError("k_pool and v_pool must be [num_blocks, Hkv, block_size, D] of q's head_dim")
+    if block_table.dim() != 2 or block_table.shape[0] != shape[0] or not block_table.is_contiguous():
+        raise ValueError("block_table must be dense [B, max_blocks_per_seq]")
+    paged = _pool_geometry(pool, stride, block_table.shape)
+    geometry = _AttnShape(shape[0], shape[2], pool[1], shape[3], block_table.shape[1] * pool[2], 0, 0, 0)
+    st = _here(stream, q, k_pool, v_pool, block_table, ctx_lens, out, workspace, n_tokens, lse, o32)
+    _check(load_library().rapid_prefill_attention_paged(
+        q.data_ptr(), rows, shape[1], _addr(n_tokens), k_pool.data_ptr(), v_pool.data_ptr(), block_table.data_ptr(),
+        ctypes.byref(paged), ctx_lens.data_ptr(), out.data_ptr(), ctypes.byref(geometry), _attn_params(params),
+        workspace.data_ptr(), _nbytes(workspace), st))
 
 
 def rapid_step_commit(ctx_lens, accept_len, gamma, status_word, stream=None) -> None:

@@ -212,6 +212,32 @@ int rapid_kv_read_fp8(const void* k_cache, const void* v_cache, const float* k_s
                               v_out, out_shape, out_lens, status_word, static_cast<cudaStream_t>(cuda_stream));
 }
 
+size_t rapid_prefill_attention_workspace_bytes(const rapid_attn_shape* shape, int T) {
+    return prefill_attention_workspace_bytes(shape, T);
+}
+
+int rapid_prefill_attention(const void* q, const rapid_kv_rows* q_rows, int T, const int32_t* n_tokens, const void* k_cache,
+                            const void* v_cache, const int32_t* ctx_lens, void* out, const rapid_attn_shape* shape,
+                            const rapid_attn_params* params, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    clear_error();
+    return launch_prefill_attention(q, q_rows, T, n_tokens, k_cache, v_cache, nullptr, nullptr, ctx_lens, out, shape, params,
+                                    workspace, workspace_bytes, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int rapid_prefill_attention_paged(const void* q, const rapid_kv_rows* q_rows, int T, const int32_t* n_tokens,
+                                  const void* k_pool, const void* v_pool, const int32_t* block_table,
+                                  const rapid_paged_kv* paged, const int32_t* ctx_lens, void* out,
+                                  const rapid_attn_shape* shape, const rapid_attn_params* params, void* workspace,
+                                  size_t workspace_bytes, void* cuda_stream) {
+    clear_error();
+    if (!paged || !block_table) {
+        set_error("rapid_prefill_attention_paged: NULL paged geometry or block table");
+        return RAPID_ERR_INVALID_ARG;
+    }
+    return launch_prefill_attention(q, q_rows, T, n_tokens, k_pool, v_pool, paged, block_table, ctx_lens, out, shape, params,
+                                    workspace, workspace_bytes, static_cast<cudaStream_t>(cuda_stream));
+}
+
 int rapid_rope_apply(const void* q, const rapid_kv_rows* q_rows, void* q_out, const rapid_kv_rows* q_out_rows,
                      const void* k, const rapid_kv_rows* k_rows, void* k_out, const rapid_kv_rows* k_out_rows, int B,
                      int T, int Hq, int Hkv, int D, const int32_t* positions, const rapid_rope* rope, int inverse,
