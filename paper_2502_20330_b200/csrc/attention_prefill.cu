@@ -40,7 +40,7 @@ namespace {
 constexpr int kKeys = 128;               // keys per tile
 constexpr int kThreads = 384;            // two softmax groups of 128; the producer, the walk, the MMA issuer, one warp idle
 constexpr int kHalfBytes = kKeys * 128;  // one 64-column half of a tile of 128 rows
-constexpr int kPoly = 3;                 // of 8 pairs of exponentials, those that the FMA pipe takes from the special-function unit
+constexpr int kPoly = 2;                 // of 8 pairs of exponentials, those that the FMA pipe takes from the special-function unit
 constexpr float kJump = 16.f;            // a score this far (log2) above a row's reference moves it
 constexpr int kMaxPrefillCtas = 256;
 constexpr int kPlanThreads = 512;        // at least the units of the tail: fewer than two for every CTA
@@ -273,6 +273,7 @@ struct Ring {
     Piece piece[kRing];
     Span span[kRing];
     uint64_t full[kRing], empty[kRing];
+    uint64_t taken;  // the producer has all copies of a piece under way: time to look for the next
 };
 
 __device__ __forceinline__ void tmem_wait_ld_of(uint32_t (&r)[32]) {  // (ties the registers to the wait)
@@ -303,7 +304,7 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
 
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t k_full[NK], k_empty[NK], v_full[NV], v_empty[NV];
-    __shared__ uint64_t q_full, q_empty, s_full[2], p_full[2], o_full[2], drain_bar;
+    __shared__ uint64_t q_full, q_empty, s_full[2], p_full[2][2], o_half[2], o_full[2], drain_bar;
     __shared__ uint32_t tmem_slot;
     __shared__ Ring ring;
     __shared__ int s_abort;
@@ -317,9 +318,16 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
         for (int i = 0; i < NV; ++i) mbar_init(&v_full[i], 1), mbar_init(&v_empty[i], 1);
         mbar_init(&q_full, 1);
         mbar_init(&q_empty, 1);
-        for (int i = 0; i < 2; ++i) mbar_init(&s_full[i], 1), mbar_init(&p_full[i], 4), mbar_init(&o_full[i], 1);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&s_full[i], 1);
+            mbar_init(&p_full[i][0], 4);
+            mbar_init(&p_full[i][1], 4);
+            mbar_init(&o_half[i], 1);
+            mbar_init(&o_full[i], 1);
+        }
         mbar_init(&drain_bar, 1);
         for (int i = 0; i < kRing; ++i) mbar_init(&ring.full[i], 1), mbar_init(&ring.empty[i], kRingUsers);
+        mbar_init(&ring.taken, 1);
         fence_mbar_init();
         s_abort = 0;
     }
@@ -409,7 +417,10 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                 __syncwarp();
                 ++n_v;
             }
-            if (lane == 0) mbar_arrive(&ring.empty[r % kRing]);
+            if (lane == 0) {
+                mbar_arrive(&ring.empty[r % kRing]);
+                mbar_arrive(&ring.taken);
+            }
             __syncwarp();
             ++r;
         }
@@ -425,6 +436,7 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
             const int s = k % kRing;
             if (k >= kRing && !warp_wait(&ring.empty[s], (k / kRing - 1) & 1, wc)) break;
             if (k > 0) {
+                if (!warp_wait(&ring.taken, (k - 1) & 1, wc)) break;
                 if (lane == 0) i = atomicAdd(&a.control->next, 1);
                 i = __shfl_sync(0xffffffffu, i, 0);
             }
@@ -470,14 +482,19 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                         if (s >= streams || !ok) continue;
                         const uint32_t tS = tmem + COL_S + 128u * s, tO = tmem + COL_O + 128u * s;
                         if (t > 0) {
-                            ok = mbar_wait_bounded(&p_full[s], p_par[s], wc);
-                            if (!ok) continue;
-                            p_par[s] ^= 1;
-                            tc_fence_after_sync();
                             const uint64_t vd = v_desc + (uint32_t)vs * (TILE >> 4);
 #pragma unroll
-                            for (int kk = 0; kk < kKeys / 16; ++kk)
-                                umma_bf16_ts(tO, tS + 8 * kk, vd + kk * (2048 >> 4), idesc_pv, (t > 1 || kk > 0) ? 1u : 0u);
+                            for (int h = 0; h < 2; ++h) {
+                                ok = ok && mbar_wait_bounded(&p_full[s][h], p_par[s], wc);
+                                if (!ok) continue;
+                                tc_fence_after_sync();
+#pragma unroll
+                                for (int kk = 4 * h; kk < 4 * h + 4; ++kk)
+                                    umma_bf16_ts(tO, tS + 8 * kk, vd + kk * (2048 >> 4), idesc_pv, (t > 1 || kk > 0) ? 1u : 0u);
+                                if (h == 0) umma_commit(&o_half[s]);
+                            }
+                            if (!ok) continue;
+                            p_par[s] ^= 1;
                             if (t == tiles) umma_commit(&o_full[s]);
                         }
                         if (t < tiles) {
@@ -544,77 +561,6 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                     const int u = g.first + t;
                     const int key0 = (u < sp.sinks ? u : sp.lo + u - sp.sinks) * kKeys;
                     tc_fence_after_sync();
-                    if (warp_valid) {
-                        const bool masked = key0 + kKeys - 1 > all_lim || (key0 < all_lo && key0 + kKeys > a.sink);
-                        bool known = t == 0;  // the references are in place for this tile
-                        uint32_t pk[kKeys / 2];
-                        uint64_t acc[2];
-                        while (true) {
-                            if (known) {
-                                float top = -INFINITY;
-    #pragma unroll 1
-                                for (int q = 0; q < kKeys / 32; ++q) {
-                                    uint32_t x[32];
-                                    tmem_ld_x32(tS + 32 * q, x);
-                                    tmem_wait_ld_of(x);
-                                    uint32_t seen = 0xffffffffu;
-                                    if (masked) seen = bits(wlo - key0 - 32 * q, lim - key0 - 32 * q) | bits(0, min(a.sink - 1, lim) - key0 - 32 * q);
-    #pragma unroll
-                                    for (int k = 0; k < 32; ++k) {
-                                        const float s = seen >> k & 1 ? __uint_as_float(x[k]) : -INFINITY;
-                                        top = max3(top, s, s);
-                                    }
-                                }
-                                top *= c;
-                                const bool move = row_valid && !(top <= m_ref + kJump) && top != -INFINITY;
-                                const float factor = move ? fast_exp2(m_ref - top) : 1.f;  // 0 when there was no reference
-                                if (move) {
-                                    l_run *= factor;
-                                    m_ref = top;
-                                }
-                                if (t > 0 && __any_sync(0xffffffffu, move)) scale_o<D>(tO, factor);
-                            }
-                            const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
-                            const uint64_t c2 = f32x2(c, c), m2 = f32x2(-m_use, -m_use);
-                            float mx[2] = {-INFINITY, -INFINITY};
-                            acc[0] = acc[1] = 0;
-    #pragma unroll
-                            for (int q = 0; q < kKeys / 32; ++q) {
-                                uint32_t x[32];
-                                tmem_ld_x32(tS + 32 * q, x);
-                                tmem_wait_ld_of(x);
-                                if (masked) {
-                                    const uint32_t seen = bits(wlo - key0 - 32 * q, lim - key0 - 32 * q) | bits(0, min(a.sink - 1, lim) - key0 - 32 * q);
-    #pragma unroll
-                                    for (int k = 0; k < 32; ++k)
-                                        if (!(seen >> k & 1)) x[k] = __float_as_uint(-INFINITY);
-                                }
-    #pragma unroll
-                                for (int k = 0; k < 32; k += 2) {
-                                    float p0, p1;
-                                    mx[(k >> 1) & 1] = max3(mx[(k >> 1) & 1], __uint_as_float(x[k]), __uint_as_float(x[k + 1]));
-                                    f32x2_split(f32x2_fma(f32x2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), c2, m2), p0, p1);
-                                    if ((k >> 1) % 8 < kPoly) {
-                                        exp2_poly(p0, p1);
-                                    } else {
-                                        p0 = fast_exp2(p0);
-                                        p1 = fast_exp2(p1);
-                                    }
-                                    acc[(k >> 1) & 1] = f32x2_add(acc[(k >> 1) & 1], f32x2(p0, p1));
-                                    pk[16 * q + (k >> 1)] = pack_bf16x2(p0, p1);
-                                }
-                            }
-                            if (known) break;
-                            const float top = max3(mx[0], mx[1], mx[1]) * c;
-                            if (!__any_sync(0xffffffffu, row_valid && !(top <= m_ref + kJump) && top != -INFINITY)) break;
-                            known = true;
-                        }
-                        tmem_st_x32(tS, reinterpret_cast<const uint32_t(&)[32]>(pk[0]));
-                        tmem_st_x32(tS + 32, reinterpret_cast<const uint32_t(&)[32]>(pk[32]));
-                        float s0, s1;
-                        f32x2_split(f32x2_add(acc[0], acc[1]), s0, s1);
-                        l_run += s0 + s1;
-                    }
                     if (stream == 0 && key0 + kKeys > g.L) {
                         // V rows past the keys may hold any bits: zero them so that 0 * row = 0 (stream 1's PV goes out behind stream 0's)
                         const int vt = n_tiles + t, vs = vt % NV;
@@ -629,10 +575,88 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                                     make_uint4(0, 0, 0, 0);
                         fence_proxy_async_smem();
                     }
-                    tmem_wait_st();
-                    tc_fence_before_sync();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&p_full[stream]);
+                    const bool masked = key0 + kKeys - 1 > all_lim || (key0 < all_lo && key0 + kKeys > a.sink);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        if (warp_valid) {
+                            const uint32_t tX = tS + 64 * h;
+                            uint32_t seen[2] = {0xffffffffu, 0xffffffffu};
+                            if (masked) {
+#pragma unroll
+                                for (int q = 0; q < 2; ++q) {
+                                    const int k0 = key0 + 64 * h + 32 * q;
+                                    seen[q] = bits(wlo - k0, lim - k0) | bits(0, min(a.sink - 1, lim) - k0);
+                                }
+                            }
+                            bool known = t == 0 && h == 0;  // the references are in place for these scores
+                            uint32_t pk[32];
+                            uint64_t acc[2];
+                            while (true) {
+                                uint32_t x[2][32];
+                                tmem_ld_x32(tX, x[0]);
+                                tmem_ld_x32(tX + 32, x[1]);
+                                tmem_wait_ld_of(x[0]);
+                                tmem_wait_ld_of(x[1]);
+                                if (masked) {
+#pragma unroll
+                                    for (int k = 0; k < 64; ++k)
+                                        if (!(seen[k >> 5] >> (k & 31) & 1)) x[k >> 5][k & 31] = __float_as_uint(-INFINITY);
+                                }
+                                float mx[2] = {-INFINITY, -INFINITY};
+                                if (known) {
+#pragma unroll
+                                    for (int k = 0; k < 64; k += 2)
+                                        mx[(k >> 1) & 1] = max3(mx[(k >> 1) & 1], __uint_as_float(x[k >> 5][k & 31]), __uint_as_float(x[k >> 5][(k & 31) + 1]));
+                                    const float top = max3(mx[0], mx[1], mx[1]) * c;
+                                    const bool move = row_valid && !(top <= m_ref + kJump) && top != -INFINITY;
+                                    const float factor = move ? fast_exp2(m_ref - top) : 1.f;  // 0 when there was no reference
+                                    if (move) {
+                                        l_run *= factor;
+                                        m_ref = top;
+                                    }
+                                    if ((t > 0 || h > 0) && __any_sync(0xffffffffu, move)) {
+                                        if (h > 0) {  // O at rest: the PV of the tile's first half has completed
+                                            ok = warp_wait(&o_half[stream], j & 1, wc);
+                                            tc_fence_after_sync();
+                                        }
+                                        if (ok) scale_o<D>(tO, factor);
+                                    }
+                                }
+                                const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
+                                const uint64_t c2 = f32x2(c, c), m2 = f32x2(-m_use, -m_use);
+                                acc[0] = acc[1] = 0;
+#pragma unroll
+                                for (int k = 0; k < 64; k += 2) {
+                                    const float x0 = __uint_as_float(x[k >> 5][k & 31]), x1 = __uint_as_float(x[k >> 5][(k & 31) + 1]);
+                                    float p0, p1;
+                                    mx[(k >> 1) & 1] = max3(mx[(k >> 1) & 1], x0, x1);
+                                    f32x2_split(f32x2_fma(f32x2(x0, x1), c2, m2), p0, p1);
+                                    if ((k >> 1) % 8 < kPoly) {
+                                        exp2_poly(p0, p1);
+                                    } else {
+                                        p0 = fast_exp2(p0);
+                                        p1 = fast_exp2(p1);
+                                    }
+                                    acc[(k >> 1) & 1] = f32x2_add(acc[(k >> 1) & 1], f32x2(p0, p1));
+                                    pk[k >> 1] = pack_bf16x2(p0, p1);
+                                }
+                                if (known) break;
+                                const float top = max3(mx[0], mx[1], mx[1]) * c;
+                                if (!__any_sync(0xffffffffu, row_valid && !(top <= m_ref + kJump) && top != -INFINITY)) break;
+                                known = true;
+                            }
+                            if (!ok) break;
+                            tmem_st_x32(tS + 32 * h, pk);
+                            float s0, s1;
+                            f32x2_split(f32x2_add(acc[0], acc[1]), s0, s1);
+                            l_run += s0 + s1;
+                        }
+                        tmem_wait_st();
+                        tc_fence_before_sync();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&p_full[stream][h]);
+                    }
+                    if (!ok) break;
                 }
                 if (!ok) break;
                 // ---- the end of the piece ----
