@@ -5,7 +5,7 @@
 //
 // The G query heads of a KV head share its keys, so a row tile (the M axis of the MMAs, 128 rows) is 128 / G neighbouring
 // rows of all G heads.  A unit is one KV head of one sequence and two row tiles, which go through the same K/V tiles of 128 keys:
-// stream s (four softmax warps, S and O accumulators) has row tile s.
+// stream s (eight softmax warps, S and O accumulators) has row tile s.
 //
 //   S_s[128 x 128] = Q_s K^T   A = Q tile, B = K tile, both K-major in shared memory
 //   O_s[128 x D]  += P_s V     A = P (bf16, over the first half of S_s's columns), B = V tile, MN-major
@@ -14,7 +14,9 @@
 // the other are at theirs.  It works them off in that order, so the QK^T that overwrites S_s goes out right behind the PV that reads P
 // from it, and scores in hand mean that the PV before them has completed.
 //
-// Softmax.  A row's reference moves only when a score is 2^16 above it, so the exponentials of a tile need not wait for its maximum: they
+// Softmax.  Four warps have a quarter of a stream's rows and half of a tile's keys each, four the other half: with one warp for both halves a
+// tile took half as long again (646 us for 554 at 8,192 rows), two warps to a scheduler being too few to hide tensor memory's
+// latency.  The two warps of a quarter meet once a tile.  A row's reference moves only when a score is 2^16 above it, so the exponentials of a tile need not wait for its maximum: they
 // go by the reference in place, the maximum is found on the way, and a tile that moves a reference (the first of a unit, hardly any
 // other) is done over; nothing of it was stored.
 //
@@ -38,9 +40,9 @@ namespace rapid {
 namespace {
 
 constexpr int kKeys = 128;               // keys per tile
-constexpr int kThreads = 384;            // two softmax groups of 128; the producer, the walk, the MMA issuer, one warp idle
+constexpr int kSoftmaxWarps = 16;        // of each stream eight: four quarters of the rows by two halves of the keys
+constexpr int kThreads = 32 * (kSoftmaxWarps + 3);  // and the producer, the walk, the MMA issuer
 constexpr int kHalfBytes = kKeys * 128;  // one 64-column half of a tile of 128 rows
-constexpr int kPoly = 2;                 // of 8 pairs of exponentials, those that the FMA pipe takes from the special-function unit
 constexpr float kJump = 16.f;            // a score this far (log2) above a row's reference moves it
 constexpr int kMaxPrefillCtas = 256;
 constexpr int kPlanThreads = 512;        // at least the units of the tail: fewer than two for every CTA
@@ -53,8 +55,6 @@ constexpr int kMaxUnits = 1 << 24;
 __host__ __device__ constexpr int k_slots(int D) { return D == 128 ? 2 : 4; }
 __host__ __device__ constexpr int v_slots(int D) { return D == 128 ? 3 : 6; }
 __host__ __device__ constexpr int tile_bytes(int D) { return (D / 64) * kHalfBytes; }
-__host__ __device__ constexpr int smem_bytes(int D) { return (2 + k_slots(D) + v_slots(D)) * tile_bytes(D) + 1024; }
-
 // A piece of work: `tiles` tiles of a unit from the first-th of its list on (-1 tiles: the end).  slot < 0: the whole unit, whose
 // output is written; else a partial goes into that slot.
 struct __align__(16) Piece {
@@ -266,15 +266,28 @@ __global__ void __launch_bounds__(kPlanThreads) prefill_plan_kernel(const __grid
     if (tid == 0) *a.control = {a.num_ctas, whole + pieces, cuts, 0};
 }
 
-constexpr int kRing = 2;        // pieces a CTA has in hand: the one at work and the next
-constexpr int kRingUsers = 10;  // arrivals that free one: 8 softmax warps, the producer, the MMA issuer
+constexpr int kRing = 2;                          // pieces a CTA has in hand: the one at work and the next
+constexpr int kRingUsers = kSoftmaxWarps + 2;     // arrivals that free one: the softmax warps, the producer, the MMA issuer
 
-struct Ring {
+// What the roles share, behind the tiles in shared memory.
+template <int D>
+struct Shared {
     Piece piece[kRing];
     Span span[kRing];
-    uint64_t full[kRing], empty[kRing];
+    uint64_t ring_full[kRing], ring_empty[kRing];
     uint64_t taken;  // the producer has all copies of a piece under way: time to look for the next
+    uint64_t k_full[k_slots(D)], k_empty[k_slots(D)], v_full[v_slots(D)], v_empty[v_slots(D)];
+    uint64_t q_full, q_empty, s_full[2], p_full[2], o_full[2], drain;
+    uint64_t pair[2][4];              // the two warps that share a quarter of a stream's rows
+    uint32_t flag[2][2][2][4];        // [turn][stream][half][quarter]: a score outgrew its row's reference
+    float sum[2][2][128];             // [stream][half][row]
+    uint32_t tmem;
+    int abort;
 };
+template <int D>
+constexpr int smem_bytes() {
+    return (2 + k_slots(D) + v_slots(D)) * tile_bytes(D) + (int)sizeof(Shared<D>);
+}
 
 __device__ __forceinline__ void tmem_wait_ld_of(uint32_t (&r)[32]) {  // (ties the registers to the wait)
     asm volatile("tcgen05.wait::ld.sync.aligned;"
@@ -299,63 +312,61 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
     constexpr int NH = D / 64;
     constexpr int NK = k_slots(D), NV = v_slots(D);
     constexpr uint32_t TILE = tile_bytes(D);
-    constexpr uint32_t OFF_Q = 0, OFF_K = 2 * TILE, OFF_V = OFF_K + NK * TILE;
+    constexpr uint32_t OFF_Q = 0, OFF_K = 2 * TILE, OFF_V = OFF_K + NK * TILE, OFF_SHARED = OFF_V + NV * TILE;
     constexpr uint32_t TMEM_COLS = 512, COL_S = 0, COL_O = 256;  // stream s: S at COL_S + 128 s, O at COL_O + 128 s
+    constexpr int kProducer = kSoftmaxWarps, kWalk = kProducer + 1, kIssuer = kProducer + 2;
 
-    extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t k_full[NK], k_empty[NK], v_full[NV], v_empty[NV];
-    __shared__ uint64_t q_full, q_empty, s_full[2], p_full[2][2], o_half[2], o_full[2], drain_bar;
-    __shared__ uint32_t tmem_slot;
-    __shared__ Ring ring;
-    __shared__ int s_abort;
-
-    const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    uint8_t* smem = smem_raw + (smem_base - smem_u32(smem_raw));
+    extern __shared__ __align__(1024) uint8_t smem[];
+    const uint32_t smem_base = smem_u32(smem);
+    Shared<D>& sh = *reinterpret_cast<Shared<D>*>(smem + OFF_SHARED);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (smem_base & 1023) {  // (the swizzled tiles need it; the declaration asks for it)
+        if (threadIdx.x == 0) atomicOr(a.status, RAPID_STATUS_PIPELINE_TIMEOUT);
+        return;
+    }
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < NK; ++i) mbar_init(&k_full[i], 1), mbar_init(&k_empty[i], 1);
-        for (int i = 0; i < NV; ++i) mbar_init(&v_full[i], 1), mbar_init(&v_empty[i], 1);
-        mbar_init(&q_full, 1);
-        mbar_init(&q_empty, 1);
+        for (int i = 0; i < NK; ++i) mbar_init(&sh.k_full[i], 1), mbar_init(&sh.k_empty[i], 1);
+        for (int i = 0; i < NV; ++i) mbar_init(&sh.v_full[i], 1), mbar_init(&sh.v_empty[i], 1);
+        mbar_init(&sh.q_full, 1);
+        mbar_init(&sh.q_empty, 1);
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&s_full[i], 1);
-            mbar_init(&p_full[i][0], 4);
-            mbar_init(&p_full[i][1], 4);
-            mbar_init(&o_half[i], 1);
-            mbar_init(&o_full[i], 1);
+            mbar_init(&sh.s_full[i], 1);
+            mbar_init(&sh.p_full[i], kSoftmaxWarps / 2);
+            mbar_init(&sh.o_full[i], 1);
+            for (int q = 0; q < 4; ++q) mbar_init(&sh.pair[i][q], 2);
         }
-        mbar_init(&drain_bar, 1);
-        for (int i = 0; i < kRing; ++i) mbar_init(&ring.full[i], 1), mbar_init(&ring.empty[i], kRingUsers);
-        mbar_init(&ring.taken, 1);
+        mbar_init(&sh.drain, 1);
+        for (int i = 0; i < kRing; ++i) mbar_init(&sh.ring_full[i], 1), mbar_init(&sh.ring_empty[i], kRingUsers);
+        mbar_init(&sh.taken, 1);
         fence_mbar_init();
-        s_abort = 0;
+        sh.abort = 0;
     }
-    if (warp == 8 && lane == 0) {
+    if (warp == kProducer && lane == 0) {
         prefetch_tensormap(&tmK);
         prefetch_tensormap(&tmV);
         prefetch_tensormap(&tmQ);
     }
-    if (warp == 10) tmem_alloc(&tmem_slot, TMEM_COLS);  // the same warp frees it
+    if (warp == kIssuer) tmem_alloc(&sh.tmem, TMEM_COLS);  // the same warp frees it
     griddep_wait();
     griddep_launch_dependents();
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
-    const uint32_t tmem = tmem_slot;
-    const WaitCtx wc = {&s_abort, a.wait_limit};
+    const uint32_t tmem = sh.tmem;
+    const WaitCtx wc = {&sh.abort, a.wait_limit};
 
     int r = 0;  // pieces taken from the ring; a role that comes to the end marker, or whose wait runs out, stops
-    if (warp == 8) {
+    if (warp == kProducer) {
         // ---------------- producer: the unit's Q tiles and its K/V tiles ----------------
         int n_q = 0, n_k = 0, n_v = 0;  // copies issued
         const int parts = kKeys / a.box_rows;
         const uint32_t part_bytes = kHalfBytes / parts;
         bool ok = true;
         while (ok) {
-            ok = warp_wait(&ring.full[r % kRing], (r / kRing) & 1, wc);
-            const Piece g = ring.piece[r % kRing];
-            const Span sp = ring.span[r % kRing];
+            ok = warp_wait(&sh.ring_full[r % kRing], (r / kRing) & 1, wc);
+            const Piece g = sh.piece[r % kRing];
+            const Span sp = sh.span[r % kRing];
             if (!ok || g.tiles < 0) break;
             for (int t = 0; t < g.tiles && ok; ++t) {
                 const int u = g.first + t;
@@ -377,172 +388,174 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                     }
                 }
                 const int ks = n_k % NK, vs = n_v % NV;
-                if (n_k >= NK) ok = warp_wait(&k_empty[ks], (n_k / NK - 1) & 1, wc);
+                if (n_k >= NK) ok = warp_wait(&sh.k_empty[ks], (n_k / NK - 1) & 1, wc);
                 if (!ok) break;
                 if (elect_one()) {
-                    mbar_arrive_expect_tx(&k_full[ks], TILE);
+                    mbar_arrive_expect_tx(&sh.k_full[ks], TILE);
                     for (int q = 0; q < parts; ++q)
 #pragma unroll
                         for (int h = 0; h < NH; ++h)
-                            tma_load_4d(smem + OFF_K + ks * TILE + h * kHalfBytes + q * part_bytes, &tmK, &k_full[ks],
+                            tma_load_4d(smem + OFF_K + ks * TILE + h * kHalfBytes + q * part_bytes, &tmK, &sh.k_full[ks],
                                         h * 64, c1[q], g.kvh, c3[q]);
                 }
                 __syncwarp();
                 ++n_k;
                 if (t == 0) {  // (behind the first K tile, which need not wait for the unit before)
-                    if (n_q > 0) ok = warp_wait(&q_empty, (n_q - 1) & 1, wc);
+                    if (n_q > 0) ok = warp_wait(&sh.q_empty, (n_q - 1) & 1, wc);
                     if (!ok) break;
                     const int streams = g.n - g.row0 > a.rows_tile ? 2 : 1;
                     if (elect_one()) {
-                        mbar_arrive_expect_tx(&q_full, (uint32_t)(streams * a.rows_tile * a.G * D * 2));
+                        mbar_arrive_expect_tx(&sh.q_full, (uint32_t)(streams * a.rows_tile * a.G * D * 2));
                         for (int s = 0; s < streams; ++s)
 #pragma unroll
                             for (int h = 0; h < NH; ++h)
-                                tma_load_4d(smem + OFF_Q + s * TILE + h * kHalfBytes, &tmQ, &q_full, h * 64, g.kvh * a.G,
+                                tma_load_4d(smem + OFF_Q + s * TILE + h * kHalfBytes, &tmQ, &sh.q_full, h * 64, g.kvh * a.G,
                                             g.row0 + s * a.rows_tile, g.b);
                     }
                     __syncwarp();
                     ++n_q;
                 }
-                if (n_v >= NV) ok = warp_wait(&v_empty[vs], (n_v / NV - 1) & 1, wc);
+                if (n_v >= NV) ok = warp_wait(&sh.v_empty[vs], (n_v / NV - 1) & 1, wc);
                 if (!ok) break;
                 if (elect_one()) {
-                    mbar_arrive_expect_tx(&v_full[vs], TILE);
+                    mbar_arrive_expect_tx(&sh.v_full[vs], TILE);
                     for (int q = 0; q < parts; ++q)
 #pragma unroll
                         for (int h = 0; h < NH; ++h)
-                            tma_load_4d(smem + OFF_V + vs * TILE + h * kHalfBytes + q * part_bytes, &tmV, &v_full[vs],
+                            tma_load_4d(smem + OFF_V + vs * TILE + h * kHalfBytes + q * part_bytes, &tmV, &sh.v_full[vs],
                                         h * 64, c1[q], g.kvh, c3[q]);
                 }
                 __syncwarp();
                 ++n_v;
             }
             if (lane == 0) {
-                mbar_arrive(&ring.empty[r % kRing]);
-                mbar_arrive(&ring.taken);
+                mbar_arrive(&sh.ring_empty[r % kRing]);
+                mbar_arrive(&sh.taken);
             }
             __syncwarp();
             ++r;
         }
         // every copy lands before the CTA gives up its shared memory, whoever may have given up waiting for it
-        if (n_q > 0) mbar_wait_drain(&q_full, (n_q - 1) & 1);
-        for (int s = 0; s < NK && s < n_k; ++s) mbar_wait_drain(&k_full[(n_k - 1 - s) % NK], ((n_k - 1 - s) / NK) & 1);
-        for (int s = 0; s < NV && s < n_v; ++s) mbar_wait_drain(&v_full[(n_v - 1 - s) % NV], ((n_v - 1 - s) / NV) & 1);
-    } else if (warp == 9) {
+        if (n_q > 0) mbar_wait_drain(&sh.q_full, (n_q - 1) & 1);
+        for (int s = 0; s < NK && s < n_k; ++s) mbar_wait_drain(&sh.k_full[(n_k - 1 - s) % NK], ((n_k - 1 - s) / NK) & 1);
+        for (int s = 0; s < NV && s < n_v; ++s) mbar_wait_drain(&sh.v_full[(n_v - 1 - s) % NV], ((n_v - 1 - s) / NV) & 1);
+    } else if (warp == kWalk) {
         // ---------------- the walk: pieces from the list into the ring ----------------
         const int pieces = a.control->pieces;
         int i = blockIdx.x;
         for (int k = 0;; ++k) {
             const int s = k % kRing;
-            if (k >= kRing && !warp_wait(&ring.empty[s], (k / kRing - 1) & 1, wc)) break;
+            if (k >= kRing && !warp_wait(&sh.ring_empty[s], (k / kRing - 1) & 1, wc)) break;
             if (k > 0) {
-                if (!warp_wait(&ring.taken, (k - 1) & 1, wc)) break;
+                if (!warp_wait(&sh.taken, (k - 1) & 1, wc)) break;
                 if (lane == 0) i = atomicAdd(&a.control->next, 1);
                 i = __shfl_sync(0xffffffffu, i, 0);
             }
             if (lane == 0) {
                 if (i < pieces) {
                     const Piece g = a.pieces[i];
-                    ring.piece[s] = g;
-                    ring.span[s] = span_of(a, g.row0, g.n, g.L);
+                    sh.piece[s] = g;
+                    sh.span[s] = span_of(a, g.row0, g.n, g.L);
                 } else {
-                    ring.piece[s].tiles = -1;
+                    sh.piece[s].tiles = -1;
                 }
-                mbar_arrive(&ring.full[s]);
+                mbar_arrive(&sh.ring_full[s]);
             }
             __syncwarp();
             if (i >= pieces) break;
         }
-    } else if (warp == 10) {
-        // ---------------- MMA issuer: one thread, alone in this branch: what is called here is inlined, no function is ----------------
-        if (elect_one()) {
-            constexpr uint32_t idesc_qk = umma_idesc_bf16(128, kKeys, 0, 0);
-            constexpr uint32_t idesc_pv = umma_idesc_bf16(128, D, 0, 1);
-            const uint64_t q_desc = umma_smem_desc(smem_base + OFF_Q, 16, 1024);
-            const uint64_t k_desc = umma_smem_desc(smem_base + OFF_K, 16, 1024);
-            const uint64_t v_desc = umma_smem_desc(smem_base + OFF_V, kHalfBytes, 1024);
-            int n_q = 0, ks = 0, k_par = 0, vs = 0, v_par = 0;
-            int p_par[2] = {0, 0};
-            bool ok = true;
-            while (ok) {
-                ok = mbar_wait_bounded(&ring.full[r % kRing], (r / kRing) & 1, wc);
-                if (!ok) break;
-                const int tiles = ring.piece[r % kRing].tiles;
-                const int streams = ring.piece[r % kRing].n - ring.piece[r % kRing].row0 > a.rows_tile ? 2 : 1;
-                if (tiles < 0) break;
-                if (tiles > 0) {
-                    ok = mbar_wait_bounded(&q_full, n_q & 1, wc);
-                    ++n_q;
-                }
-                for (int t = 0; t <= tiles && tiles > 0 && ok; ++t) {
-                    if (t < tiles) ok = mbar_wait_bounded(&k_full[ks], k_par, wc);
-                    if (ok && t > 0) ok = mbar_wait_bounded(&v_full[vs], v_par, wc);
+    } else if (warp == kIssuer) {
+        // ---------------- MMA issuer: a warp in step, of which one lane issues ----------------
+        constexpr uint32_t idesc_qk = umma_idesc_bf16(128, kKeys, 0, 0);
+        constexpr uint32_t idesc_pv = umma_idesc_bf16(128, D, 0, 1);
+        const bool leader = elect_one();
+        const uint64_t q_desc = umma_smem_desc(smem_base + OFF_Q, 16, 1024);
+        const uint64_t k_desc = umma_smem_desc(smem_base + OFF_K, 16, 1024);
+        const uint64_t v_desc = umma_smem_desc(smem_base + OFF_V, kHalfBytes, 1024);
+        int n_q = 0, n_k = 0, n_v = 0;  // units and tiles so far
+        int p_par[2] = {0, 0};
+        bool ok = true;
+        while (ok) {
+            ok = warp_wait(&sh.ring_full[r % kRing], (r / kRing) & 1, wc);
+            const int tiles = __shfl_sync(0xffffffffu, sh.piece[r % kRing].tiles, 0);
+            const int streams = __shfl_sync(0xffffffffu, sh.piece[r % kRing].n - sh.piece[r % kRing].row0, 0) > a.rows_tile ? 2 : 1;
+            if (!ok || tiles < 0) break;
+            if (tiles > 0) {
+                ok = warp_wait(&sh.q_full, n_q & 1, wc);
+                ++n_q;
+            }
+            for (int t = 0; t <= tiles && tiles > 0 && ok; ++t) {
+                const int ks = n_k % NK, vs = n_v % NV;
 #pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        if (s >= streams || !ok) continue;
-                        const uint32_t tS = tmem + COL_S + 128u * s, tO = tmem + COL_O + 128u * s;
-                        if (t > 0) {
+                for (int s = 0; s < 2; ++s) {
+                    if (s >= streams) continue;
+                    const uint32_t tS = tmem + COL_S + 128u * s, tO = tmem + COL_O + 128u * s;
+                    if (t > 0) {
+                        if (s == 0) ok = ok && warp_wait(&sh.v_full[vs], (n_v / NV) & 1, wc);
+                        ok = ok && warp_wait(&sh.p_full[s], p_par[s], wc);
+                        p_par[s] ^= 1;
+                        tc_fence_after_sync();
+                        if (ok && leader) {
                             const uint64_t vd = v_desc + (uint32_t)vs * (TILE >> 4);
 #pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                ok = ok && mbar_wait_bounded(&p_full[s][h], p_par[s], wc);
-                                if (!ok) continue;
-                                tc_fence_after_sync();
-#pragma unroll
-                                for (int kk = 4 * h; kk < 4 * h + 4; ++kk)
-                                    umma_bf16_ts(tO, tS + 8 * kk, vd + kk * (2048 >> 4), idesc_pv, (t > 1 || kk > 0) ? 1u : 0u);
-                                if (h == 0) umma_commit(&o_half[s]);
-                            }
-                            if (!ok) continue;
-                            p_par[s] ^= 1;
-                            if (t == tiles) umma_commit(&o_full[s]);
+                            for (int kk = 0; kk < kKeys / 16; ++kk)
+                                umma_bf16_ts(tO, tS + 8 * kk, vd + kk * (2048 >> 4), idesc_pv, (t > 1 || kk > 0) ? 1u : 0u);
+                            if (t == tiles) umma_commit(&sh.o_full[s]);
                         }
-                        if (t < tiles) {
-                            tc_fence_after_sync();
+                        __syncwarp();
+                    }
+                    if (t < tiles) {
+                        if (s == 0) ok = ok && warp_wait(&sh.k_full[ks], (n_k / NK) & 1, wc);
+                        tc_fence_after_sync();
+                        if (ok && leader) {
                             const uint64_t qd = q_desc + (uint32_t)s * (TILE >> 4), kd = k_desc + (uint32_t)ks * (TILE >> 4);
 #pragma unroll
                             for (int kk = 0; kk < D / 16; ++kk) {
                                 const uint32_t off = (kk >> 2) * (kHalfBytes >> 4) + (kk & 3) * 2;
                                 umma_bf16_ss(tS, qd + off, kd + off, idesc_qk, kk > 0);
                             }
-                            umma_commit(&s_full[s]);
+                            umma_commit(&sh.s_full[s]);
                         }
-                    }
-                    if (!ok) break;
-                    if (t < tiles) {
-                        umma_commit(&k_empty[ks]);
-                        if (++ks == NK) ks = 0, k_par ^= 1;
-                        if (t == tiles - 1) umma_commit(&q_empty);
-                    }
-                    if (t > 0) {
-                        umma_commit(&v_empty[vs]);
-                        if (++vs == NV) vs = 0, v_par ^= 1;
+                        __syncwarp();
                     }
                 }
-                if (!ok) break;
-                mbar_arrive(&ring.empty[r % kRing]);
-                ++r;
+                if (ok && leader) {
+                    if (t < tiles) umma_commit(&sh.k_empty[ks]);
+                    if (t == tiles - 1) umma_commit(&sh.q_empty);
+                    if (t > 0) umma_commit(&sh.v_empty[vs]);
+                }
+                __syncwarp();
+                n_k += t < tiles;
+                n_v += t > 0;
             }
-            // every MMA issued here has completed before tensor memory is freed
-            umma_commit(&drain_bar);
+            if (!ok) break;
+            if (lane == 0) mbar_arrive(&sh.ring_empty[r % kRing]);
+            __syncwarp();
+            ++r;
+        }
+        // every MMA issued here has completed before tensor memory is freed
+        if (leader) {
+            umma_commit(&sh.drain);
             const long long t0 = clock64();
-            while (!mbar_try_wait(&drain_bar, 0) && clock64() - t0 < kWaitCycleLimit) {}
+            while (!mbar_try_wait(&sh.drain, 0) && clock64() - t0 < kWaitCycleLimit) {}
         }
         __syncwarp();
-    } else if (warp < 8) {
-        // ---------------- softmax warps: stream = warp / 4, row of the tile = 32 (warp % 4) + lane ----------------
-        const int stream = warp >> 2;
-        const int row = (warp & 3) * 32 + lane;
-        const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t tS = tmem + lane_base + COL_S + 128u * stream, tO = tmem + lane_base + COL_O + 128u * stream;
+    } else {
+        // ---------------- softmax warps: stream, half of a tile's keys, quarter of its rows ----------------
+        const int stream = warp >> 3, half = warp >> 2 & 1, quarter = warp & 3;
+        const int row = quarter * 32 + lane;
+        const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
+        const uint32_t tS = tmem + lane_base + COL_S + 128u * stream, tO = tmem + lane_base + COL_O + 128u * stream + half * (D / 2);
+        uint64_t* pair = &sh.pair[stream][quarter];
         const float c = a.scale_log2;
         const int row_t = row / a.G, row_h = row - row_t * a.G;  // row of the sequence within the tile, head in the group
         int j = 0, n_tiles = 0, done = 0;  // tiles of this stream, tiles of the CTA before the piece, pieces of this stream
+        int met = 0;                       // times that the two warps of a quarter have met
         bool ok = true;
         while (ok) {
-            ok = warp_wait(&ring.full[r % kRing], (r / kRing) & 1, wc);
-            const Piece g = ring.piece[r % kRing];
-            const Span sp = ring.span[r % kRing];
+            ok = warp_wait(&sh.ring_full[r % kRing], (r / kRing) & 1, wc);
+            const Piece g = sh.piece[r % kRing];
+            const Span sp = sh.span[r % kRing];
             if (!ok || g.tiles < 0) break;
             const int i0 = g.row0 + stream * a.rows_tile;  // the tile's first row of the sequence
             if (i0 < g.n) {
@@ -556,115 +569,132 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                 const int all_lo = a.window ? p0 + a.rows_tile - 1 - a.window + 1 : 0;
                 float m_ref = -INFINITY, l_run = 0.f;
                 for (int t = 0; t < g.tiles; ++t, ++j) {
-                    ok = warp_wait(&s_full[stream], j & 1, wc);
+                    ok = warp_wait(&sh.s_full[stream], j & 1, wc);
                     if (!ok) break;
                     const int u = g.first + t;
                     const int key0 = (u < sp.sinks ? u : sp.lo + u - sp.sinks) * kKeys;
                     tc_fence_after_sync();
-                    if (stream == 0 && key0 + kKeys > g.L) {
-                        // V rows past the keys may hold any bits: zero them so that 0 * row = 0 (stream 1's PV goes out behind stream 0's)
+                    if (warp_valid) {
+                        const bool masked = key0 + kKeys - 1 > all_lim || (key0 < all_lo && key0 + kKeys > a.sink);
+                        uint32_t x[32], pk[32];
+                        float mx[2];
+                        uint64_t acc[2];
+                        auto load = [&](int q) {  // the scores of keys 32 q .. 32 q + 31 of the tile, those out of sight -inf
+                            tmem_ld_x32(tS + 32 * q, x);
+                            tmem_wait_ld_of(x);
+                            if (masked) {
+                                const int k0 = key0 + 32 * q;
+                                const uint32_t seen = bits(wlo - k0, lim - k0) | bits(0, min(a.sink - 1, lim) - k0);
+#pragma unroll
+                                for (int k = 0; k < 32; ++k)
+                                    if (!(seen >> k & 1)) x[k] = __float_as_uint(-INFINITY);
+                            }
+                        };
+                        auto largest = [&] {
+#pragma unroll
+                            for (int k = 0; k < 32; k += 2) mx[(k >> 1) & 1] = max3(mx[(k >> 1) & 1], __uint_as_float(x[k]), __uint_as_float(x[k + 1]));
+                        };
+                        auto weigh = [&](int at) {  // by the reference in place
+                            const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
+                            const uint64_t c2 = f32x2(c, c), m2 = f32x2(-m_use, -m_use);
+#pragma unroll
+                            for (int k = 0; k < 32; k += 2) {
+                                float p0, p1;
+                                f32x2_split(f32x2_fma(f32x2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), c2, m2), p0, p1);
+                                p0 = fast_exp2(p0);
+                                p1 = fast_exp2(p1);
+                                acc[(k >> 1) & 1] = f32x2_add(acc[(k >> 1) & 1], f32x2(p0, p1));
+                                pk[at + (k >> 1)] = pack_bf16x2(p0, p1);
+                            }
+                        };
+                        bool again = t == 0;  // no references yet
+                        if (!again) {
+                            acc[0] = acc[1] = 0;
+                            mx[0] = mx[1] = -INFINITY;
+                            load(2 * half);
+                            largest();
+                            weigh(0);
+                            load(2 * half + 1);
+                            largest();
+                            weigh(16);
+                            const float top = max3(mx[0], mx[1], mx[1]) * c;
+                            again = __any_sync(0xffffffffu, row_valid && !(top <= m_ref + kJump) && top != -INFINITY);
+                            // the other half of the keys; and neither warp writes over scores that the other has not read
+                            if (lane == 0) {
+                                sh.flag[met & 1][stream][half][quarter] = again;
+                                mbar_arrive(pair);
+                            }
+                            ok = warp_wait(pair, met & 1, wc);
+                            if (!ok) break;
+                            again |= *(volatile uint32_t*)&sh.flag[met & 1][stream][half ^ 1][quarter] != 0;
+                            ++met;
+                        }
+                        if (again) {  // the references first, by the whole row, then the probabilities once more
+                            mx[0] = mx[1] = -INFINITY;
+#pragma unroll 1
+                            for (int q = 0; q < kKeys / 32; ++q) {
+                                load(q);
+                                largest();
+                            }
+                            const float top = max3(mx[0], mx[1], mx[1]) * c;
+                            const bool move = row_valid && !(top <= m_ref + kJump) && top != -INFINITY;
+                            const float factor = move ? fast_exp2(m_ref - top) : 1.f;  // 0 when there was no reference
+                            if (move) {
+                                l_run *= factor;
+                                m_ref = top;
+                            }
+                            if (t > 0 && __any_sync(0xffffffffu, move)) scale_o<D / 2>(tO, factor);
+                            acc[0] = acc[1] = 0;
+                            load(2 * half);
+                            weigh(0);
+                            load(2 * half + 1);
+                            weigh(16);
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(pair);
+                            ok = warp_wait(pair, met & 1, wc);
+                            if (!ok) break;
+                            ++met;
+                        }
+                        tmem_st_x32(tS + 32 * half, pk);
+                        float s0, s1;
+                        f32x2_split(f32x2_add(acc[0], acc[1]), s0, s1);
+                        l_run += s0 + s1;
+                    }
+                    if (key0 + kKeys > g.L) {
+                        // V rows past the keys may hold any bits: zero them so that 0 * row = 0
                         const int vt = n_tiles + t, vs = vt % NV;
-                        ok = warp_wait(&v_full[vs], (vt / NV) & 1, wc);
+                        ok = warp_wait(&sh.v_full[vs], (vt / NV) & 1, wc);
                         if (!ok) break;
                         const int bad = g.L - key0;
                         const int chunks = (kKeys - bad) * 8;
 #pragma unroll
                         for (int h = 0; h < NH; ++h)
-                            for (int ch = row; ch < chunks; ch += 128)
+                            for (int ch = half * 128 + row; ch < chunks; ch += 256)
                                 *reinterpret_cast<uint4*>(smem + OFF_V + vs * TILE + h * kHalfBytes + bad * 128 + ch * 16) =
                                     make_uint4(0, 0, 0, 0);
                         fence_proxy_async_smem();
                     }
-                    const bool masked = key0 + kKeys - 1 > all_lim || (key0 < all_lo && key0 + kKeys > a.sink);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        if (warp_valid) {
-                            const uint32_t tX = tS + 64 * h;
-                            uint32_t seen[2] = {0xffffffffu, 0xffffffffu};
-                            if (masked) {
-#pragma unroll
-                                for (int q = 0; q < 2; ++q) {
-                                    const int k0 = key0 + 64 * h + 32 * q;
-                                    seen[q] = bits(wlo - k0, lim - k0) | bits(0, min(a.sink - 1, lim) - k0);
-                                }
-                            }
-                            bool known = t == 0 && h == 0;  // the references are in place for these scores
-                            uint32_t pk[32];
-                            uint64_t acc[2];
-                            while (true) {
-                                uint32_t x[2][32];
-                                tmem_ld_x32(tX, x[0]);
-                                tmem_ld_x32(tX + 32, x[1]);
-                                tmem_wait_ld_of(x[0]);
-                                tmem_wait_ld_of(x[1]);
-                                if (masked) {
-#pragma unroll
-                                    for (int k = 0; k < 64; ++k)
-                                        if (!(seen[k >> 5] >> (k & 31) & 1)) x[k >> 5][k & 31] = __float_as_uint(-INFINITY);
-                                }
-                                float mx[2] = {-INFINITY, -INFINITY};
-                                if (known) {
-#pragma unroll
-                                    for (int k = 0; k < 64; k += 2)
-                                        mx[(k >> 1) & 1] = max3(mx[(k >> 1) & 1], __uint_as_float(x[k >> 5][k & 31]), __uint_as_float(x[k >> 5][(k & 31) + 1]));
-                                    const float top = max3(mx[0], mx[1], mx[1]) * c;
-                                    const bool move = row_valid && !(top <= m_ref + kJump) && top != -INFINITY;
-                                    const float factor = move ? fast_exp2(m_ref - top) : 1.f;  // 0 when there was no reference
-                                    if (move) {
-                                        l_run *= factor;
-                                        m_ref = top;
-                                    }
-                                    if ((t > 0 || h > 0) && __any_sync(0xffffffffu, move)) {
-                                        if (h > 0) {  // O at rest: the PV of the tile's first half has completed
-                                            ok = warp_wait(&o_half[stream], j & 1, wc);
-                                            tc_fence_after_sync();
-                                        }
-                                        if (ok) scale_o<D>(tO, factor);
-                                    }
-                                }
-                                const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
-                                const uint64_t c2 = f32x2(c, c), m2 = f32x2(-m_use, -m_use);
-                                acc[0] = acc[1] = 0;
-#pragma unroll
-                                for (int k = 0; k < 64; k += 2) {
-                                    const float x0 = __uint_as_float(x[k >> 5][k & 31]), x1 = __uint_as_float(x[k >> 5][(k & 31) + 1]);
-                                    float p0, p1;
-                                    mx[(k >> 1) & 1] = max3(mx[(k >> 1) & 1], x0, x1);
-                                    f32x2_split(f32x2_fma(f32x2(x0, x1), c2, m2), p0, p1);
-                                    if ((k >> 1) % 8 < kPoly) {
-                                        exp2_poly(p0, p1);
-                                    } else {
-                                        p0 = fast_exp2(p0);
-                                        p1 = fast_exp2(p1);
-                                    }
-                                    acc[(k >> 1) & 1] = f32x2_add(acc[(k >> 1) & 1], f32x2(p0, p1));
-                                    pk[k >> 1] = pack_bf16x2(p0, p1);
-                                }
-                                if (known) break;
-                                const float top = max3(mx[0], mx[1], mx[1]) * c;
-                                if (!__any_sync(0xffffffffu, row_valid && !(top <= m_ref + kJump) && top != -INFINITY)) break;
-                                known = true;
-                            }
-                            if (!ok) break;
-                            tmem_st_x32(tS + 32 * h, pk);
-                            float s0, s1;
-                            f32x2_split(f32x2_add(acc[0], acc[1]), s0, s1);
-                            l_run += s0 + s1;
-                        }
-                        tmem_wait_st();
-                        tc_fence_before_sync();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&p_full[stream][h]);
-                    }
-                    if (!ok) break;
+                    tmem_wait_st();
+                    tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sh.p_full[stream]);
                 }
                 if (!ok) break;
-                // ---- the end of the piece ----
+                // ---- the end of the piece: each warp has half of the columns ----
                 if (g.tiles > 0) {
-                    ok = warp_wait(&o_full[stream], done & 1, wc);
+                    ok = warp_wait(&sh.o_full[stream], done & 1, wc);
                     if (!ok) break;
                     ++done;
                     tc_fence_after_sync();
+                    if (warp_valid) {
+                        sh.sum[stream][half][row] = l_run;
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(pair);
+                        ok = warp_wait(pair, met & 1, wc);
+                        if (!ok) break;
+                        ++met;
+                        l_run = sh.sum[stream][0][row] + sh.sum[stream][1][row];
+                    }
                 }
                 const bool empty = m_ref == -INFINITY;  // the row saw no key
                 const float inv = empty ? 0.f : 1.f / l_run;
@@ -672,8 +702,9 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                 float* slot = a.slots + (size_t)max(g.slot, 0) * slot_floats(a.slot_rows, D);
                 const int srow = stream * 128 + row;
 #pragma unroll
-                for (int q = 0; q < D / 32; ++q) {
+                for (int q = 0; q < D / 64; ++q) {
                     uint32_t o[32] = {};
+                    const int d0 = half * (D / 2) + 32 * q;
                     if (g.tiles > 0) {
                         tmem_ld_x32(tO + 32 * q, o);
                         tmem_wait_ld_of(o);
@@ -681,12 +712,12 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                     if (row_valid && g.slot >= 0) {
 #pragma unroll
                         for (int k = 0; k < 32; k += 4)
-                            *reinterpret_cast<uint4*>(slot + ((size_t)(8 * q + k / 4) * a.slot_rows + srow) * 4) =
+                            *reinterpret_cast<uint4*>(slot + ((size_t)((d0 + k) / 4) * a.slot_rows + srow) * 4) =
                                 make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
                     } else if (row_valid) {
 #pragma unroll
                         for (int k = 0; k < 32; ++k) o[k] = empty ? 0u : __float_as_uint(__uint_as_float(o[k]) * inv);
-                        uint4* to = reinterpret_cast<uint4*>(a.out + at * D + 32 * q);
+                        uint4* to = reinterpret_cast<uint4*>(a.out + at * D + d0);
 #pragma unroll
                         for (int k = 0; k < 32; k += 8)
                             to[k / 8] = make_uint4(pack_bf16x2(__uint_as_float(o[k]), __uint_as_float(o[k + 1])),
@@ -696,12 +727,12 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                         if (a.out_f32)
 #pragma unroll
                             for (int k = 0; k < 32; k += 4)
-                                *reinterpret_cast<uint4*>(a.out_f32 + at * D + 32 * q + k) = make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+                                *reinterpret_cast<uint4*>(a.out_f32 + at * D + d0 + k) = make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
                     }
                     __syncwarp();
                 }
                 tc_fence_before_sync();
-                if (row_valid) {
+                if (row_valid && half == 0) {
                     if (g.slot >= 0) {
                         slot[(size_t)a.slot_rows * D + srow] = m_ref;
                         slot[(size_t)a.slot_rows * (D + 1) + srow] = l_run;
@@ -712,18 +743,18 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
             }
             n_tiles += g.tiles;
             __syncwarp();
-            if (lane == 0) mbar_arrive(&ring.empty[r % kRing]);
+            if (lane == 0) mbar_arrive(&sh.ring_empty[r % kRing]);
             ++r;
         }
     }
 
     tc_fence_before_sync();
     __syncthreads();
-    if (warp == 10) {
+    if (warp == kIssuer) {
         tc_fence_after_sync();
         tmem_dealloc(tmem, TMEM_COLS);
     }
-    if (threadIdx.x == 0 && s_abort) atomicOr(a.status, RAPID_STATUS_PIPELINE_TIMEOUT);
+    if (threadIdx.x == 0 && sh.abort) atomicOr(a.status, RAPID_STATUS_PIPELINE_TIMEOUT);
 }
 
 // Merge of the units that were cut: out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s over a row's partials.  An item is
@@ -864,8 +895,8 @@ WsLayout ws_layout(const rapid_attn_shape* s, int T) {
 
 template <int D>
 int launch(const CUtensorMap (&tm)[3], const PrefillArgs& a, int sms, void* split_done, cudaStream_t stream) {
-    constexpr int smem = smem_bytes(D);
-    static_assert(smem <= 232448 - 1024, "shared memory (dynamic + static)");
+    constexpr int smem = smem_bytes<D>();
+    static_assert(smem <= 232448, "shared memory");
     int dev = 0;
     RAPID_CUDA_CHECK(cudaGetDevice(&dev));
     static std::atomic<bool> configured[64];  // (first calls may come from several threads at once; all set the same)
