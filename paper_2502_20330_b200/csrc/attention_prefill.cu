@@ -486,12 +486,13 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
             }
             for (int t = 0; t <= tiles && tiles > 0 && ok; ++t) {
                 const int ks = n_k % NK, vs = n_v % NV;
+                if (t > 0) ok = warp_wait(&sh.v_full[vs], (n_v / NV) & 1, wc);
+                if (t < tiles) ok = ok && warp_wait(&sh.k_full[ks], (n_k / NK) & 1, wc);
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
                     if (s >= streams) continue;
                     const uint32_t tS = tmem + COL_S + 128u * s, tO = tmem + COL_O + 128u * s;
                     if (t > 0) {
-                        if (s == 0) ok = ok && warp_wait(&sh.v_full[vs], (n_v / NV) & 1, wc);
                         ok = ok && warp_wait(&sh.p_full[s], p_par[s], wc);
                         p_par[s] ^= 1;
                         tc_fence_after_sync();
@@ -505,7 +506,6 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                         __syncwarp();
                     }
                     if (t < tiles) {
-                        if (s == 0) ok = ok && warp_wait(&sh.k_full[ks], (n_k / NK) & 1, wc);
                         tc_fence_after_sync();
                         if (ok && leader) {
                             const uint64_t qd = q_desc + (uint32_t)s * (TILE >> 4), kd = k_desc + (uint32_t)ks * (TILE >> 4);
@@ -616,7 +616,6 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                             weigh(0);
                             load(2 * half + 1);
                             largest();
-                            weigh(16);
                             const float top = max3(mx[0], mx[1], mx[1]) * c;
                             again = __any_sync(0xffffffffu, row_valid && !(top <= m_ref + kJump) && top != -INFINITY);
                             // the other half of the keys; and neither warp writes over scores that the other has not read
@@ -624,6 +623,7 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                                 sh.flag[met & 1][stream][half][quarter] = again;
                                 mbar_arrive(pair);
                             }
+                            weigh(16);
                             ok = warp_wait(pair, met & 1, wc);
                             if (!ok) break;
                             again |= *(volatile uint32_t*)&sh.flag[met & 1][stream][half ^ 1][quarter] != 0;
