@@ -209,7 +209,7 @@ __global__ void __launch_bounds__(kPlanThreads) prefill_plan_kernel(const __grid
     sizes[tid] = tid < tail ? mine.tiles : 0;
     __syncthreads();
     // The length of a piece: every warp weighs one.  With `waves` pieces for every CTA a unit is cut into waves * CTAs / units
-    // parts; the estimate is whole rounds of pieces of the mean cost (or, behind whole units, an even share and half a piece),
+    // parts; the estimate is whole rounds of pieces of the mean cost (or, behind whole units, an even share and a quarter of a piece),
     // and what the partials cost.
     {
         int most = 0;
@@ -232,7 +232,7 @@ __global__ void __launch_bounds__(kPlanThreads) prefill_plan_kernel(const __grid
         for (int o = 16; o; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
         if (lane == 0) {
             const float mean = (all + kPieceCost * count) / max(count, 1), top = len + kPieceCost;
-            float est = whole ? mean * count / a.num_ctas + 0.5f * top
+            float est = whole ? mean * count / a.num_ctas + 0.25f * top
                               : mean * ((count + a.num_ctas - 1) / a.num_ctas) + top - mean;
             est += kSlotCost * cut;
             if (cut > a.max_slots || count > kMaxTail) est = INFINITY;
@@ -287,6 +287,15 @@ struct Shared {
 template <int D>
 constexpr int smem_bytes() {
     return (2 + k_slots(D) + v_slots(D)) * tile_bytes(D) + (int)sizeof(Shared<D>);
+}
+
+// A whole warp's wait.  What happens when the barrier is not there yet is kept out of line, or a dozen copies of it crowd the
+// loops out of the instruction cache.
+__device__ __noinline__ bool wait_longer(uint64_t* bar, uint32_t parity, volatile int* abort, long long limit) {
+    return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, WaitCtx{abort, limit}));
+}
+__device__ __forceinline__ bool role_wait(uint64_t* bar, uint32_t parity, const WaitCtx& wc) {
+    return __all_sync(0xffffffffu, mbar_try_wait(bar, parity)) || wait_longer(bar, parity, wc.abort, wc.limit);
 }
 
 __device__ __forceinline__ void tmem_wait_ld_of(uint32_t (&r)[32]) {  // (ties the registers to the wait)
@@ -364,15 +373,17 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
         const uint32_t part_bytes = kHalfBytes / parts;
         bool ok = true;
         while (ok) {
-            ok = warp_wait(&sh.ring_full[r % kRing], (r / kRing) & 1, wc);
+            ok = role_wait(&sh.ring_full[r % kRing], (r / kRing) & 1, wc);
             const Piece g = sh.piece[r % kRing];
             const Span sp = sh.span[r % kRing];
             if (!ok || g.tiles < 0) break;
+#pragma unroll 1
             for (int t = 0; t < g.tiles && ok; ++t) {
                 const int u = g.first + t;
                 const int key0 = (u < sp.sinks ? u : sp.lo + u - sp.sinks) * kKeys;
                 int c1[2] = {key0, 0}, c3[2] = {g.b, g.b};
                 if (a.block_table) {
+#pragma unroll 1
                     for (int q = 0; q < parts; ++q) {
                         const int pos = key0 + q * a.box_rows;
                         c1[q] = pos & (a.block_size - 1);
@@ -388,12 +399,13 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                     }
                 }
                 const int ks = n_k % NK, vs = n_v % NV;
-                if (n_k >= NK) ok = warp_wait(&sh.k_empty[ks], (n_k / NK - 1) & 1, wc);
+                if (n_k >= NK) ok = role_wait(&sh.k_empty[ks], (n_k / NK - 1) & 1, wc);
                 if (!ok) break;
                 if (elect_one()) {
                     mbar_arrive_expect_tx(&sh.k_full[ks], TILE);
+#pragma unroll 1
                     for (int q = 0; q < parts; ++q)
-#pragma unroll
+#pragma unroll 1
                         for (int h = 0; h < NH; ++h)
                             tma_load_4d(smem + OFF_K + ks * TILE + h * kHalfBytes + q * part_bytes, &tmK, &sh.k_full[ks],
                                         h * 64, c1[q], g.kvh, c3[q]);
@@ -401,13 +413,14 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                 __syncwarp();
                 ++n_k;
                 if (t == 0) {  // (behind the first K tile, which need not wait for the unit before)
-                    if (n_q > 0) ok = warp_wait(&sh.q_empty, (n_q - 1) & 1, wc);
+                    if (n_q > 0) ok = role_wait(&sh.q_empty, (n_q - 1) & 1, wc);
                     if (!ok) break;
                     const int streams = g.n - g.row0 > a.rows_tile ? 2 : 1;
                     if (elect_one()) {
                         mbar_arrive_expect_tx(&sh.q_full, (uint32_t)(streams * a.rows_tile * a.G * D * 2));
+#pragma unroll 1
                         for (int s = 0; s < streams; ++s)
-#pragma unroll
+#pragma unroll 1
                             for (int h = 0; h < NH; ++h)
                                 tma_load_4d(smem + OFF_Q + s * TILE + h * kHalfBytes, &tmQ, &sh.q_full, h * 64, g.kvh * a.G,
                                             g.row0 + s * a.rows_tile, g.b);
@@ -415,12 +428,13 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                     __syncwarp();
                     ++n_q;
                 }
-                if (n_v >= NV) ok = warp_wait(&sh.v_empty[vs], (n_v / NV - 1) & 1, wc);
+                if (n_v >= NV) ok = role_wait(&sh.v_empty[vs], (n_v / NV - 1) & 1, wc);
                 if (!ok) break;
                 if (elect_one()) {
                     mbar_arrive_expect_tx(&sh.v_full[vs], TILE);
+#pragma unroll 1
                     for (int q = 0; q < parts; ++q)
-#pragma unroll
+#pragma unroll 1
                         for (int h = 0; h < NH; ++h)
                             tma_load_4d(smem + OFF_V + vs * TILE + h * kHalfBytes + q * part_bytes, &tmV, &sh.v_full[vs],
                                         h * 64, c1[q], g.kvh, c3[q]);
@@ -437,7 +451,9 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
         }
         // every copy lands before the CTA gives up its shared memory, whoever may have given up waiting for it
         if (n_q > 0) mbar_wait_drain(&sh.q_full, (n_q - 1) & 1);
+#pragma unroll 1
         for (int s = 0; s < NK && s < n_k; ++s) mbar_wait_drain(&sh.k_full[(n_k - 1 - s) % NK], ((n_k - 1 - s) / NK) & 1);
+#pragma unroll 1
         for (int s = 0; s < NV && s < n_v; ++s) mbar_wait_drain(&sh.v_full[(n_v - 1 - s) % NV], ((n_v - 1 - s) / NV) & 1);
     } else if (warp == kWalk) {
         // ---------------- the walk: pieces from the list into the ring ----------------
@@ -445,9 +461,9 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
         int i = blockIdx.x;
         for (int k = 0;; ++k) {
             const int s = k % kRing;
-            if (k >= kRing && !warp_wait(&sh.ring_empty[s], (k / kRing - 1) & 1, wc)) break;
+            if (k >= kRing && !role_wait(&sh.ring_empty[s], (k / kRing - 1) & 1, wc)) break;
             if (k > 0) {
-                if (!warp_wait(&sh.taken, (k - 1) & 1, wc)) break;
+                if (!role_wait(&sh.taken, (k - 1) & 1, wc)) break;
                 if (lane == 0) i = atomicAdd(&a.control->next, 1);
                 i = __shfl_sync(0xffffffffu, i, 0);
             }
@@ -484,6 +500,7 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                 ok = warp_wait(&sh.q_full, n_q & 1, wc);
                 ++n_q;
             }
+#pragma unroll 1
             for (int t = 0; t <= tiles && tiles > 0 && ok; ++t) {
                 const int ks = n_k % NK, vs = n_v % NV;
                 if (t > 0) ok = warp_wait(&sh.v_full[vs], (n_v / NV) & 1, wc);
@@ -553,7 +570,7 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
         int met = 0;                       // times that the two warps of a quarter have met
         bool ok = true;
         while (ok) {
-            ok = warp_wait(&sh.ring_full[r % kRing], (r / kRing) & 1, wc);
+            ok = role_wait(&sh.ring_full[r % kRing], (r / kRing) & 1, wc);
             const Piece g = sh.piece[r % kRing];
             const Span sp = sh.span[r % kRing];
             if (!ok || g.tiles < 0) break;
@@ -568,8 +585,9 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                 const int all_lim = a.all_visible ? g.L - 1 : p0;
                 const int all_lo = a.window ? p0 + a.rows_tile - 1 - a.window + 1 : 0;
                 float m_ref = -INFINITY, l_run = 0.f;
+#pragma unroll 1
                 for (int t = 0; t < g.tiles; ++t, ++j) {
-                    ok = warp_wait(&sh.s_full[stream], j & 1, wc);
+                    ok = role_wait(&sh.s_full[stream], j & 1, wc);
                     if (!ok) break;
                     const int u = g.first + t;
                     const int key0 = (u < sp.sinks ? u : sp.lo + u - sp.sinks) * kKeys;
@@ -624,7 +642,7 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                                 mbar_arrive(pair);
                             }
                             weigh(16);
-                            ok = warp_wait(pair, met & 1, wc);
+                            ok = role_wait(pair, met & 1, wc);
                             if (!ok) break;
                             again |= *(volatile uint32_t*)&sh.flag[met & 1][stream][half ^ 1][quarter] != 0;
                             ++met;
@@ -651,7 +669,7 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                             weigh(16);
                             __syncwarp();
                             if (lane == 0) mbar_arrive(pair);
-                            ok = warp_wait(pair, met & 1, wc);
+                            ok = role_wait(pair, met & 1, wc);
                             if (!ok) break;
                             ++met;
                         }
@@ -663,7 +681,7 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                     if (key0 + kKeys > g.L) {
                         // V rows past the keys may hold any bits: zero them so that 0 * row = 0
                         const int vt = n_tiles + t, vs = vt % NV;
-                        ok = warp_wait(&sh.v_full[vs], (vt / NV) & 1, wc);
+                        ok = role_wait(&sh.v_full[vs], (vt / NV) & 1, wc);
                         if (!ok) break;
                         const int bad = g.L - key0;
                         const int chunks = (kKeys - bad) * 8;
@@ -682,7 +700,7 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                 if (!ok) break;
                 // ---- the end of the piece: each warp has half of the columns ----
                 if (g.tiles > 0) {
-                    ok = warp_wait(&sh.o_full[stream], done & 1, wc);
+                    ok = role_wait(&sh.o_full[stream], done & 1, wc);
                     if (!ok) break;
                     ++done;
                     tc_fence_after_sync();
@@ -690,7 +708,7 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                         sh.sum[stream][half][row] = l_run;
                         __syncwarp();
                         if (lane == 0) mbar_arrive(pair);
-                        ok = warp_wait(pair, met & 1, wc);
+                        ok = role_wait(pair, met & 1, wc);
                         if (!ok) break;
                         ++met;
                         l_run = sh.sum[stream][0][row] + sh.sum[stream][1][row];
@@ -701,7 +719,7 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                 const size_t at = ((size_t)g.b * a.T + i0 + row_t) * a.Hq + (size_t)g.kvh * a.G + row_h;
                 float* slot = a.slots + (size_t)max(g.slot, 0) * slot_floats(a.slot_rows, D);
                 const int srow = stream * 128 + row;
-#pragma unroll
+#pragma unroll 1
                 for (int q = 0; q < D / 64; ++q) {
                     uint32_t o[32] = {};
                     const int d0 = half * (D / 2) + 32 * q;
@@ -709,27 +727,52 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                         tmem_ld_x32(tO + 32 * q, o);
                         tmem_wait_ld_of(o);
                     }
-                    if (row_valid && g.slot >= 0) {
-#pragma unroll
-                        for (int k = 0; k < 32; k += 4)
-                            *reinterpret_cast<uint4*>(slot + ((size_t)((d0 + k) / 4) * a.slot_rows + srow) * 4) =
-                                make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
-                    } else if (row_valid) {
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) o[k] = empty ? 0u : __float_as_uint(__uint_as_float(o[k]) * inv);
-                        uint4* to = reinterpret_cast<uint4*>(a.out + at * D + d0);
-#pragma unroll
-                        for (int k = 0; k < 32; k += 8)
-                            to[k / 8] = make_uint4(pack_bf16x2(__uint_as_float(o[k]), __uint_as_float(o[k + 1])),
-                                                   pack_bf16x2(__uint_as_float(o[k + 2]), __uint_as_float(o[k + 3])),
-                                                   pack_bf16x2(__uint_as_float(o[k + 4]), __uint_as_float(o[k + 5])),
-                                                   pack_bf16x2(__uint_as_float(o[k + 6]), __uint_as_float(o[k + 7])));
-                        if (a.out_f32)
+                    if (g.slot >= 0) {
+                        if (row_valid) {
 #pragma unroll
                             for (int k = 0; k < 32; k += 4)
-                                *reinterpret_cast<uint4*>(a.out_f32 + at * D + d0 + k) = make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+                                *reinterpret_cast<uint4*>(slot + ((size_t)((d0 + k) / 4) * a.slot_rows + srow) * 4) =
+                                    make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+                        }
+                        __syncwarp();
+                        continue;
+                    }
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) o[k] = empty ? 0u : __float_as_uint(__uint_as_float(o[k]) * inv);
+                    if (a.out_f32 && row_valid) {
+#pragma unroll
+                        for (int k = 0; k < 32; k += 4)
+                            *reinterpret_cast<uint4*>(a.out_f32 + at * D + d0 + k) = make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
                     }
                     __syncwarp();
+                    // A lane has 64 bytes of its row, in four words of 16; among four neighbouring lanes the words change places,
+                    // so that each store writes the 64 bytes of whole rows: lane 4 i + k, word k of the rows 4 i + 0 .. 3.
+                    uint32_t w[4][4];
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) w[k >> 2][k & 3] = pack_bf16x2(__uint_as_float(o[2 * k]), __uint_as_float(o[2 * k + 1]));
+#pragma unroll
+                    for (int step = 1; step < 4; step <<= 1) {
+                        const bool up = lane & step;
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) {
+                            if (u & step) continue;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {  // this lane keeps word u (or u + step) and gives the other away
+                                const uint32_t give = up ? w[u][i] : w[u + step][i];
+                                const uint32_t got = __shfl_xor_sync(0xffffffffu, give, step);
+                                if (up) w[u][i] = got;
+                                else w[u + step][i] = got;
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const int from = (lane & ~3) + u;  // the row's lane
+                        const int rt = __shfl_sync(0xffffffffu, row_t, from), rh = __shfl_sync(0xffffffffu, row_h, from);
+                        if (rt < a.rows_tile && i0 + rt < g.n)
+                            *reinterpret_cast<uint4*>(a.out + (((size_t)g.b * a.T + i0 + rt) * a.Hq + (size_t)g.kvh * a.G + rh) * D + d0 + 8 * (lane & 3)) =
+                                make_uint4(w[u][0], w[u][1], w[u][2], w[u][3]);
+                    }
                 }
                 tc_fence_before_sync();
                 if (row_valid && half == 0) {
