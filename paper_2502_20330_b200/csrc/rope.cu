@@ -7,7 +7,10 @@
 // whole turns are taken off there, and what is left, at most half a turn, goes to 32 bits (2^-25 of a turn).  The angles are worked out
 // once a token and serve all its heads.
 //
-// Bound: HBM.  Every element is read and written once, 4 bytes; an SM's blocks have 24 - 64 KB of reads in flight.
+// Bound: HBM.  Every element is read and written once, 4 bytes; an SM's four blocks of 256 threads have up to 128 KB of reads under way.
+// Four items of 32 bytes a thread at 64 registers: 100 us for two videos of 20,011 tokens at 28/4 heads of 128 (6.5 TB/s), 191 us for
+// prompts of up to 24,000 tokens at 32/8 heads with their append (6.0 TB/s); three items 120 and 224, six 141 and 233, two at six blocks an
+// SM 106 and 187.  Calls of few tokens are a launch and one round trip (3.2 us).
 #include <math.h>
 
 #include "common.cuh"
@@ -18,9 +21,10 @@ namespace rapid {
 namespace {
 
 constexpr int kRopeThreads = 256;
-constexpr int kRopeItems = 3;       // items of 32 bytes that a thread has in flight
+constexpr int kRopeItems = 4;       // items of 32 bytes that a thread has in flight
+constexpr int kRopeBlocks = 4;      // blocks an SM holds: 64 registers a thread
 constexpr int kRopeMaxD = 256;
-constexpr int kRopeMaxTokens = 4;   // tokens of a block
+constexpr int kRopeMaxTokens = 16;  // tokens of a block
 
 struct RopeTensor {  // [B, T, H, D] bf16 by element strides
     __nv_bfloat16* p;
@@ -51,7 +55,7 @@ __device__ __forceinline__ float2 unpack_bf16x2(uint32_t v) {
 
 // One item is 16 elements of a row, two 16-byte words: eight pairs, or 16 elements that are not turned.
 template <bool INTER>
-__global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constant__ RopeArgs a) {
+__global__ void __launch_bounds__(kRopeThreads, kRopeBlocks) rope_kernel(const __grid_constant__ RopeArgs a) {
     // cos and sin of the block's tokens: two pairs to a word, the words of an item spread so that the
     // threads of a row read neighbouring ones
     __shared__ float4 turn[kRopeMaxTokens * kRopeMaxD / 4];
@@ -255,12 +259,14 @@ int rope_of(const char* who, const rapid_rope* rope, RopeArgs& a) {
 }
 
 int launch(RopeArgs& a, int interleaved, cudaStream_t stream) {
-    // Four tokens a block give each thread one angle and six items at 48 heads of 128; while that leaves SMs without a block,
-    // one token.
+    // As many tokens a block as give its threads four to six items each, fewer while that leaves SMs without four blocks.  (Two videos
+    // at 32 heads of 128, four tokens: 100 us, two 136, eight 111; a prompt at 10 heads of 64, sixteen tokens: 7.4 us, four 9.2.)
     int dev = 0, sms = 0;
     RAPID_CUDA_CHECK(cudaGetDevice(&dev));
     RAPID_CUDA_CHECK(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-    a.tokens = (int64_t)a.B * a.T >= (int64_t)4 * kRopeMaxTokens * sms ? kRopeMaxTokens : 1;
+    const int64_t items = (int64_t)(a.Hq + (a.ctx ? 2 : 1) * a.Hkv) * (a.D / 16);
+    a.tokens = kRopeMaxTokens;
+    while (a.tokens > 1 && (a.tokens * items > 6 * kRopeThreads || (int64_t)a.B * a.T < (int64_t)4 * a.tokens * sms)) a.tokens /= 2;
     const dim3 grid((a.T + a.tokens - 1) / a.tokens, a.B);
     RAPID_CUDA_CHECK(launch_dependent(interleaved ? rope_kernel<true> : rope_kernel<false>, grid, dim3(kRopeThreads), 0, stream, a));
     count_launch(1);
