@@ -50,6 +50,7 @@ constexpr int kMaxTail = 640;            // pieces the tail is cut into at most
 constexpr int kSeqInSmem = 1024;
 constexpr float kPieceCost = 2.5f;       // tiles that a piece costs beside its own
 constexpr float kSlotCost = 0.03f;       // tiles that a partial costs the whole call, written and read
+constexpr float kMergeCost = 2.f;        // tiles that it takes to join any
 constexpr int kMaxUnits = 1 << 24;
 
 __host__ __device__ constexpr int k_slots(int D) { return D == 128 ? 2 : 4; }
@@ -66,8 +67,9 @@ struct __align__(16) Cut {
     int b, kvh, row0, n;
     int slot, parts, reserved0, reserved1;
 };
+constexpr int kFewParts = 8, kSomeFew = 1, kSomeMany = 2;
 struct Control {
-    int next, pieces, cuts, reserved;
+    int next, pieces, cuts, shapes;  // shapes: whether there are cuts of few parts, and of many
 };
 
 struct PrefillArgs {
@@ -234,7 +236,7 @@ __global__ void __launch_bounds__(kPlanThreads) prefill_plan_kernel(const __grid
             const float mean = (all + kPieceCost * count) / max(count, 1), top = len + kPieceCost;
             float est = whole ? mean * count / a.num_ctas + 0.25f * top
                               : mean * ((count + a.num_ctas - 1) / a.num_ctas) + top - mean;
-            est += kSlotCost * cut;
+            if (cut) est += kMergeCost + kSlotCost * cut;
             if (cut > a.max_slots || count > kMaxTail) est = INFINITY;
             sh_est[warp] = est;
             sh_len[warp] = len;
@@ -263,7 +265,10 @@ __global__ void __launch_bounds__(kPlanThreads) prefill_plan_kernel(const __grid
         }
         if (parts > 1) a.cuts[cut0] = {mine.b, mine.kvh, mine.row0, mine.n, slot0, parts, 0, 0};
     }
-    if (tid == 0) *a.control = {a.num_ctas, whole + pieces, cuts, 0};
+    const int few = __syncthreads_or(parts > 1 && parts <= kFewParts), many = __syncthreads_or(parts > kFewParts);
+    // (a CTA's first piece is the one of its own number: where there are fewer, an end marker)
+    for (int i = whole + pieces + tid; i < a.num_ctas; i += kPlanThreads) a.pieces[i].tiles = -1;
+    if (tid == 0) *a.control = {a.num_ctas, whole + pieces, cuts, (few ? kSomeFew : 0) | (many ? kSomeMany : 0)};
 }
 
 constexpr int kRing = 2;                          // pieces a CTA has in hand: the one at work and the next
@@ -457,8 +462,7 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
         for (int s = 0; s < NV && s < n_v; ++s) mbar_wait_drain(&sh.v_full[(n_v - 1 - s) % NV], ((n_v - 1 - s) / NV) & 1);
     } else if (warp == kWalk) {
         // ---------------- the walk: pieces from the list into the ring ----------------
-        const int pieces = a.control->pieces;
-        int i = blockIdx.x;
+        int i = blockIdx.x, pieces = i + 1;  // (how many there are is asked for beside the first)
         for (int k = 0;; ++k) {
             const int s = k % kRing;
             if (k >= kRing && !role_wait(&sh.ring_empty[s], (k / kRing - 1) & 1, wc)) break;
@@ -467,8 +471,10 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                 if (lane == 0) i = atomicAdd(&a.control->next, 1);
                 i = __shfl_sync(0xffffffffu, i, 0);
             }
+            const int known = pieces;
+            if (k == 0) pieces = a.control->pieces;
             if (lane == 0) {
-                if (i < pieces) {
+                if (i < known) {
                     const Piece g = a.pieces[i];
                     sh.piece[s] = g;
                     sh.span[s] = span_of(a, g.row0, g.n, g.L);
@@ -801,101 +807,127 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
 }
 
 // Merge of the units that were cut: out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s over a row's partials.  An item is
-// 32 rows (lane = row) and 16 columns; its warps take the partials w, w + W, ..., four of each in flight, and meet in shared memory.
-// The order of the sums is fixed.
+// 32 rows (lane = row) and 16 columns.  Where a unit has few parts, a block's warps take an item each (one round trip, nothing to
+// join); where it has many, they split an item's parts.  The order of the sums is fixed either way.
+struct MergeSum {
+    float m, l;
+    float4 acc[4];
+};
+// The parts first, first + step, ... of the item at rows srow, columns 4 d4 .. 4 d4 + 15; four of them in flight at a time.
+__device__ __forceinline__ MergeSum merge_parts(const PrefillArgs& a, const float* base, size_t per, int D, int srow, int d4, bool valid,
+                                                int first, int step, int parts) {
+    constexpr int UN = 4;
+    MergeSum r;
+    r.m = -INFINITY;
+    r.l = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) r.acc[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int x0 = first; x0 < parts; x0 += step * UN) {
+        float ms[UN], ls[UN];
+        float4 o[UN][4];
+#pragma unroll
+        for (int u = 0; u < UN; ++u) {
+            const int x = x0 + step * u;
+            ms[u] = -INFINITY;
+            if (x < parts && valid) {
+                const float* s = base + (size_t)x * per;
+                ms[u] = __ldcg(s + (size_t)a.slot_rows * D + srow);
+                ls[u] = __ldcg(s + (size_t)a.slot_rows * (D + 1) + srow);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[u][j] = __ldcg(reinterpret_cast<const float4*>(s) + (size_t)(d4 + j) * a.slot_rows + srow);
+            }
+        }
+        float top = r.m;
+#pragma unroll
+        for (int u = 0; u < UN; ++u) top = max3(top, ms[u], ms[u]);
+        const float keep = r.m == -INFINITY ? 0.f : exp2f(r.m - top);
+        r.m = top;
+        r.l *= keep;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) r.acc[j].x *= keep, r.acc[j].y *= keep, r.acc[j].z *= keep, r.acc[j].w *= keep;
+#pragma unroll
+        for (int u = 0; u < UN; ++u) {
+            if (ms[u] == -INFINITY) continue;  // a part in which the row saw no key
+            const float wgt = exp2f(ms[u] - top);
+            r.l += wgt * ls[u];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                r.acc[j].x += wgt * o[u][j].x;
+                r.acc[j].y += wgt * o[u][j].y;
+                r.acc[j].z += wgt * o[u][j].z;
+                r.acc[j].w += wgt * o[u][j].w;
+            }
+        }
+    }
+    return r;
+}
+// Four columns of row `sr` of a cut unit.
+__device__ __forceinline__ void merge_write(const PrefillArgs& a, const Cut& g, int D, int sr, int d4, float M, float L, float4 v) {
+    const int rt = (sr & 127) / a.G, rh = (sr & 127) - rt * a.G, i = g.row0 + (sr >> 7) * a.rows_tile + rt;
+    if (rt >= a.rows_tile || i >= g.n) return;
+    const size_t at = ((size_t)g.b * a.T + i) * a.Hq + (size_t)g.kvh * a.G + rh;
+    const float inv = M == -INFINITY ? 0.f : 1.f / L;
+    v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+    *reinterpret_cast<uint2*>(a.out + at * D + d4 * 4) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+    if (a.out_f32) *reinterpret_cast<float4*>(a.out_f32 + at * D + d4 * 4) = v;
+    if (a.lse_out && d4 == 0) a.lse_out[at] = M == -INFINITY ? -INFINITY : (M + log2f(L)) * 0.69314718055994530942f;
+}
 template <int D>
 __global__ void __launch_bounds__(128) prefill_merge_kernel(const __grid_constant__ PrefillArgs a) {
-    constexpr int W = 4, UN = 4;
+    constexpr int W = 4, PER_ROWS = D / 64;  // 32 rows are 4 * PER_ROWS items
     __shared__ float4 sh_acc[W][4][32];
     __shared__ float sh_m[W][32], sh_l[W][32];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     griddep_wait();
     griddep_launch_dependents();
     const int groups = a.slot_rows / 32;
-    const int items = a.control->cuts * groups * (D / 16);
-    for (int item = blockIdx.x; item < items; item += gridDim.x) {
-        const Cut g = a.cuts[item / (groups * (D / 16))];
-        const int rest = item % (groups * (D / 16));
-        const int srow = rest / (D / 16) * 32 + lane, d4 = rest % (D / 16) * 4;
-        const int stream = srow >> 7, row_t = (srow & 127) / a.G;
-        const int i = g.row0 + stream * a.rows_tile + row_t;  // row of the sequence
-        const bool valid = row_t < a.rows_tile && i < g.n;
-        const size_t per = slot_floats(a.slot_rows, D);
-        const float* base = a.slots + (size_t)g.slot * per;
-        float m = -INFINITY, l = 0.f;
-        float4 acc[4];
+    const Control ctl = *a.control;
+    const size_t per = slot_floats(a.slot_rows, D);
+    if (ctl.shapes & kSomeFew) {
+        for (int quad = blockIdx.x; quad < ctl.cuts * groups * PER_ROWS; quad += gridDim.x) {
+            const Cut g = a.cuts[quad / (groups * PER_ROWS)];
+            if (g.parts > kFewParts) continue;
+            const int rest = quad % (groups * PER_ROWS);
+            const int srow = rest / PER_ROWS * 32 + lane, d4 = (rest % PER_ROWS * 4 + warp) * 4, rt = (srow & 127) / a.G;
+            const bool valid = rt < a.rows_tile && g.row0 + (srow >> 7) * a.rows_tile + rt < g.n;
+            const MergeSum r = merge_parts(a, a.slots + (size_t)g.slot * per, per, D, srow, d4, valid, 0, 1, g.parts);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int x0 = warp; x0 < g.parts; x0 += W * UN) {
-            float ms[UN], ls[UN];
-            float4 o[UN][4];
-#pragma unroll
-            for (int u = 0; u < UN; ++u) {
-                const int x = x0 + W * u;
-                ms[u] = -INFINITY;
-                if (x < g.parts && valid) {
-                    const float* s = base + (size_t)x * per;
-                    ms[u] = __ldcg(s + (size_t)a.slot_rows * D + srow);
-                    ls[u] = __ldcg(s + (size_t)a.slot_rows * (D + 1) + srow);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) o[u][j] = __ldcg(reinterpret_cast<const float4*>(s) + (size_t)(d4 + j) * a.slot_rows + srow);
-                }
-            }
-            float top = m;
-#pragma unroll
-            for (int u = 0; u < UN; ++u) top = max3(top, ms[u], ms[u]);
-            const float keep = m == -INFINITY ? 0.f : exp2f(m - top);
-            m = top;
-            l *= keep;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[j].x *= keep, acc[j].y *= keep, acc[j].z *= keep, acc[j].w *= keep;
-#pragma unroll
-            for (int u = 0; u < UN; ++u) {
-                if (ms[u] == -INFINITY) continue;  // a part in which the row saw no key
-                const float wgt = exp2f(ms[u] - top);
-                l += wgt * ls[u];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    acc[j].x += wgt * o[u][j].x;
-                    acc[j].y += wgt * o[u][j].y;
-                    acc[j].z += wgt * o[u][j].z;
-                    acc[j].w += wgt * o[u][j].w;
-                }
-            }
+            for (int j = 0; j < 4; ++j) merge_write(a, g, D, srow, d4 + j, r.m, r.l, r.acc[j]);
         }
+    }
+    if (!(ctl.shapes & kSomeMany)) return;
+    for (int item = blockIdx.x; item < ctl.cuts * groups * PER_ROWS * 4; item += gridDim.x) {
+        const Cut g = a.cuts[item / (groups * PER_ROWS * 4)];
+        if (g.parts <= kFewParts) continue;
+        const int rest = item % (groups * PER_ROWS * 4);
+        const int srow0 = rest / (PER_ROWS * 4) * 32, d4 = rest % (PER_ROWS * 4) * 4;
+        const int srow = srow0 + lane, rt = (srow & 127) / a.G;
+        const bool valid = rt < a.rows_tile && g.row0 + (srow >> 7) * a.rows_tile + rt < g.n;
+        const MergeSum r = merge_parts(a, a.slots + (size_t)g.slot * per, per, D, srow, d4, valid, warp, W, g.parts);
         __syncthreads();  // (the item before has been read)
-        sh_m[warp][lane] = m;
-        sh_l[warp][lane] = l;
+        sh_m[warp][lane] = r.m;
+        sh_l[warp][lane] = r.l;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) sh_acc[warp][j][lane] = acc[j];
+        for (int j = 0; j < 4; ++j) sh_acc[warp][j][lane] = r.acc[j];
         __syncthreads();
         // four neighbouring threads write the 16 columns of a row
         const int row = threadIdx.x >> 2, j = threadIdx.x & 3;
-        const int sr = rest / (D / 16) * 32 + row, rt = (sr & 127) / a.G, rh = (sr & 127) - rt * a.G;
-        const int ii = g.row0 + (sr >> 7) * a.rows_tile + rt;
-        if (rt < a.rows_tile && ii < g.n) {
-            float M = -INFINITY, L = 0.f;
+        float M = -INFINITY, L = 0.f;
 #pragma unroll
-            for (int k = 0; k < W; ++k) M = max3(M, sh_m[k][row], sh_m[k][row]);
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int w = 0; w < W; ++w) M = max3(M, sh_m[w][row], sh_m[w][row]);
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-            for (int k = 0; k < W; ++k) {
-                if (sh_m[k][row] == -INFINITY) continue;
-                const float wgt = exp2f(sh_m[k][row] - M);
-                const float4 o = sh_acc[k][j][row];
-                L += wgt * sh_l[k][row];
-                v.x += wgt * o.x;
-                v.y += wgt * o.y;
-                v.z += wgt * o.z;
-                v.w += wgt * o.w;
-            }
-            const size_t at = ((size_t)g.b * a.T + ii) * a.Hq + (size_t)g.kvh * a.G + rh;
-            const float inv = M == -INFINITY ? 0.f : 1.f / L;
-            v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
-            *reinterpret_cast<uint2*>(a.out + at * D + (d4 + j) * 4) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
-            if (a.out_f32) *reinterpret_cast<float4*>(a.out_f32 + at * D + (d4 + j) * 4) = v;
-            if (a.lse_out && d4 + j == 0) a.lse_out[at] = M == -INFINITY ? -INFINITY : (M + log2f(L)) * 0.69314718055994530942f;
+        for (int w = 0; w < W; ++w) {
+            if (sh_m[w][row] == -INFINITY) continue;
+            const float wgt = exp2f(sh_m[w][row] - M);
+            const float4 o = sh_acc[w][j][row];
+            L += wgt * sh_l[w][row];
+            v.x += wgt * o.x;
+            v.y += wgt * o.y;
+            v.z += wgt * o.z;
+            v.w += wgt * o.w;
         }
+        merge_write(a, g, D, srow0 + row, d4 + j, M, L, v);
     }
 }
 
