@@ -315,8 +315,10 @@ __device__ __forceinline__ void tmem_wait_ld_of(uint32_t (&r)[32]) {  // (ties t
 
 // Bits lo .. hi (of 0 .. 31) of a word; lo and hi may lie outside.
 __device__ __forceinline__ uint32_t bits(int lo, int hi) {
-    if (hi < 0 || lo > 31 || lo > hi) return 0;
-    return (hi >= 31 ? 0xffffffffu : (2u << hi) - 1) & ~(lo <= 0 ? 0u : (1u << lo) - 1);
+    const int from = max(lo, 0), n = max(hi - from + 1, 0);
+    uint32_t r;
+    asm("bmsk.clamp.b32 %0, %1, %2;" : "=r"(r) : "r"(from), "r"(n));
+    return r;
 }
 
 template <int D>
@@ -635,19 +637,33 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                         if (!again) {
                             acc[0] = acc[1] = 0;
                             mx[0] = mx[1] = -INFINITY;
-                            load(2 * half);
-                            largest();
-                            weigh(0);
-                            load(2 * half + 1);
-                            largest();
-                            const float top = max3(mx[0], mx[1], mx[1]) * c;
-                            again = __any_sync(0xffffffffu, row_valid && !(top <= m_ref + kJump) && top != -INFINITY);
-                            // the other half of the keys; and neither warp writes over scores that the other has not read
-                            if (lane == 0) {
-                                sh.flag[met & 1][stream][half][quarter] = again;
-                                mbar_arrive(pair);
+                            auto tell = [&] {  // the other half of the keys; and neither warp writes over scores that the other has not read
+                                const float top = max3(mx[0], mx[1], mx[1]) * c;
+                                again = __any_sync(0xffffffffu, row_valid && !(top <= m_ref + kJump) && top != -INFINITY);
+                                if (lane == 0) {
+                                    sh.flag[met & 1][stream][half][quarter] = again;
+                                    mbar_arrive(pair);
+                                }
+                            };
+                            if (masked) {
+                                load(2 * half);
+                                largest();
+                                weigh(0);
+                                load(2 * half + 1);
+                                largest();
+                                tell();
+                                weigh(16);
+                            } else {  // straight through, with no test for masked keys between the halves
+                                tmem_ld_x32(tS + 64 * half, x);
+                                tmem_wait_ld_of(x);
+                                largest();
+                                weigh(0);
+                                tmem_ld_x32(tS + 64 * half + 32, x);
+                                tmem_wait_ld_of(x);
+                                largest();
+                                tell();
+                                weigh(16);
                             }
-                            weigh(16);
                             ok = role_wait(pair, met & 1, wc);
                             if (!ok) break;
                             again |= *(volatile uint32_t*)&sh.flag[met & 1][stream][half ^ 1][quarter] != 0;
@@ -657,6 +673,8 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                             mx[0] = mx[1] = -INFINITY;
 #pragma unroll 1
                             for (int q = 0; q < kKeys / 32; ++q) {
+                                const int k0 = key0 + 32 * q;  // (nothing to find where no row of the warp sees any key)
+                                if (masked && !__any_sync(0xffffffffu, (bits(wlo - k0, lim - k0) | bits(0, min(a.sink - 1, lim) - k0)) != 0)) continue;
                                 load(q);
                                 largest();
                             }
@@ -744,41 +762,26 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                         continue;
                     }
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) o[k] = empty ? 0u : __float_as_uint(__uint_as_float(o[k]) * inv);
-                    if (a.out_f32 && row_valid) {
+                    for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * inv);
+                    if (__any_sync(0xffffffffu, empty)) {
 #pragma unroll
-                        for (int k = 0; k < 32; k += 4)
-                            *reinterpret_cast<uint4*>(a.out_f32 + at * D + d0 + k) = make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+                        for (int k = 0; k < 32; ++k) o[k] = empty ? 0u : o[k];
                     }
-                    __syncwarp();
-                    // A lane has 64 bytes of its row, in four words of 16; among four neighbouring lanes the words change places,
-                    // so that each store writes the 64 bytes of whole rows: lane 4 i + k, word k of the rows 4 i + 0 .. 3.
-                    uint32_t w[4][4];
+                    if (row_valid) {
+                        uint4* to = reinterpret_cast<uint4*>(a.out + at * D + d0);
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) w[k >> 2][k & 3] = pack_bf16x2(__uint_as_float(o[2 * k]), __uint_as_float(o[2 * k + 1]));
+                        for (int k = 0; k < 32; k += 8)
+                            to[k / 8] = make_uint4(pack_bf16x2(__uint_as_float(o[k]), __uint_as_float(o[k + 1])),
+                                                   pack_bf16x2(__uint_as_float(o[k + 2]), __uint_as_float(o[k + 3])),
+                                                   pack_bf16x2(__uint_as_float(o[k + 4]), __uint_as_float(o[k + 5])),
+                                                   pack_bf16x2(__uint_as_float(o[k + 6]), __uint_as_float(o[k + 7])));
+                        if (a.out_f32) {
 #pragma unroll
-                    for (int step = 1; step < 4; step <<= 1) {
-                        const bool up = lane & step;
-#pragma unroll
-                        for (int u = 0; u < 4; ++u) {
-                            if (u & step) continue;
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {  // this lane keeps word u (or u + step) and gives the other away
-                                const uint32_t give = up ? w[u][i] : w[u + step][i];
-                                const uint32_t got = __shfl_xor_sync(0xffffffffu, give, step);
-                                if (up) w[u][i] = got;
-                                else w[u + step][i] = got;
-                            }
+                            for (int k = 0; k < 32; k += 4)
+                                *reinterpret_cast<uint4*>(a.out_f32 + at * D + d0 + k) = make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
                         }
                     }
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        const int from = (lane & ~3) + u;  // the row's lane
-                        const int rt = __shfl_sync(0xffffffffu, row_t, from), rh = __shfl_sync(0xffffffffu, row_h, from);
-                        if (rt < a.rows_tile && i0 + rt < g.n)
-                            *reinterpret_cast<uint4*>(a.out + (((size_t)g.b * a.T + i0 + rt) * a.Hq + (size_t)g.kvh * a.G + rh) * D + d0 + 8 * (lane & 3)) =
-                                make_uint4(w[u][0], w[u][1], w[u][2], w[u][3]);
-                    }
+                    __syncwarp();
                 }
                 tc_fence_before_sync();
                 if (row_valid && half == 0) {
