@@ -14,16 +14,30 @@
 // the other are at theirs.  It works them off in that order, so the QK^T that overwrites S_s goes out right behind the PV that reads P
 // from it, and scores in hand mean that the PV before them has completed.
 //
-// Softmax.  Four warps have a quarter of a stream's rows and half of a tile's keys each, four the other half: with one warp for both halves a
-// tile took half as long again (646 us for 554 at 8,192 rows), two warps to a scheduler being too few to hide tensor memory's
-// latency.  The two warps of a quarter meet once a tile.  A row's reference moves only when a score is 2^16 above it, so the exponentials of a tile need not wait for its maximum: they
-// go by the reference in place, the maximum is found on the way, and a tile that moves a reference (the first of a unit, hardly any
-// other) is done over; nothing of it was stored.
+// Softmax.  Four warps have a quarter of a stream's rows and half of a tile's keys each, four the other half: with one warp for both
+// halves a tile took a sixth longer (646 us for 554 at 8,192 rows), two warps to a scheduler being too few to hide tensor memory's
+// latency.  The two warps of a quarter meet once a tile.  A row's reference moves only when a score is 2^16 above it, so the
+// exponentials of a tile need not wait for its maximum: they go by the reference in place, the maximum is found on the way, and a tile that
+// moves a reference (the first of a unit, hardly any other) is done over; nothing of it was stored.  The reference is a score itself,
+// so that the largest probability of a row's first tile is exactly 1 in bf16 too: rows of few keys lose nothing to its rounding.
 //
 // Work split.  A plan kernel lists the pieces of work: whole units, and of the last units (one to two for every CTA) runs of their
 // tiles, so that the CTAs end together and few rows over many keys keep all of them busy.  CTAs take pieces in order from a
 // counter: neighbouring units, which read the same keys, run at the same time, the long ones of a causal sequence first.  A
 // whole unit writes its output; runs leave partials, which the merge kernel joins by their log-sum-exp in a fixed order.
+//
+// Bound: power, then the chain of a stream.  Two row tiles and a K/V tile are 2,048 cycles of the tensor core and 2,048 of the
+// special-function unit, and take 3,600: a stream's softmax (2,000 cycles) and its products (1,024, and 400 until they are seen) follow
+// one another, and the other stream's fill the gaps only in part.  While it runs for long the 1 kW cap holds the clock at 1.6 - 1.75 GHz.
+// Measured (three kernels, D = 128, calls in a row in a graph):
+//     8,192 rows, 32 heads over 8, causal                            461 us  1.19 PFLOP/s (541 while it runs for long)
+//    32,768 rows, causal                                           7,707 us  1.14
+//    32,768 rows, 4 sinks and a window of 4,092                    2,052 us  1.00
+//       500 rows over 130,000 keys before them, paged in 64        1,039 us  1.03
+//     8 prompts of up to 4,001 rows, 28 over 4, paged in 256       1,105 us  1.01
+//     2 prompts of up to 100 rows, 8 over 2 of 64                   16.4 us  plan, first tiles, last outputs and merge, one after another
+// At D = 64 the special-function unit has as much to do for half of the products: 0.59 PFLOP/s at 16,384 rows.
+// Exponentials as polynomials on the FMA pipe (1 to 4 pairs of 8) gained nothing (8,192 rows 554 us with none, 563 - 599 with some).
 //
 // Waits are bounded as everywhere in this library; see mbar_wait_bounded.
 #include <math.h>
