@@ -812,17 +812,69 @@ def rapid_kv_read_fp8(k_cache, v_cache, k_scale, v_scale, ctx_lens, chunk_idx, c
 
 @lru_cache(maxsize=512)
 def _row_strides(x, st):
-    return _KvRows(*_told(x, st))
+    return ctypes.byref(_KvRows(*_told(x, st)))
 
 
 @lru_cache(maxsize=512)
-def _pool_geometry(k, kst, table):
-    return _PagedKv(k[2], k[0], table[1], 0, *_told(k, kst))
+def _turned(x, st, out, out_st, other, what):
+    """Strides of a tensor [B, T, heads, D] and of its output; ``other`` is the tensor that turns with it, or None."""
+    if len(x) != 4 or out != x:
+        raise ValueError(what + " and its output must be [B, T, heads, D]")
+    if other is not None and (x[0], x[1], x[3]) != (other[0], other[1], other[3]):
+        raise ValueError("q and k disagree on batch, rows or head_dim")
+    return _row_strides(x, st), _row_strides(out, out_st)
 
 
 @lru_cache(maxsize=512)
-def _append_geometry(k, kst, Hq, Lmax):
-    return _AttnShape(k[0], Hq, k[1], k[3], Lmax, *_told(k, kst))
+def _new_rows_geometry(new, nst, q, qst, q_out):
+    """(q's strides, the new rows' strides, query heads)"""
+    if len(new) != 4:
+        raise ValueError("k_new and v_new must be [B, T, Hkv, D]")
+    if q is None:
+        return None, _row_strides(new, nst), new[2]
+    if len(q) != 4 or (q[0], q[1], q[3]) != (new[0], new[1], new[3]) or q_out != q:
+        raise ValueError("q must be [B, T, Hq, D] with the new rows' B, T and D, q_out the same and dense")
+    return _row_strides(q, qst), _row_strides(new, nst), q[2]
+
+
+@lru_cache(maxsize=512)
+def _rope_cache_geometry(cache, cst, new, Hq):
+    """The cache that new rows [B, T, Hkv, D] go into."""
+    if len(cache) != 4 or (cache[0], cache[1], cache[3]) != (new[0], new[2], new[3]):
+        raise ValueError("k_cache and v_cache must be [B, Hkv, Lmax, D] of the new rows' batch, KV heads and head_dim")
+    return ctypes.byref(_AttnShape(cache[0], Hq, cache[1], cache[3], cache[2], *_told(cache, cst)))
+
+
+@lru_cache(maxsize=512)
+def _rope_pool_geometry(pool, pst, table, new, Hq):
+    """(pool, shape) that new rows [B, T, Hkv, D] go into through a table."""
+    if len(pool) != 4 or (pool[1], pool[3]) != (new[2], new[3]):
+        raise ValueError("k_pool and v_pool must be [num_blocks, Hkv, block_size, D] of the new rows' KV heads and head_dim")
+    if len(table) != 2 or table[0] != new[0]:
+        raise ValueError("block_table must be dense [B, max_blocks_per_seq]")
+    return (ctypes.byref(_PagedKv(pool[2], pool[0], table[1], 0, *_told(pool, pst))),
+            ctypes.byref(_AttnShape(new[0], Hq, new[2], new[3], table[1] * pool[2], 0, 0, 0)))
+
+
+@lru_cache(maxsize=512)
+def _prefill_geometry(q, qst, out, cache, cst):
+    if len(q) != 4 or out != q:
+        raise ValueError("q must be [B, T, Hq, D], out the same and dense")
+    if len(cache) != 4 or cache[0] != q[0] or cache[3] != q[3]:
+        raise ValueError("k_cache and v_cache must be [B, Hkv, Lmax, D] of q's batch and head_dim")
+    return _row_strides(q, qst), ctypes.byref(_AttnShape(cache[0], q[2], cache[1], cache[3], cache[2], *_told(cache, cst)))
+
+
+@lru_cache(maxsize=512)
+def _prefill_paged_geometry(q, qst, out, pool, pst, table):
+    if len(q) != 4 or out != q:
+        raise ValueError("q must be [B, T, Hq, D], out the same and dense")
+    if len(pool) != 4 or pool[3] != q[3]:
+        raise ValueError("k_pool and v_pool must be [num_blocks, Hkv, block_size, D] of q's head_dim")
+    if len(table) != 2 or table[0] != q[0]:
+        raise ValueError("block_table must be dense [B, max_blocks_per_seq]")
+    return (_row_strides(q, qst), ctypes.byref(_PagedKv(pool[2], pool[0], table[1], 0, *_told(pool, pst))),
+            ctypes.byref(_AttnShape(q[0], q[2], pool[1], q[3], table[1] * pool[2], 0, 0, 0)))
 
 
 @lru_cache(maxsize=64)
@@ -854,62 +906,50 @@ def _rope(rope, D, positions, B, T):
     return _Rope(f.data_ptr(), rope.rotary_dim, 1 if rope.interleaved else 0, rope.scale, axes, pairs)
 
 
-def _turned(x, y, what):
-    if not (x.dtype is y.dtype is _BF16):
-        raise TypeError(what + " and its output must be bfloat16")
-    if x.dim() != 4 or x.shape != y.shape:
-        raise ValueError(what + " and its output must be [B, T, heads, D]")
-    return x.shape, _row_strides(x.shape, x.stride()), _row_strides(y.shape, y.stride())
-
-
 def rapid_rope_apply(q, q_out, k, k_out, positions, rope: Rope, inverse: bool = False, stream=None) -> None:
     """Turns q [B, T, Hq, D] and k [B, T, Hkv, D] (bf16, may be strided; either may be None, with its output) by their
     positions [B, T] or [n_axes, B, T] (int32).  An output may be its input.  ``inverse`` turns back (the gradient)."""
     if (q is None) != (q_out is None) or (k is None) != (k_out is None) or (q is None and k is None):
         raise ValueError("q and k need an output each, and one of them has to be given")
-    shape = qr = qor = kr = kor = None
-    Hq = Hkv = 0
-    if q is not None:
-        shape, qr, qor = _turned(q, q_out, "q")
-        Hq = shape[2]
-    if k is not None:
-        ks, kr, kor = _turned(k, k_out, "k")
-        Hkv = ks[2]
-        if shape is not None and (ks[0], ks[1], ks[3]) != (shape[0], shape[1], shape[3]):
-            raise ValueError("q and k disagree on batch, rows or head_dim")
-        shape = ks
     if positions is None:
         raise ValueError("positions are required")
-    B, T, _, D = shape
+    for t in (q, q_out, k, k_out):
+        if t is not None and t.dtype is not _BF16:
+            raise TypeError("q, k and their outputs must be bfloat16")
+    qs = ks = qr = qor = kr = kor = None
+    if q is not None:
+        qs = q.shape
+        qr, qor = _turned(qs, q.stride(), q_out.shape, q_out.stride(), None, "q")
+    if k is not None:
+        ks = k.shape
+        kr, kor = _turned(ks, k.stride(), k_out.shape, k_out.stride(), qs, "k")
+    B, T, _, D = ks if qs is None else qs
     r = _rope(rope, D, positions, B, T)
     st = _here(stream, q, q_out, k, k_out, positions, rope.inv_freq)
-    ref = lambda g: None if g is None else ctypes.byref(g)  # noqa: E731
-    _check(load_library().rapid_rope_apply(_addr(q), ref(qr), _addr(q_out), ref(qor), _addr(k), ref(kr), _addr(k_out), ref(kor),
-                                           B, T, Hq, Hkv, D, positions.data_ptr(), ctypes.byref(r), 1 if inverse else 0, st))
+    _check(load_library().rapid_rope_apply(_addr(q), qr, _addr(q_out), qor, _addr(k), kr, _addr(k_out), kor, B, T,
+                                           0 if qs is None else qs[2], 0 if ks is None else ks[2], D, positions.data_ptr(),
+                                           ctypes.byref(r), 1 if inverse else 0, st))
 
 
-def _append_rows(q, k_new, v_new, q_out, n_tokens, ctx_lens, ctx_lens_out):
-    """(B, T, Hq, Hkv, D) and the strides of q and of the new rows"""
-    if not (k_new.dtype is v_new.dtype is _BF16):
-        raise TypeError("k_new / v_new must be bfloat16")
-    shape, stride = _alike(k_new, v_new, "k_new and v_new")
-    if len(shape) != 4:
-        raise ValueError("k_new and v_new must be [B, T, Hkv, D]")
-    B, T, Hkv, D = shape
-    Hq, qr = Hkv, None
-    if (q is None) != (q_out is None):
-        raise ValueError("q needs q_out, and q_out needs q")
-    if q is not None:
+def _append_rows(q, k_new, v_new, q_out, k_cache, v_cache, n_tokens, ctx_lens, ctx_lens_out):
+    """(shape of the new rows, q's strides, the rows' strides, query heads)"""
+    if not (k_new.dtype is v_new.dtype is k_cache.dtype is v_cache.dtype is _BF16):
+        raise TypeError("the new rows and the cache must be bfloat16")
+    new, nst = _alike(k_new, v_new, "k_new and v_new")
+    if q is None or q_out is None:
+        if q is not q_out:
+            raise ValueError("q needs q_out, and q_out needs q")
+        qr, rows, Hq = _new_rows_geometry(new, nst, None, None, None)
+    else:
         if not (q.dtype is q_out.dtype is _BF16):
             raise TypeError("q and q_out must be bfloat16")
-        qs = q.shape
-        if len(qs) != 4 or (qs[0], qs[1], qs[3]) != (B, T, D) or q_out.shape != qs or not q_out.is_contiguous():
-            raise ValueError("q must be [B, T, Hq, D] with the new rows' B, T and D, q_out the same and dense")
-        Hq, qr = qs[2], ctypes.byref(_row_strides(qs, q.stride()))
-    _lens(n_tokens, B, "n_tokens")
-    _lens(ctx_lens, B, "ctx_lens")
-    _lens(ctx_lens_out, B, "ctx_lens_out")
-    return B, T, Hq, Hkv, D, qr, ctypes.byref(_row_strides(shape, stride))
+        if not q_out.is_contiguous():
+            raise ValueError("q_out must be dense")
+        qr, rows, Hq = _new_rows_geometry(new, nst, q.shape, q.stride(), q_out.shape)
+    _lens(n_tokens, new[0], "n_tokens")
+    _lens(ctx_lens, new[0], "ctx_lens")
+    _lens(ctx_lens_out, new[0], "ctx_lens_out")
+    return new, qr, rows, Hq
 
 
 def rapid_kv_append_rope(q, k_new, v_new, q_out, k_cache, v_cache, ctx_lens, ctx_lens_out, rope: Rope, status_word,
@@ -918,42 +958,33 @@ def rapid_kv_append_rope(q, k_new, v_new, q_out, k_cache, v_cache, ctx_lens, ctx
     them and turns q [B, T, Hq, D] into q_out (bf16; q and the new rows may be strided, q may be None).  n_tokens [B] of the
     rows count (None: all); positions as in rapid_rope_apply (None: ctx_lens + row); ctx_lens_out (None, another tensor, or
     ctx_lens itself) receives ctx_lens + n_tokens."""
-    B, T, Hq, Hkv, D, qr, rows = _append_rows(q, k_new, v_new, q_out, n_tokens, ctx_lens, ctx_lens_out)
-    if not (k_cache.dtype is v_cache.dtype is _BF16):
-        raise TypeError("k_cache / v_cache must be bfloat16")
-    cache, stride = _alike(k_cache, v_cache, "k_cache and v_cache")
-    if len(cache) != 4 or (cache[0], cache[1], cache[3]) != (B, Hkv, D):
-        raise ValueError("k_cache and v_cache must be [B, Hkv, Lmax, D] of the new rows' batch, KV heads and head_dim")
-    geometry = _append_geometry(cache, stride, Hq, cache[2])
-    r = _rope(rope, D, positions, B, T)
+    new, qr, rows, Hq = _append_rows(q, k_new, v_new, q_out, k_cache, v_cache, n_tokens, ctx_lens, ctx_lens_out)
+    geometry = _rope_cache_geometry(*_alike(k_cache, v_cache, "k_cache and v_cache"), new, Hq)
+    r = _rope(rope, new[3], positions, new[0], new[1])
     st = _here(stream, q, k_new, v_new, q_out, k_cache, v_cache, ctx_lens, ctx_lens_out, rope.inv_freq, status_word, n_tokens,
                positions)
     _check(load_library().rapid_kv_append_rope(
-        _addr(q), qr, k_new.data_ptr(), v_new.data_ptr(), rows, T, _addr(n_tokens), _addr(q_out), k_cache.data_ptr(),
-        v_cache.data_ptr(), ctx_lens.data_ptr(), _addr(ctx_lens_out), ctypes.byref(r), _addr(positions), ctypes.byref(geometry),
+        _addr(q), qr, k_new.data_ptr(), v_new.data_ptr(), rows, new[1], _addr(n_tokens), _addr(q_out), k_cache.data_ptr(),
+        v_cache.data_ptr(), ctx_lens.data_ptr(), _addr(ctx_lens_out), ctypes.byref(r), _addr(positions), geometry,
         status_word.data_ptr(), st))
 
 
 def rapid_kv_append_rope_paged(q, k_new, v_new, q_out, k_pool, v_pool, block_table, ctx_lens, ctx_lens_out, rope: Rope,
                                status_word, n_tokens=None, positions=None, stream=None) -> None:
     """rapid_kv_append_rope into pools [num_blocks, Hkv, block_size, D] through block_table [B, max_blocks] (int32)."""
-    B, T, Hq, Hkv, D, qr, rows = _append_rows(q, k_new, v_new, q_out, n_tokens, ctx_lens, ctx_lens_out)
-    if not (k_pool.dtype is v_pool.dtype is _BF16) or block_table.dtype is not _I32:
-        raise TypeError("the pools must be bfloat16, block_table int32")
-    pool, stride = _alike(k_pool, v_pool, "k_pool and v_pool")
-    if len(pool) != 4 or (pool[1], pool[3]) != (Hkv, D):
-        raise ValueError("k_pool and v_pool must be [num_blocks, Hkv, block_size, D] of the new rows' KV heads and head_dim")
-    if block_table.dim() != 2 or block_table.shape[0] != B or not block_table.is_contiguous():
+    new, qr, rows, Hq = _append_rows(q, k_new, v_new, q_out, k_pool, v_pool, n_tokens, ctx_lens, ctx_lens_out)
+    if block_table.dtype is not _I32:
+        raise TypeError("block_table must be int32")
+    if not block_table.is_contiguous():
         raise ValueError("block_table must be dense [B, max_blocks_per_seq]")
-    paged = _pool_geometry(pool, stride, block_table.shape)
-    shape = _AttnShape(B, Hq, Hkv, D, block_table.shape[1] * pool[2], 0, 0, 0)
-    r = _rope(rope, D, positions, B, T)
+    paged, geometry = _rope_pool_geometry(*_alike(k_pool, v_pool, "k_pool and v_pool"), block_table.shape, new, Hq)
+    r = _rope(rope, new[3], positions, new[0], new[1])
     st = _here(stream, q, k_new, v_new, q_out, k_pool, v_pool, block_table, ctx_lens, ctx_lens_out, rope.inv_freq, status_word,
                n_tokens, positions)
     _check(load_library().rapid_kv_append_rope_paged(
-        _addr(q), qr, k_new.data_ptr(), v_new.data_ptr(), rows, T, _addr(n_tokens), _addr(q_out), k_pool.data_ptr(),
-        v_pool.data_ptr(), block_table.data_ptr(), ctypes.byref(paged), ctx_lens.data_ptr(), _addr(ctx_lens_out),
-        ctypes.byref(r), _addr(positions), ctypes.byref(shape), status_word.data_ptr(), st))
+        _addr(q), qr, k_new.data_ptr(), v_new.data_ptr(), rows, new[1], _addr(n_tokens), _addr(q_out), k_pool.data_ptr(),
+        v_pool.data_ptr(), block_table.data_ptr(), paged, ctx_lens.data_ptr(), _addr(ctx_lens_out), ctypes.byref(r),
+        _addr(positions), geometry, status_word.data_ptr(), st))
 
 
 def prefill_attention_workspace_bytes(B, Hq, Hkv, D, T) -> int:
@@ -962,24 +993,23 @@ def prefill_attention_workspace_bytes(B, Hq, Hkv, D, T) -> int:
     return int(load_library().rapid_prefill_attention_workspace_bytes(ctypes.byref(s), T))
 
 
-def _prefill_rows(q, out, ctx_lens, n_tokens, params):
-    """(shape of q, its strides, lse_out, out_f32)"""
+def _prefill_outputs(q, out, ctx_lens, n_tokens, params):
+    """(lse_out, out_f32)"""
     if not (q.dtype is out.dtype is _BF16):
         raise TypeError("q and out must be bfloat16")
-    shape = q.shape
-    if len(shape) != 4 or out.shape != shape or not out.is_contiguous():
-        raise ValueError("q must be [B, T, Hq, D], out the same and dense")
+    if not out.is_contiguous():
+        raise ValueError("out must be dense [B, T, Hq, D]")
     if ctx_lens is None:
         raise ValueError("ctx_lens are required")
-    _lens(ctx_lens, shape[0], "ctx_lens")
-    _lens(n_tokens, shape[0], "n_tokens")
-    lse = o32 = None
-    if params is not None:
-        lse, o32 = params.lse_out, params.out_f32
-        for t, n in ((lse, q.numel() // shape[3]), (o32, q.numel())):
-            if t is not None and (t.dtype is not _F32 or t.numel() != n or not t.is_contiguous()):
-                raise ValueError("lse_out must be dense float32 [B, T, Hq] and out_f32 [B, T, Hq, D]")
-    return shape, ctypes.byref(_row_strides(shape, q.stride())), lse, o32
+    B = q.shape[0]
+    _lens(ctx_lens, B, "ctx_lens")
+    _lens(n_tokens, B, "n_tokens")
+    if params is None:
+        return None, None
+    for t, n in ((params.lse_out, q.numel() // q.shape[-1]), (params.out_f32, q.numel())):
+        if t is not None and (t.dtype is not _F32 or t.numel() != n or not t.is_contiguous()):
+            raise ValueError("lse_out must be dense float32 [B, T, Hq] and out_f32 [B, T, Hq, D]")
+    return params.lse_out, params.out_f32
 
 
 def rapid_prefill_attention(q, k_cache, v_cache, ctx_lens, out, workspace, n_tokens=None, params: Optional[AttnParams] = None,
@@ -989,15 +1019,12 @@ def rapid_prefill_attention(q, k_cache, v_cache, ctx_lens, out, workspace, n_tok
     sink_keys or all_keys_visible.  bf16."""
     if not (k_cache.dtype is v_cache.dtype is _BF16):
         raise TypeError("k_cache / v_cache must be bfloat16")
-    shape, rows, lse, o32 = _prefill_rows(q, out, ctx_lens, n_tokens, params)
-    cache, stride = _alike(k_cache, v_cache, "k_cache and v_cache")
-    if len(cache) != 4 or cache[0] != shape[0] or cache[3] != shape[3]:
-        raise ValueError("k_cache and v_cache must be [B, Hkv, Lmax, D] of q's batch and head_dim")
-    geometry = _append_geometry(cache, stride, shape[2], cache[2])
-    st = _here(stream, q, k_cache, v_cache, ctx_lens, out, workspace, n_tokens, lse, o32)
+    extra = _prefill_outputs(q, out, ctx_lens, n_tokens, params)
+    rows, geometry = _prefill_geometry(q.shape, q.stride(), out.shape, *_alike(k_cache, v_cache, "k_cache and v_cache"))
+    st = _here(stream, q, k_cache, v_cache, ctx_lens, out, workspace, n_tokens, *extra)
     _check(load_library().rapid_prefill_attention(
-        q.data_ptr(), rows, shape[1], _addr(n_tokens), k_cache.data_ptr(), v_cache.data_ptr(), ctx_lens.data_ptr(), out.data_ptr(),
-        ctypes.byref(geometry), _attn_params(params), workspace.data_ptr(), _nbytes(workspace), st))
+        q.data_ptr(), rows, q.shape[1], _addr(n_tokens), k_cache.data_ptr(), v_cache.data_ptr(), ctx_lens.data_ptr(), out.data_ptr(),
+        geometry, _attn_params(params), workspace.data_ptr(), _nbytes(workspace), st))
 
 
 def rapid_prefill_attention_paged(q, k_pool, v_pool, block_table, ctx_lens, out, workspace, n_tokens=None,
@@ -1005,19 +1032,15 @@ def rapid_prefill_attention_paged(q, k_pool, v_pool, block_table, ctx_lens, out,
     """rapid_prefill_attention over pools [num_blocks, Hkv, block_size, D] through block_table [B, max_blocks] (int32)."""
     if not (k_pool.dtype is v_pool.dtype is _BF16) or block_table.dtype is not _I32:
         raise TypeError("the pools must be bfloat16, block_table int32")
-    shape, rows, lse, o32 = _prefill_rows(q, out, ctx_lens, n_tokens, params)
-    pool, stride = _alike(k_pool, v_pool, "k_pool and v_pool")
-    if len(pool) != 4 or pool[3] != shape[3]:
-        raise ValueError("k_pool and v_pool must be [num_blocks, Hkv, block_size, D] of q's head_dim")
-    if block_table.dim() != 2 or block_table.shape[0] != shape[0] or not block_table.is_contiguous():
+    if not block_table.is_contiguous():
         raise ValueError("block_table must be dense [B, max_blocks_per_seq]")
-    paged = _pool_geometry(pool, stride, block_table.shape)
-    geometry = _AttnShape(shape[0], shape[2], pool[1], shape[3], block_table.shape[1] * pool[2], 0, 0, 0)
-    st = _here(stream, q, k_pool, v_pool, block_table, ctx_lens, out, workspace, n_tokens, lse, o32)
+    extra = _prefill_outputs(q, out, ctx_lens, n_tokens, params)
+    rows, paged, geometry = _prefill_paged_geometry(q.shape, q.stride(), out.shape, *_alike(k_pool, v_pool, "k_pool and v_pool"),
+                                                    block_table.shape)
+    st = _here(stream, q, k_pool, v_pool, block_table, ctx_lens, out, workspace, n_tokens, *extra)
     _check(load_library().rapid_prefill_attention_paged(
-        q.data_ptr(), rows, shape[1], _addr(n_tokens), k_pool.data_ptr(), v_pool.data_ptr(), block_table.data_ptr(),
-        ctypes.byref(paged), ctx_lens.data_ptr(), out.data_ptr(), ctypes.byref(geometry), _attn_params(params),
-        workspace.data_ptr(), _nbytes(workspace), st))
+        q.data_ptr(), rows, q.shape[1], _addr(n_tokens), k_pool.data_ptr(), v_pool.data_ptr(), block_table.data_ptr(), paged,
+        ctx_lens.data_ptr(), out.data_ptr(), geometry, _attn_params(params), workspace.data_ptr(), _nbytes(workspace), st))
 
 
 def rapid_step_commit(ctx_lens, accept_len, gamma, status_word, stream=None) -> None:
