@@ -164,11 +164,11 @@ __device__ __forceinline__ int block_scan(int v, int* sh, int* total) {
 __global__ void __launch_bounds__(kPlanThreads) prefill_plan_kernel(const __grid_constant__ PrefillArgs a) {
     __shared__ int sh_start[kSeqInSmem + 1], sh_scan[kPlanThreads / 32], sizes[kPlanThreads];
     __shared__ float sh_est[kPlanThreads / 32];
-    __shared__ int sh_len[kPlanThreads / 32];
+    __shared__ int sh_len[kPlanThreads / 32], sh_shapes;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     griddep_wait();
     griddep_launch_dependents();
-    if (tid == 0) *a.plan_sig = 0;
+    if (tid == 0) *a.plan_sig = 0, sh_shapes = 0;
     const bool in_smem = a.B <= kSeqInSmem;
     int units = 0;
     for (int b0 = 0; b0 < a.B; b0 += kPlanThreads) {
@@ -231,29 +231,33 @@ __global__ void __launch_bounds__(kPlanThreads) prefill_plan_kernel(const __grid
         int most = 0;
         for (int i = lane; i < tail; i += 32) most = max(most, sizes[i]);
         most = __reduce_max_sync(0xffffffffu, most);
-        const int parts = max(1, (int)((long long)(warp + 1) * a.num_ctas / max(tail, 1)));
-        const int len = max(1, (most + parts - 1) / parts);
-        int count = 0, cut = 0;
-        long long sum = 0;
-        for (int i = lane; i < tail; i += 32) {
-            const int c = max(1, (sizes[i] + len - 1) / len);
-            count += c;
-            cut += c > 1 ? c : 0;
-            sum += sizes[i];
-        }
-        count = __reduce_add_sync(0xffffffffu, count);
-        cut = __reduce_add_sync(0xffffffffu, cut);
-        float all = (float)sum;
+        if (most > 2) {  // (to cut one or two tiles never pays)
+            const int parts = max(1, (int)((long long)(warp + 1) * a.num_ctas / max(tail, 1)));
+            const int len = max(1, (most + parts - 1) / parts);
+            int count = 0, cut = 0;
+            long long sum = 0;
+            for (int i = lane; i < tail; i += 32) {
+                const int c = max(1, (sizes[i] + len - 1) / len);
+                count += c;
+                cut += c > 1 ? c : 0;
+                sum += sizes[i];
+            }
+            count = __reduce_add_sync(0xffffffffu, count);
+            cut = __reduce_add_sync(0xffffffffu, cut);
+            float all = (float)sum;
 #pragma unroll
-        for (int o = 16; o; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
-        if (lane == 0) {
-            const float mean = (all + kPieceCost * count) / max(count, 1), top = len + kPieceCost;
-            float est = whole ? mean * count / a.num_ctas + 0.25f * top
-                              : mean * ((count + a.num_ctas - 1) / a.num_ctas) + top - mean;
-            if (cut) est += kMergeCost + kSlotCost * cut;
-            if (cut > a.max_slots || count > kMaxTail) est = INFINITY;
-            sh_est[warp] = est;
-            sh_len[warp] = len;
+            for (int o = 16; o; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+            if (lane == 0) {
+                const float mean = (all + kPieceCost * count) / max(count, 1), top = len + kPieceCost;
+                float est = whole ? mean * count / a.num_ctas + 0.25f * top
+                                  : mean * ((count + a.num_ctas - 1) / a.num_ctas) + top - mean;
+                if (cut) est += kMergeCost + kSlotCost * cut;
+                if (cut > a.max_slots || count > kMaxTail) est = INFINITY;
+                sh_est[warp] = est;
+                sh_len[warp] = len;
+            }
+        } else if (lane == 0) {
+            sh_est[warp] = INFINITY;
         }
         __syncthreads();
     }
@@ -263,11 +267,14 @@ __global__ void __launch_bounds__(kPlanThreads) prefill_plan_kernel(const __grid
     for (int w = 0; w < kPlanThreads / 32; ++w)
         if (sh_est[w] < best) best = sh_est[w], len = sh_len[w];
     const int parts = tid >= tail ? 0 : best == INFINITY ? 1 : max(1, (mine.tiles + len - 1) / len);
-    const int cut_parts = parts > 1 ? parts : 0;
-    int pieces, slots, cuts;
-    const int piece0 = block_scan(parts, sh_scan, &pieces) - parts;
-    const int slot0 = block_scan(cut_parts, sh_scan, &slots) - cut_parts;
-    const int cut0 = block_scan(parts > 1, sh_scan, &cuts) - (parts > 1);
+    // pieces, partials and cut units before this thread's, in one sum: each is at most 640, ten bits
+    static_assert(kMaxTail < 1024 && kPlanThreads <= 512, "fields of ten bits");
+    if (parts > 1) atomicOr(&sh_shapes, parts <= kFewParts ? kSomeFew : kSomeMany);
+    const int one = parts | (parts > 1 ? parts << 10 | 1 << 20 : 0);
+    int sums;
+    const int before = block_scan(one, sh_scan, &sums) - one;
+    const int piece0 = before & 1023, slot0 = before >> 10 & 1023, cut0 = before >> 20;
+    const int pieces = sums & 1023, cuts = sums >> 20;
     if (tid < tail) {
         const int tiles = mine.tiles;
         for (int i = 0; i < parts; ++i) {
@@ -279,10 +286,9 @@ __global__ void __launch_bounds__(kPlanThreads) prefill_plan_kernel(const __grid
         }
         if (parts > 1) a.cuts[cut0] = {mine.b, mine.kvh, mine.row0, mine.n, slot0, parts, 0, 0};
     }
-    const int few = __syncthreads_or(parts > 1 && parts <= kFewParts), many = __syncthreads_or(parts > kFewParts);
     // (a CTA's first piece is the one of its own number: where there are fewer, an end marker)
     for (int i = whole + pieces + tid; i < a.num_ctas; i += kPlanThreads) a.pieces[i].tiles = -1;
-    if (tid == 0) *a.control = {a.num_ctas, whole + pieces, cuts, (few ? kSomeFew : 0) | (many ? kSomeMany : 0)};
+    if (tid == 0) *a.control = {a.num_ctas, whole + pieces, cuts, sh_shapes};
 }
 
 constexpr int kRing = 2;                          // pieces a CTA has in hand: the one at work and the next
