@@ -35,7 +35,7 @@
 //    32,768 rows, 4 sinks and a window of 4,092                    2,052 us  1.00
 //       500 rows over 130,000 keys before them, paged in 64        1,039 us  1.03
 //     8 prompts of up to 4,001 rows, 28 over 4, paged in 256       1,105 us  1.01
-//     2 prompts of up to 100 rows, 8 over 2 of 64                   16.4 us  plan, first tiles, last outputs and merge, one after another
+//     2 prompts of up to 100 rows, 8 over 2 of 64                   15.3 us  plan, first tiles, last outputs and merge, one after another
 // At D = 64 the special-function unit has as much to do for half of the products: 0.59 PFLOP/s at 16,384 rows.
 // Exponentials as polynomials on the FMA pipe (1 to 4 pairs of 8) gained nothing (8,192 rows 554 us with none, 563 - 599 with some).
 //
