@@ -660,6 +660,7 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                             auto tell = [&] {  // the other half of the keys; and neither warp writes over scores that the other has not read
                                 const float top = max3(mx[0], mx[1], mx[1]) * c;
                                 again = __any_sync(0xffffffffu, row_valid && !(top <= m_ref + kJump) && top != -INFINITY);
+                                tc_fence_before_sync();
                                 if (lane == 0) {
                                     sh.flag[met & 1][stream][half][quarter] = again;
                                     mbar_arrive(pair);
@@ -686,6 +687,7 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                             }
                             ok = role_wait(pair, met & 1, wc);
                             if (!ok) break;
+                            tc_fence_after_sync();
                             again |= *(volatile uint32_t*)&sh.flag[met & 1][stream][half ^ 1][quarter] != 0;
                             ++met;
                         }
@@ -711,10 +713,12 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                             weigh(0);
                             load(2 * half + 1);
                             weigh(16);
+                            tc_fence_before_sync();
                             __syncwarp();
                             if (lane == 0) mbar_arrive(pair);
                             ok = role_wait(pair, met & 1, wc);
                             if (!ok) break;
+                            tc_fence_after_sync();
                             ++met;
                         }
                         tmem_st_x32(tS + 32 * half, pk);
