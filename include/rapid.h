@@ -428,8 +428,8 @@ typedef struct rapid_kv_rows {
  * rapid_attn_params; key tiles that no row sees are not read), or, with all_keys_visible, of all ctx_lens[b] keys.
  *   q            : device bf16, T rows per sequence, geometry of q_rows (NULL = dense [B, T, Hq, D]; strides multiples of 8)
  *   n_tokens     : device int32 [B], rows that count, in [0, T]; or NULL = T each
- *   k_cache, v_cache : device bf16, geometry of `shape` (strides honoured); entries at positions >= ctx_lens[b] are
- *                  never used, whatever their bits
+ *   k_cache, v_cache : device bf16, geometry of `shape` (strides honoured); entries at positions >= ctx_lens[b], and those
+ *                  between the sinks and the window that no row sees, are never used, whatever their bits
  *   ctx_lens     : device int32 [B], keys in the cache, the new rows included: in [n, Lmax] (in [0, Lmax] with
  *                  all_keys_visible)
  *   out          : device bf16 [B, T, Hq, D], dense; rows behind n_tokens[b] are left as they were, here as in

@@ -341,6 +341,26 @@ __device__ __forceinline__ uint32_t bits(int lo, int hi) {
     return r;
 }
 
+// A V row that no row of a unit sees may hold any bits, and 0 * NaN is NaN.  A stream's softmax warps zero those of a tile: past the keys
+// and, in the last tile of the sinks and the first one of the window, between the two.  Few tiles have any: kept out of the loop's way.
+template <int D>
+__device__ __noinline__ bool zero_hidden(uint8_t* v, Shared<D>& sh, const PrefillArgs& a, int ring, int key0, int tile, WaitCtx wc) {
+    const Piece& g = sh.piece[ring];
+    const int end = min(g.L - key0, kKeys), from = max(a.sink - key0, 0);
+    const int to = min(max(g.L - g.n + g.row0 - a.window + 1, 0) - key0, kKeys);
+    const int between = a.window ? max(to - from, 0) : 0, chunks = (between + kKeys - end) * 8;
+    if (chunks == 0) return true;
+    const int slot = tile % v_slots(D);
+    if (!role_wait(&sh.v_full[slot], (tile / v_slots(D)) & 1, wc)) return false;
+    for (int ch = threadIdx.x & 255; ch < chunks; ch += 256) {
+        const int r = ch >> 3, at = (r < between ? from + r : end + r - between) * 128 + (ch & 7) * 16;
+#pragma unroll
+        for (int h = 0; h < D / 64; ++h) *reinterpret_cast<uint4*>(v + slot * tile_bytes(D) + h * kHalfBytes + at) = make_uint4(0, 0, 0, 0);
+    }
+    fence_proxy_async_smem();
+    return true;
+}
+
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
 prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
@@ -726,19 +746,9 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                         f32x2_split(f32x2_add(acc[0], acc[1]), s0, s1);
                         l_run += s0 + s1;
                     }
-                    if (key0 + kKeys > g.L) {
-                        // V rows past the keys may hold any bits: zero them so that 0 * row = 0
-                        const int vt = n_tiles + t, vs = vt % NV;
-                        ok = role_wait(&sh.v_full[vs], (vt / NV) & 1, wc);
+                    if (key0 + kKeys > g.L || (a.window && u <= sp.sinks)) {  // V rows that no row of the unit sees
+                        ok = zero_hidden<D>(smem + OFF_V, sh, a, r % kRing, key0, n_tiles + t, wc);
                         if (!ok) break;
-                        const int bad = g.L - key0;
-                        const int chunks = (kKeys - bad) * 8;
-#pragma unroll
-                        for (int h = 0; h < NH; ++h)
-                            for (int ch = half * 128 + row; ch < chunks; ch += 256)
-                                *reinterpret_cast<uint4*>(smem + OFF_V + vs * TILE + h * kHalfBytes + bad * 128 + ch * 16) =
-                                    make_uint4(0, 0, 0, 0);
-                        fence_proxy_async_smem();
                     }
                     tmem_wait_st();
                     tc_fence_before_sync();
