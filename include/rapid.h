@@ -449,7 +449,11 @@ int rapid_prefill_attention(const void* q, const rapid_kv_rows* q_rows, int T, c
                             const void* v_cache, const int32_t* ctx_lens, void* out, const rapid_attn_shape* shape,
                             const rapid_attn_params* params, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
-/* The same over a paged cache (see rapid_paged_kv); shape->Lmax, table and bad entries as in rapid_verify_attention_paged. */
+/*
+ * The same over a paged cache (see rapid_paged_kv); shape->Lmax, table and bad entries as in rapid_verify_attention_paged.
+ * With window_keys, entries of blocks that lie wholly between the sinks and the window, so that no row sees any of their keys,
+ * are not read: such blocks may have been given back.
+ */
 int rapid_prefill_attention_paged(const void* q, const rapid_kv_rows* q_rows, int T, const int32_t* n_tokens,
                                   const void* k_pool, const void* v_pool, const int32_t* block_table,
                                   const rapid_paged_kv* paged, const int32_t* ctx_lens, void* out,

@@ -424,6 +424,7 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
             const Piece g = sh.piece[r % kRing];
             const Span sp = sh.span[r % kRing];
             if (!ok || g.tiles < 0) break;
+            const int oldest = a.window ? g.L - g.n + g.row0 - a.window + 1 : 0;  // key of the unit's windows
 #pragma unroll 1
             for (int t = 0; t < g.tiles && ok; ++t) {
                 const int u = g.first + t;
@@ -434,8 +435,8 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                     for (int q = 0; q < parts; ++q) {
                         const int pos = key0 + q * a.box_rows;
                         c1[q] = pos & (a.block_size - 1);
-                        if (pos >= g.L) {
-                            c3[q] = a.num_blocks;  // past the keys: zeros, no table entry is read
+                        if (pos >= g.L || (pos >= a.sink && pos + a.box_rows <= oldest)) {
+                            c3[q] = a.num_blocks;  // past the keys, or hidden from the unit: zeros, no table entry is read
                             continue;
                         }
                         c3[q] = __ldg(a.block_table + (size_t)g.b * a.max_blocks + (pos >> a.block_log2));

@@ -44,3 +44,20 @@ def test_values_that_no_row_sees_hold_anything(B, T, Hq, Hkv, D, old, block, win
     c.run(window_keys=window, sink_keys=sink)
     assert R.workspace_status(c.ws) == 0
     assert torch.equal(out, c.out) and torch.equal(lse, c.lse)
+
+
+@pytest.mark.parametrize("B,T,Hq,Hkv,D,old,block,window,sink", [s for s in SHAPES if 0 < s[6] < 256])
+def test_blocks_that_no_row_sees_are_given_back(B, T, Hq, Hkv, D, old, block, window, sink):
+    """Table entries of blocks between the sinks and the window, taken out as a cache that gives such blocks back does."""
+    c = _Case(B, T, Hq, Hkv, D, old, block, seed=72)
+    c.run(window_keys=window, sink_keys=sink)
+    assert R.workspace_status(c.ws) == 0
+    out, lse = c.out.clone(), c.lse.clone()
+    for b in range(B):
+        hidden = _hidden(c, b, window, sink)
+        for i in range(-(-hidden.start // block), hidden.stop // block):
+            c.table[b, i] = -1
+    assert (c.table[0, :old // block] == -1).any()
+    c.run(window_keys=window, sink_keys=sink)
+    assert R.workspace_status(c.ws) == 0
+    assert torch.equal(out, c.out) and torch.equal(lse, c.lse)
