@@ -147,7 +147,8 @@ typedef struct rapid_attn_params {
                                  keys-on-M kernel); ignored elsewhere                                   */
     int64_t wait_cycle_limit; /* SM clock cycles an on-chip wait (for a tile, for the tensor cores) may take
                                  before the kernel gives up and sets RAPID_STATUS_PIPELINE_TIMEOUT;
-                                 0 = the library's limit of about a second                              */
+                                 0 = the library's limit of about a second (2 * 10^9 cycles).  In
+                                 rapid_prefill_attention some waits last longer than a tile: see there   */
     int32_t kv_settled;       /* non-zero, together with plan = RAPID_PLAN_SETTLED and a contiguous cache: the
                                  caller states that every K/V entry OLDER than the R newest keys of each
                                  sequence (positions below ctx_lens[b] - R) was final before the work that
@@ -442,6 +443,9 @@ typedef struct rapid_kv_rows {
  * RAPID_STATUS_BAD_CTX_LEN.  A row that sees no key is 0, its log-sum-exp -inf.  fp32 accumulation, bf16 probabilities in the
  * second product; lse_out, the range of V, values that are not finite and keys of next to no weight are as in
  * rapid_verify_attention_prefix.  Three kernels per call; lengths are read on the device, so a captured call follows them.
+ * wait_cycle_limit: the parts of a CTA hand pieces of work to one another, and wait for as long as a piece takes: a run of up to
+ * ceil(keys / 128) key tiles of one KV head.  A limit has to cover the longest: 10,000 cycles a tile and 100,000 beside are
+ * enough (the library's own covers sequences of 25 million keys); a shorter one may end a call that would have gone through.
  */
 size_t rapid_prefill_attention_workspace_bytes(const rapid_attn_shape* shape, int T);
 

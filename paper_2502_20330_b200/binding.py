@@ -108,7 +108,7 @@ class AttnParams:
     sink_keys: int = 0                       # with window_keys: the first keys every row keeps seeing
     window_keys: int = 0                     # > 0: each row sees only that many newest keys up to its own
     plan: int = 0                            # PLAN_*: the workspace holds a plan made by rapid_attention_plan
-    wait_cycle_limit: int = 0                # clock cycles an on-chip wait may take; 0 = the library's limit
+    wait_cycle_limit: int = 0                # clock cycles an on-chip wait may take (prefill: the longest piece of work); 0 = the library's limit
     kv_fp8: bool = False                     # rapid_attention_plan / describe: the plan is for the FP8-cache call
     kv_settled: bool = False                 # with plan = PLAN_SETTLED: all but the newest R keys were final before
                                              # the preceding work was issued; their tiles may be copied early
