@@ -1057,12 +1057,14 @@ int launch_prefill_attention(const void* q, const rapid_kv_rows* q_rows, int T, 
         return RAPID_ERR_UNSUPPORTED;
     }
     const bool all_visible = params && params->all_keys_visible;
-    const int sink = params ? params->sink_keys : 0, window = params ? params->window_keys : 0;
+    int sink = params ? params->sink_keys : 0, window = params ? params->window_keys : 0;
     if (sink < 0 || window < 0 || (sink > 0 && window == 0) || (window > 0 && all_visible)) {
         set_error("%s: sink_keys and window_keys must not be negative, sink_keys needs a window, and a window cannot be combined with "
                   "all_keys_visible", who);
         return RAPID_ERR_INVALID_ARG;
     }
+    // (a window as long as the cache hides nothing; below that the differences of keys and windows stay within 32 bits)
+    if (window >= s.Lmax) sink = window = 0;
     const int G = s.Hq / s.Hkv;
     int64_t sl, sh, sb, keys, outer;
     int block_log2 = 0;

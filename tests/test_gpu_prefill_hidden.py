@@ -61,3 +61,17 @@ def test_blocks_that_no_row_sees_are_given_back(B, T, Hq, Hkv, D, old, block, wi
     c.run(window_keys=window, sink_keys=sink)
     assert R.workspace_status(c.ws) == 0
     assert torch.equal(out, c.out) and torch.equal(lse, c.lse)
+
+
+@pytest.mark.parametrize("D,block", [(64, 0), (128, 64)])
+def test_a_window_over_the_whole_cache_is_no_window(D, block):
+    """Windows from the cache's length to the largest there is, with sinks up to the largest: the plain causal mask, bit for bit."""
+    c = _Case(2, 300, 8, 2, D, 500, block, seed=75, slack=0)
+    c.run().check()
+    out, lse = c.out.clone(), c.lse.clone()
+    capacity = c.table.shape[1] * block if block else c.k.shape[2]
+    for window in (800, capacity, capacity + 1, 2 ** 31 - 200, 2 ** 31 - 1):
+        for sink in (0, 5, 2 ** 31 - 1):
+            c.run(window_keys=window, sink_keys=sink)
+            assert R.workspace_status(c.ws) == 0
+            assert torch.equal(out, c.out) and torch.equal(lse, c.lse), (window, sink)
