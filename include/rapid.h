@@ -447,6 +447,11 @@ typedef struct rapid_kv_rows {
  * ceil(keys / 128) key tiles of one KV head.  A limit has to cover the longest: 10,000 cycles a tile and 100,000 beside are
  * enough (the library's own covers sequences of 25 million keys); a shorter one may end a call that would have gone through.
  */
+
+/*
+ * Bytes of scratch the two calls below need for up to T rows and shape->Lmax keys (Lmax 0: any number of keys); 0 on invalid
+ * arguments.  Strides do not matter.
+ */
 size_t rapid_prefill_attention_workspace_bytes(const rapid_attn_shape* shape, int T);
 
 int rapid_prefill_attention(const void* q, const rapid_kv_rows* q_rows, int T, const int32_t* n_tokens, const void* k_cache,

@@ -987,9 +987,10 @@ def rapid_kv_append_rope_paged(q, k_new, v_new, q_out, k_pool, v_pool, block_tab
         _addr(positions), geometry, status_word.data_ptr(), st))
 
 
-def prefill_attention_workspace_bytes(B, Hq, Hkv, D, T) -> int:
-    """Scratch of rapid_prefill_attention and rapid_prefill_attention_paged for calls of up to T rows per sequence."""
-    s = _AttnShape(B, Hq, Hkv, D, 1, 0, 0, 0)
+def prefill_attention_workspace_bytes(B, Hq, Hkv, D, T, Lmax=None) -> int:
+    """Scratch of rapid_prefill_attention and rapid_prefill_attention_paged for calls of up to T rows per sequence over caches of up to
+    Lmax keys (paged: max_blocks * block_size; None: of any length, which takes the most)."""
+    s = _AttnShape(B, Hq, Hkv, D, 0 if Lmax is None else Lmax, 0, 0, 0)
     return int(load_library().rapid_prefill_attention_workspace_bytes(ctypes.byref(s), T))
 
 

@@ -66,6 +66,7 @@ constexpr float kPieceCost = 2.5f;       // tiles that a piece costs beside its 
 constexpr float kSlotCost = 0.03f;       // tiles that a partial costs the whole call, written and read
 constexpr float kMergeCost = 2.f;        // tiles that it takes to join any
 constexpr int kMaxUnits = 1 << 24;
+constexpr int64_t kMaxKeys = 0x7fffffff - 256;
 
 __host__ __device__ constexpr int k_slots(int D) { return D == 128 ? 2 : 4; }
 __host__ __device__ constexpr int v_slots(int D) { return D == 128 ? 3 : 6; }
@@ -978,7 +979,7 @@ struct WsLayout {
     int max_slots, slot_rows;
 };
 bool shape_ok(const rapid_attn_shape* s, int T) {
-    return s && s->B > 0 && s->Hq > 0 && s->Hkv > 0 && T > 0 && s->Hq % s->Hkv == 0 && (s->D == 64 || s->D == 128) &&
+    return s && s->B > 0 && s->Hq > 0 && s->Hkv > 0 && s->Lmax >= 0 && s->Lmax <= kMaxKeys && T > 0 && s->Hq % s->Hkv == 0 && (s->D == 64 || s->D == 128) &&
            s->Hq / s->Hkv <= 128 && s->B <= 65535 && s->Hkv <= 65535 && T <= (1 << 30);
 }
 int64_t units_of(const rapid_attn_shape* s, int T) {
@@ -1000,7 +1001,9 @@ WsLayout ws_layout(const rapid_attn_shape* s, int T) {
     off += kPlanThreads * sizeof(Cut);
     l.slots = off;
     l.slot_rows = T > 128 / (s->Hq / s->Hkv) ? 256 : 128;
-    l.max_slots = kMaxTail;
+    // partials: no unit of the tail is cut into more than its tiles, and none of one or two tiles is cut
+    const int64_t tiles = ((s->Lmax ? s->Lmax : kMaxKeys) + kKeys - 1) / kKeys, tail = units_of(s, T) < kPlanThreads ? units_of(s, T) : kPlanThreads;
+    l.max_slots = tiles <= 2 ? 0 : tail * tiles < kMaxTail ? (int)(tail * tiles) : kMaxTail;
     off += l.max_slots * slot_floats(l.slot_rows, s->D) * sizeof(float);
     l.total = off;
     return l;
@@ -1042,7 +1045,7 @@ int launch_prefill_attention(const void* q, const rapid_kv_rows* q_rows, int T, 
         return RAPID_ERR_INVALID_ARG;
     }
     const rapid_attn_shape& s = *shape;
-    if (s.B <= 0 || s.Hq <= 0 || s.Hkv <= 0 || s.Lmax <= 0 || T <= 0 || s.Hq % s.Hkv || s.Lmax > 0x7fffffffLL - 256) {
+    if (s.B <= 0 || s.Hq <= 0 || s.Hkv <= 0 || s.Lmax <= 0 || T <= 0 || s.Hq % s.Hkv || s.Lmax > kMaxKeys) {
         set_error("%s: invalid shape (B=%d Hq=%d Hkv=%d Lmax=%lld T=%d)", who, s.B, s.Hq, s.Hkv, (long long)s.Lmax, T);
         return RAPID_ERR_INVALID_ARG;
     }
