@@ -442,7 +442,8 @@ typedef struct rapid_kv_rows {
  * 2^24.  A sequence with a count or a length out of range is left out (its rows stay as they were) and sets
  * RAPID_STATUS_BAD_CTX_LEN.  A row that sees no key is 0, its log-sum-exp -inf.  fp32 accumulation, bf16 probabilities in the
  * second product; lse_out, the range of V, values that are not finite and keys of next to no weight are as in
- * rapid_verify_attention_prefix.  Three kernels per call; lengths are read on the device, so a captured call follows them.
+ * rapid_verify_attention_prefix, for scores (scale * q . k) below 2^23 in size; from 2^30 on, where fp32 sums leave nothing of
+ * a softmax, results need not be finite.  Three kernels per call; lengths are read on the device, so a captured call follows them.
  * wait_cycle_limit: the parts of a CTA hand pieces of work to one another, and wait for as long as a piece takes: a run of up to
  * ceil(keys / 128) key tiles of one KV head.  A limit has to cover the longest: 10,000 cycles a tile and 100,000 beside are
  * enough (the library's own covers sequences of 25 million keys); a shorter one may end a call that would have gone through.
