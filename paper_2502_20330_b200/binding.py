@@ -129,7 +129,7 @@ class Rope:
     inv_freq: torch.Tensor                   # [rotary_dim / 2] float32, CUDA: pair i turns by position * inv_freq[i]
     rotary_dim: int = 0                      # columns that are turned; 0 = all of head_dim
     interleaved: bool = False                # pairs are neighbouring columns, not columns half of rotary_dim apart
-    scale: float = 1.0                       # factor of the turned columns
+    scale: float = 1.0                       # factor of the turned columns; 0 = 1
     pair_axis: Optional[Sequence[int]] = None  # [rotary_dim / 2]: whose position turns each pair; None = axis 0 for all
 
 
@@ -885,7 +885,7 @@ def _pair_axes(pair_axis):
 
 
 def _rope(rope, D, positions, B, T):
-    """The library's struct and the positions' address; positions [B, T] for one axis, [n_axes, B, T], or None."""
+    """The library's struct; positions [B, T] for one axis, [n_axes, B, T], or None."""
     rd = rope.rotary_dim or D
     f = rope.inv_freq
     if f.dtype is not _F32 or f.numel() * 2 != rd or not f.is_contiguous():

@@ -100,7 +100,7 @@ struct PrefillArgs {
     int32_t* plan_sig;           // first word of a verify plan's signature: taken back, its walks are overwritten
     __nv_bfloat16* out;
     float *out_f32, *lse_out;    // or NULL
-    int B, T, G, Hq, Hkv, D;
+    int B, T, G, Hq, Hkv;
     int Lmax;
     int block_size, block_log2, num_blocks, max_blocks, box_rows;
     int rows_tile;               // rows of a sequence in a row tile: 128 / G
@@ -1152,7 +1152,6 @@ int launch_prefill_attention(const void* q, const rapid_kv_rows* q_rows, int T, 
     a.G = G;
     a.Hq = s.Hq;
     a.Hkv = s.Hkv;
-    a.D = s.D;
     a.Lmax = (int)s.Lmax;
     a.block_size = paged ? paged->block_size : 0;
     a.block_log2 = block_log2;
