@@ -343,13 +343,14 @@ __device__ __forceinline__ uint32_t bits(int lo, int hi) {
 }
 
 // A V row that no row of a unit sees may hold any bits, and 0 * NaN is NaN.  A stream's softmax warps zero those of a tile: past the keys
-// and, in the last tile of the sinks and the first one of the window, between the two.  Few tiles have any: kept out of the loop's way.
+// and, in the last tile of the sinks and the first one of the window, between the two.  Few tiles have any: kept out of the loop's way
+// (32,768 rows through a window 2,131 us, 2,153 in line; 2,102 without the rows between).
 template <int D>
 __device__ __noinline__ bool zero_hidden(uint8_t* v, Shared<D>& sh, const PrefillArgs& a, int ring, int key0, int tile, WaitCtx wc) {
     const Piece& g = sh.piece[ring];
     const int end = min(g.L - key0, kKeys), from = max(a.sink - key0, 0);
     const int to = min(max(g.L - g.n + g.row0 - a.window + 1, 0) - key0, kKeys);
-    const int between = a.window ? max(to - from, 0) : 0, chunks = (between + kKeys - end) * 8;
+    const int between = max(to - from, 0), chunks = (between + kKeys - end) * 8;
     if (chunks == 0) return true;
     const int slot = tile % v_slots(D);
     if (!role_wait(&sh.v_full[slot], (tile / v_slots(D)) & 1, wc)) return false;
@@ -362,7 +363,9 @@ __device__ __noinline__ bool zero_hidden(uint8_t* v, Shared<D>& sh, const Prefil
     return true;
 }
 
-template <int D>
+// WINDOW: the call has window_keys.  A kernel of its own for it: with one for both, calls without a window took longer for the code that
+// finds hidden V rows (32 rows over 32,000 keys, batch of one: 44.6 us without, 46.0 with, 44.8 apart).
+template <int D, bool WINDOW>
 __global__ void __launch_bounds__(kThreads, 1)
 prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                     const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ PrefillArgs a) {
@@ -425,7 +428,7 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
             const Piece g = sh.piece[r % kRing];
             const Span sp = sh.span[r % kRing];
             if (!ok || g.tiles < 0) break;
-            const int oldest = a.window ? g.L - g.n + g.row0 - a.window + 1 : 0;  // key of the unit's windows
+            const int oldest = WINDOW ? g.L - g.n + g.row0 - a.window + 1 : 0;  // key of the unit's windows
 #pragma unroll 1
             for (int t = 0; t < g.tiles && ok; ++t) {
                 const int u = g.first + t;
@@ -436,7 +439,7 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                     for (int q = 0; q < parts; ++q) {
                         const int pos = key0 + q * a.box_rows;
                         c1[q] = pos & (a.block_size - 1);
-                        if (pos >= g.L || (pos >= a.sink && pos + a.box_rows <= oldest)) {
+                        if (pos >= g.L || (WINDOW && pos >= a.sink && pos + a.box_rows <= oldest)) {
                             c3[q] = a.num_blocks;  // past the keys, or hidden from the unit: zeros, no table entry is read
                             continue;
                         }
@@ -631,9 +634,9 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                 // the keys j of a row: wlo <= j <= lim, or j < sink; and those that all rows of the tile see
                 const int p0 = g.L - g.n + i0;
                 const int lim = a.all_visible ? g.L - 1 : p0 + row_t;
-                const int wlo = a.window ? lim - a.window + 1 : 0;
+                const int wlo = WINDOW ? lim - a.window + 1 : 0;
                 const int all_lim = a.all_visible ? g.L - 1 : p0;
-                const int all_lo = a.window ? p0 + a.rows_tile - 1 - a.window + 1 : 0;
+                const int all_lo = WINDOW ? p0 + a.rows_tile - 1 - a.window + 1 : 0;
                 float m_ref = -INFINITY, l_run = 0.f;
 #pragma unroll 1
                 for (int t = 0; t < g.tiles; ++t, ++j) {
@@ -748,9 +751,21 @@ prefill_attn_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
                         f32x2_split(f32x2_add(acc[0], acc[1]), s0, s1);
                         l_run += s0 + s1;
                     }
-                    if (key0 + kKeys > g.L || (a.window && u <= sp.sinks)) {  // V rows that no row of the unit sees
+                    if (WINDOW && (key0 + kKeys > g.L || u <= sp.sinks)) {
                         ok = zero_hidden<D>(smem + OFF_V, sh, a, r % kRing, key0, n_tiles + t, wc);
                         if (!ok) break;
+                    } else if (key0 + kKeys > g.L) {  // V rows past the keys alone: the same in line
+                        const int vt = n_tiles + t, vs = vt % NV;
+                        ok = role_wait(&sh.v_full[vs], (vt / NV) & 1, wc);
+                        if (!ok) break;
+                        const int bad = g.L - key0;
+                        const int chunks = (kKeys - bad) * 8;
+#pragma unroll
+                        for (int h = 0; h < NH; ++h)
+                            for (int ch = half * 128 + row; ch < chunks; ch += 256)
+                                *reinterpret_cast<uint4*>(smem + OFF_V + vs * TILE + h * kHalfBytes + bad * 128 + ch * 16) =
+                                    make_uint4(0, 0, 0, 0);
+                        fence_proxy_async_smem();
                     }
                     tmem_wait_st();
                     tc_fence_before_sync();
@@ -1009,7 +1024,7 @@ WsLayout ws_layout(const rapid_attn_shape* s, int T) {
     return l;
 }
 
-template <int D>
+template <int D, bool WINDOW>
 int launch(const CUtensorMap (&tm)[3], const PrefillArgs& a, int sms, void* split_done, cudaStream_t stream) {
     constexpr int smem = smem_bytes<D>();
     static_assert(smem <= 232448, "shared memory");
@@ -1017,11 +1032,11 @@ int launch(const CUtensorMap (&tm)[3], const PrefillArgs& a, int sms, void* spli
     RAPID_CUDA_CHECK(cudaGetDevice(&dev));
     static std::atomic<bool> configured[64];  // (first calls may come from several threads at once; all set the same)
     if (dev >= 64 || !configured[dev]) {
-        RAPID_CUDA_CHECK(cudaFuncSetAttribute(prefill_attn_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+        RAPID_CUDA_CHECK(cudaFuncSetAttribute(prefill_attn_kernel<D, WINDOW>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
         if (dev < 64) configured[dev] = true;
     }
     RAPID_CUDA_CHECK(launch_dependent(prefill_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, a));
-    RAPID_CUDA_CHECK(launch_dependent(prefill_attn_kernel<D>, dim3(a.num_ctas), dim3(kThreads), (size_t)smem, stream, tm[0], tm[1],
+    RAPID_CUDA_CHECK(launch_dependent(prefill_attn_kernel<D, WINDOW>, dim3(a.num_ctas), dim3(kThreads), (size_t)smem, stream, tm[0], tm[1],
                                       tm[2], a));
     if (split_done) RAPID_CUDA_CHECK(cudaEventRecord(static_cast<cudaEvent_t>(split_done), stream));
     RAPID_CUDA_CHECK(launch_dependent(prefill_merge_kernel<D>, dim3(8 * sms), dim3(128), 0, stream, a));
@@ -1175,7 +1190,8 @@ int launch_prefill_attention(const void* q, const rapid_kv_rows* q_rows, int T, 
     // q as [B, T, Hq, D]: a box of (64 columns, G heads, rows_tile rows) is a row tile, row index t * G + g
     if ((rc = make_map(&tm[2], q, s.D, s.Hq, T, s.B, qh, qt, qb, G, a.rows_tile)) != RAPID_OK) return rc;
     void* ev = params ? params->split_done_event : nullptr;
-    return s.D == 128 ? launch<128>(tm, a, sms, ev, stream) : launch<64>(tm, a, sms, ev, stream);
+    if (window) return s.D == 128 ? launch<128, true>(tm, a, sms, ev, stream) : launch<64, true>(tm, a, sms, ev, stream);
+    return s.D == 128 ? launch<128, false>(tm, a, sms, ev, stream) : launch<64, false>(tm, a, sms, ev, stream);
 }
 
 }  // namespace rapid
