@@ -10,6 +10,10 @@
 //   S_s[128 x 128] = Q_s K^T   A = Q tile, B = K tile, both K-major in shared memory
 //   O_s[128 x D]  += P_s V     A = P (bf16, over the first half of S_s's columns), B = V tile, MN-major
 //
+// P is rounded to bf16 because both operands of a product have one type and V is bf16: a probability is off by at most 2^-8 of itself, an
+// output by 2^-8 of the weighted mean of |v| (2.0 - 2.4e-3 of an output's norm for 1.4 - 1.7e-3 with fp32 probabilities).  The row sums add
+// the fp32 probabilities.
+//
 // One thread issues all products, in the order PV_0 QK_0 PV_1 QK_1: while the tensor core is at one stream's, the softmax warps of
 // the other are at theirs.  It works them off in that order, so the QK^T that overwrites S_s goes out right behind the PV that reads P
 // from it, and scores in hand mean that the PV before them has completed.
@@ -30,14 +34,17 @@
 // special-function unit, and take 3,600: a stream's softmax (2,000 cycles) and its products (1,024, and 400 until they are seen) follow
 // one another, and the other stream's fill the gaps only in part.  While it runs for long the 1 kW cap holds the clock at 1.6 - 1.75 GHz.
 // Measured (three kernels, D = 128, calls in a row in a graph):
-//     8,192 rows, 32 heads over 8, causal                            461 us  1.19 PFLOP/s (541 while it runs for long)
-//    32,768 rows, causal                                           7,707 us  1.14
-//    32,768 rows, 4 sinks and a window of 4,092                    2,052 us  1.00
-//       500 rows over 130,000 keys before them, paged in 64        1,039 us  1.03
-//     8 prompts of up to 4,001 rows, 28 over 4, paged in 256       1,105 us  1.01
-//     2 prompts of up to 100 rows, 8 over 2 of 64                   15.3 us  plan, first tiles, last outputs and merge, one after another
-// At D = 64 the special-function unit has as much to do for half of the products: 0.59 PFLOP/s at 16,384 rows.
-// Exponentials as polynomials on the FMA pipe (1 to 4 pairs of 8) gained nothing (8,192 rows 554 us with none, 563 - 599 with some).
+//     8,192 rows, 32 heads over 8, causal                            468 us  1.17 PFLOP/s (547 while it runs for long)
+//    32,768 rows, causal                                           7,928 us  1.11
+//    32,768 rows, 4 sinks and a window of 4,092                    2,088 us  0.99
+//       500 rows over 130,000 keys before them, paged in 64        1,067 us  1.00
+//     8 prompts of up to 4,001 rows, 28 over 4, paged in 256       1,127 us  0.99
+//     2 prompts of up to 100 rows, 8 over 2 of 64                   15.6 us  plan, first tiles, last outputs and merge, one after another
+//       500 rows, all of 65,000 keys visible                         502 us  1.06
+// (boxes differ by up to 4 %).  At D = 64 the special-function unit has as much to do for half of the products: 16,384 rows of 8 heads 454 us,
+// 0.61 PFLOP/s; tensor memory has 128 columns to spare there, which are not used.
+// Exponentials as polynomials on the FMA pipe (1 to 4 pairs of 8) gained nothing at D = 128 (8,192 rows 554 us with none, 563 - 599 with some);
+// at D = 64 they were not tried.  19 warps leave a thread 96 registers; 40 to 52 bytes a thread are spilled.
 //
 // Waits are bounded as everywhere in this library; see mbar_wait_bounded.
 #include <math.h>

@@ -10,8 +10,8 @@
 // Bound: HBM.  Every element is read and written once, 4 bytes; an SM's four blocks of 256 threads have up to 128 KB of reads under way.
 // Four items of 32 bytes a thread at 64 registers: 100 us for two videos of 20,011 tokens at 28/4 heads of 128 (6.5 TB/s), 191 us for
 // prompts of up to 24,000 tokens at 32/8 heads with their append (6.0 TB/s); three items 120 and 224, six 141 and 233, two at six blocks an
-// SM 106 and 187.  Calls of few tokens are a launch and dependent accesses: the rotation 2.5 us (positions and rows, then the stores), an
-// append 3.2 us (lengths, then rows and table entries, then the stores).
+// SM 106 and 187.  Calls of few tokens are a launch and dependent accesses: the rotation 2.6 us (positions and rows, then the stores), an
+// append 3.3 us (lengths, then rows and table entries, then the stores).
 #include <math.h>
 
 #include "common.cuh"
